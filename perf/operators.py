@@ -127,8 +127,9 @@ def draw(rng):
         c = dict(c, Nq=min(N, 3000), Nk=min(N, 3000))
     flops = work(c)["flops"]
     if flops > MOST_FLOPS:
-        N = int(c["Nk"] * (MOST_FLOPS / flops) ** 0.5)
-        c = dict(c, Nq=N, Nk=N)
+        less = (MOST_FLOPS / flops) ** (0.5 if not c["window"] else 1.0)
+        N = int(c["Nk"] * less)
+        c = dict(c, Nq=N, Nk=N, prefix=int(c["prefix"] * less))
     return c
 
 

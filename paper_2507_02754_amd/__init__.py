@@ -11,6 +11,18 @@ interleaves it with dot-product attention (`InterleavedStack`).
 
 from .autograd import SimplicialAttnFunction, simplicial_attention  # noqa: F401
 from .layer import InterleavedStack, SimplicialAttention  # noqa: F401
+from .layers_autograd import TokenLogprobs, dot_attention, norm_rotate, token_logprobs  # noqa: F401
+from .layers_binding import (  # noqa: F401
+    rotary_freqs,
+    simplicial_dot_attn_bwd,
+    simplicial_dot_attn_bwd_workspace_size,
+    simplicial_dot_attn_fwd,
+    simplicial_dot_attn_fwd_workspace_size,
+    simplicial_logprobs_bwd,
+    simplicial_logprobs_fwd,
+    simplicial_norm_rotate_bwd,
+    simplicial_norm_rotate_fwd,
+)
 from .binding import (  # noqa: F401
     DTYPE_BF16,
     DTYPE_F32,

@@ -1,0 +1,110 @@
+// What the dot-product attention kernels share: which keys a query sees, for a
+// single pair and for a block of 32 rows by 32 keys, and the walk over the blocks
+// that hold a visible pair.
+//
+// A row is r = G i + g: query head g of the K-side head's group at query i, at
+// position p = L - Nq + i of the L keys.
+#pragma once
+
+#include "layers_internal.h"
+#include "mfma_common.h"
+
+namespace sa {
+
+constexpr float kInf = __builtin_inff();
+constexpr int kDotBlock = 32;
+
+// One sequence's mask.
+struct DotMask {
+  int L, first;  // keys; position of query 0
+  int prefix, causal, window;
+  const int* docs;  // of this sequence, or null
+  const int2* ranges;
+  __device__ __forceinline__ DotMask(const DotArgs& a, int b) {
+    L = a.lens ? min(max(a.lens[b], 0), a.Nk) : a.Nk;
+    first = L - a.Nq;
+    prefix = a.prefix ? min(a.prefix[b], L) : 0;
+    causal = a.causal;
+    window = a.window;
+    docs = a.docs ? a.docs + static_cast<int64_t>(b) * a.Nk : nullptr;
+    ranges = a.docs ? a.ranges + static_cast<int64_t>(b) * ((a.Nk + kDotBlock - 1) / kDotBlock) : nullptr;
+  }
+  __device__ __forceinline__ int doc(int p) const { return docs && p >= 0 && p < L ? docs[p] : 0; }
+  // Whether the query at p (p < 0: none) sees key j; document numbers dq, dk.
+  __device__ __forceinline__ bool sees(int p, int j, int dq, int dk) const {
+    const bool near = (!causal || j <= p) && (window == 0 || abs(p - j) < window);
+    return (near || j < prefix) && j < L && p >= 0 && (!docs || (dq == dk && dk >= 0));
+  }
+};
+
+// Positions p0 .. p1 of a block's rows or of its keys, and the range of their document
+// numbers.
+struct DotSpan {
+  int p0, p1, dmin, dmax;
+  __device__ __forceinline__ DotSpan(const DotMask& m, int lo, int hi) : p0(lo), p1(hi), dmin(0), dmax(0) {
+    if (m.docs && hi >= 0 && lo < m.L) {
+      const int last = min(hi, m.L - 1) / kDotBlock;
+      const int2 r = m.ranges[max(lo, 0) / kDotBlock];
+      dmin = r.x, dmax = r.y;
+      for (int t = max(lo, 0) / kDotBlock + 1; t <= last; ++t) {
+        const int2 s = m.ranges[t];
+        dmin = min(dmin, s.x), dmax = max(dmax, s.y);
+      }
+    }
+  }
+};
+// Whether any (live), or every (full) query of q sees any / every key of k. live may
+// be true, and full false, of a block for which they need not be.
+__device__ __forceinline__ bool dot_live(const DotMask& m, const DotSpan& q, const DotSpan& k) {
+  const bool near = (!m.causal || k.p0 <= q.p1) &&
+                    (m.window == 0 || (k.p1 > max(q.p0, 0) - m.window && (m.causal || k.p0 < q.p1 + m.window)));
+  return (near || k.p0 < m.prefix) && k.p0 < m.L && q.p1 >= 0 &&
+         (!m.docs || (k.dmax >= 0 && q.dmax >= k.dmin && k.dmax >= q.dmin));
+}
+__device__ __forceinline__ bool dot_full(const DotMask& m, const DotSpan& q, const DotSpan& k) {
+  const bool near = (!m.causal || k.p1 <= q.p0) &&
+                    (m.window == 0 || (q.p1 - k.p0 < m.window && (m.causal || k.p1 - q.p0 < m.window)));
+  return (near || k.p1 < m.prefix) && k.p1 < m.L && q.p0 >= 0 &&
+         (!m.docs || (k.dmin == k.dmax && q.dmin == q.dmax && k.dmin == q.dmin && k.dmin >= 0));
+}
+// Key blocks that any of the rows may see: [lo, hi).
+__device__ __forceinline__ void key_blocks(const DotMask& m, const DotSpan& q, int& lo, int& hi) {
+  const int from = m.window && m.prefix <= 0 ? max(max(q.p0, 0) - m.window + 1, 0) : 0;
+  const int to = m.causal ? min(max(q.p1 + 1, m.prefix), m.L) : m.L;
+  lo = from / kDotBlock;
+  hi = q.p1 < 0 ? lo : (to + kDotBlock - 1) / kDotBlock;
+}
+// Row blocks that may see any of the keys (G rows a position, R rows): [lo, hi).
+__device__ __forceinline__ void row_blocks(const DotMask& m, const DotSpan& k, int G, int R, int& lo, int& hi) {
+  const bool all = k.p0 < m.prefix;
+  int from = max(-m.first, 0), to = R / G;  // queries
+  if (!all && m.causal) from = max(from, k.p0 - m.first);
+  if (!all && m.window) {
+    to = static_cast<int>(min(static_cast<int64_t>(to), static_cast<int64_t>(k.p1) + m.window - m.first));
+    if (!m.causal) from = max(from, k.p0 - m.window + 1 - m.first);
+  }
+  lo = static_cast<int>(static_cast<int64_t>(from) * G / kDotBlock);
+  hi = k.p0 >= m.L || to <= from ? lo : static_cast<int>((static_cast<int64_t>(to) * G + kDotBlock - 1) / kDotBlock);
+}
+
+// Walks the blocks lo + off, lo + off + step, .. < hi that are live: 64 at a time are
+// looked at, one a lane. test(block, live, full) and body(block, full), all wavefront-uniform
+// but for test's block.
+template <typename Test, typename Body>
+__device__ __forceinline__ void walk_blocks(int lo, int hi, int off, int step, Test test, Body body) {
+  const int lane = threadIdx.x & 63;
+  const int count = lo + off < hi ? (hi - lo - off + step - 1) / step : 0;
+  for (int n0 = 0; n0 < count; n0 += 64) {
+    bool live = false, full = false;
+    if (n0 + lane < count) test(lo + off + (n0 + lane) * step, live, full);
+    unsigned long long todo = __builtin_amdgcn_ballot_w64(live);
+    const unsigned long long whole = __builtin_amdgcn_ballot_w64(full);
+    while (todo) {
+      const int i = __builtin_ctzll(todo);
+      todo &= todo - 1;
+      body(lo + off + (n0 + i) * step, static_cast<bool>((whole >> i) & 1));
+    }
+  }
+}
+
+}  // namespace sa

@@ -1,0 +1,317 @@
+// C-ABI entry points of include/simplicial_layers.h: argument validation (host
+// only, before any HIP call) and error mapping.
+#include "simplicial_layers.h"
+
+#include <limits.h>
+#include <math.h>
+
+#include <initializer_list>
+
+#include "layers_internal.h"
+
+namespace {
+
+bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+// Pointers that may not be null, 16-byte aligned as all of the library's.
+bool good(std::initializer_list<const void*> ptrs) {
+  for (const void* p : ptrs)
+    if (!p || !aligned(p, 16)) return false;
+  return true;
+}
+bool good_or_null(std::initializer_list<const void*> ptrs) {
+  for (const void* p : ptrs)
+    if (!aligned(p, 4)) return false;
+  return true;
+}
+int to_status(hipError_t e) { return e == hipSuccess ? SA_OK : SA_ERR_HIP; }
+int element_size(int32_t dtype) { return dtype == SA_DTYPE_F32 ? 4 : 2; }
+bool known(int32_t dtype) { return dtype == SA_DTYPE_F32 || dtype == SA_DTYPE_BF16; }
+bool known_dim(int64_t D) { return D == 16 || D == 32 || D == 64 || D == 128; }
+
+// a * b * c within `most` (all positive).
+bool product_fits(int64_t a, int64_t b, int64_t c, int64_t most) { return a <= most / b && a * b <= most / c; }
+
+constexpr int64_t kElements = int64_t(1) << 40;  // of a tensor
+
+// A view's strides: not negative, its rows 16-byte aligned.
+bool good_stride(int64_t s, int32_t dtype) { return s >= 0 && s <= kElements && s * element_size(dtype) % 16 == 0; }
+
+// ---- norm and rotation ----
+
+int check_rotate(int32_t count, const void* const* x, const int64_t* strides, const int32_t* heads,
+                 const int64_t* positions, int64_t pos_stride, int64_t B, int64_t N, int64_t D, int32_t norm,
+                 float eps, int32_t layout, const double* freqs, int32_t nfreq, int32_t dtype, int32_t wdtype,
+                 const void* const* weight) {
+  if (count < 1 || count > SA_ROTATE_MAX || !x || !strides || !heads) return SA_ERR_INVALID;
+  if (B <= 0 || N <= 0 || D <= 0 || B > INT_MAX || N > INT_MAX || !product_fits(B, N, 1, INT_MAX)) return SA_ERR_INVALID;
+  if (!known(dtype) || !known(wdtype) || !known_dim(D)) return SA_ERR_UNSUPPORTED;
+  int64_t all = 0;
+  for (int t = 0; t < count; ++t) {
+    if (!good({x[t]}) || heads[t] < 1) return SA_ERR_INVALID;
+    for (int i = 0; i < 3; ++i)
+      if (!good_stride(strides[3 * t + i], dtype)) return SA_ERR_INVALID;
+    if (weight && weight[t] && (!norm || !aligned(weight[t], 4))) return SA_ERR_INVALID;
+    all += heads[t];
+  }
+  // A launch holds less than 2^32 threads (D / 16 a position), a tensor 2^40 elements.
+  if (all > INT_MAX || B * N > (INT_MAX / (D / 16)) || !product_fits(B * N, all, D, kElements)) return SA_ERR_INVALID;
+  if (!aligned(positions, 8) || pos_stride < 0 || (positions && pos_stride != 0 && pos_stride < N)) return SA_ERR_INVALID;
+  if (norm && !(isfinite(eps) && eps >= 0.f)) return SA_ERR_INVALID;
+  if (layout != SA_ROTATE_HALF && layout != SA_ROTATE_PAIRS && layout != SA_ROTATE_AXIS) return SA_ERR_INVALID;
+  if (nfreq < 0 || nfreq > (layout == SA_ROTATE_AXIS ? D / 3 : D / 2) || (nfreq && !freqs)) return SA_ERR_INVALID;
+  if (layout == SA_ROTATE_HALF && nfreq % 8 != 0) return SA_ERR_UNSUPPORTED;
+  for (int i = 0; i < nfreq; ++i)
+    if (!isfinite(freqs[i])) return SA_ERR_INVALID;
+  return SA_OK;
+}
+
+sa::RotArgs rotate_args(int32_t count, const void* const* x, const int64_t* strides, const void* const* weight,
+                        const int32_t* heads, const int64_t* positions, int64_t pos_stride, int64_t start, int64_t B,
+                        int64_t N, int64_t D, int32_t norm, float eps, int32_t layout, const double* freqs,
+                        int32_t nfreq, int32_t dtype, int32_t wdtype) {
+  sa::RotArgs a = {};
+  for (int t = 0; t < count; ++t) {
+    a.x[t] = x[t];
+    a.w[t] = weight ? weight[t] : nullptr;
+    a.sb[t] = strides[3 * t], a.sn[t] = strides[3 * t + 1], a.sh[t] = strides[3 * t + 2];
+    a.heads[t] = heads[t];
+  }
+  a.count = count;
+  a.pos = positions, a.pos_stride = pos_stride, a.start = start;
+  a.B = static_cast<int>(B), a.N = static_cast<int>(N), a.D = static_cast<int>(D);
+  a.norm = norm != 0, a.eps = eps, a.layout = layout, a.nfreq = nfreq, a.dtype = dtype, a.wdtype = wdtype;
+  for (int i = 0; i < nfreq; ++i) a.turns[i] = freqs[i] * 0.15915494309189533577;  // 1 / 2 pi
+  return a;
+}
+
+// ---- dot-product attention ----
+
+int check_dot(int64_t B, int64_t Nq, int64_t Nk, int64_t H, int64_t Hkv, int64_t D, int32_t window, int32_t dtype) {
+  if (B <= 0 || Nq <= 0 || Nk <= 0 || H <= 0 || Hkv <= 0 || D <= 0 || Nq > Nk || window < 0) return SA_ERR_INVALID;
+  if (Hkv > H || H % Hkv != 0) return SA_ERR_INVALID;
+  // Rows of a sequence and positions are 32-bit numbers, and a launch holds less than
+  // 2^32 threads, 256 for each block of 32 rows or keys.
+  const int64_t rows = int64_t(1) << 30, blocks = int64_t(1) << 23;
+  if (Nk > rows || B > rows || H > rows || !product_fits(H / Hkv, Nk, 1, rows)) return SA_ERR_INVALID;
+  if (!product_fits(B, Hkv, (H / Hkv * Nk + 31) / 32, blocks)) return SA_ERR_INVALID;
+  if (!known(dtype) || !known_dim(D)) return SA_ERR_UNSUPPORTED;
+  return SA_OK;
+}
+// A block of 32 rows is read through 32-bit offsets: its positions and all heads
+// within 2^31 bytes.
+bool block_fits(int64_t sn, int64_t sh, int64_t heads, int64_t D, int32_t dtype) {
+  const int64_t most = (int64_t(1) << 31) / element_size(dtype);
+  return sn < most / 64 && sh < most / 4 && 33 * sn + (heads - 1) * sh + D < most && (heads - 1) <= most / (sh ? sh : 1);
+}
+
+struct DotCall {
+  int64_t B, Nq, Nk, H, Hkv, D, st[9];
+  float scale, softcap;
+  int32_t causal, window;
+  const float* slopes;
+  const int32_t *documents, *prefix, *k_lens;
+  int32_t dtype;
+};
+int check_dot_call(const DotCall& c) {
+  const int rc = check_dot(c.B, c.Nq, c.Nk, c.H, c.Hkv, c.D, c.window, c.dtype);
+  if (rc != SA_OK) return rc;
+  if (!isfinite(c.scale) || !isfinite(c.softcap) || c.softcap < 0.f) return SA_ERR_INVALID;
+  for (int64_t s : c.st)
+    if (!good_stride(s, c.dtype)) return SA_ERR_INVALID;
+  if (!block_fits(c.st[1], c.st[2], c.H, c.D, c.dtype) || !block_fits(c.st[4], c.st[5], 1, c.D, c.dtype) ||
+      !block_fits(c.st[7], c.st[8], 1, c.D, c.dtype) || !block_fits(c.H * c.D, c.D, c.H, c.D, c.dtype))
+    return SA_ERR_UNSUPPORTED;
+  return good_or_null({c.slopes, c.documents, c.prefix, c.k_lens}) ? SA_OK : SA_ERR_INVALID;
+}
+sa::DotArgs dot_args(const DotCall& c, const void* q, const void* k, const void* v) {
+  sa::DotArgs a = {};
+  a.q = q, a.k = k, a.v = v;
+  a.qsb = c.st[0], a.qsn = c.st[1], a.qsh = c.st[2];
+  a.ksb = c.st[3], a.ksn = c.st[4], a.ksh = c.st[5];
+  a.vsb = c.st[6], a.vsn = c.st[7], a.vsh = c.st[8];
+  a.B = static_cast<int>(c.B), a.Nq = static_cast<int>(c.Nq), a.Nk = static_cast<int>(c.Nk), a.H = static_cast<int>(c.H);
+  a.Hkv = static_cast<int>(c.Hkv), a.D = static_cast<int>(c.D), a.G = a.H / a.Hkv;
+  a.scale = c.scale, a.cap = c.softcap, a.causal = c.causal != 0;
+  a.window = c.window >= c.Nk ? 0 : c.window;  // (no distance reaches Nk)
+  a.slopes = c.slopes, a.docs = c.documents, a.prefix = c.prefix, a.lens = c.k_lens;
+  a.dtype = c.dtype;
+  return a;
+}
+
+}  // namespace
+
+extern "C" {
+
+int simplicial_norm_rotate_fwd(int32_t count, const void* const* x, const int64_t* strides,
+                               const void* const* weight, void* const* y, const int32_t* heads,
+                               const int64_t* positions, int64_t pos_stride, int64_t start, int64_t B,
+                               int64_t N, int64_t D, int32_t norm, float eps, int32_t layout,
+                               const double* freqs, int32_t nfreq, int32_t dtype, int32_t wdtype,
+                               void* stream) {
+  const int rc = check_rotate(count, x, strides, heads, positions, pos_stride, B, N, D, norm, eps, layout, freqs,
+                              nfreq, dtype, wdtype, weight);
+  if (rc != SA_OK) return rc;
+  if (!y) return SA_ERR_INVALID;
+  sa::RotArgs a = rotate_args(count, x, strides, weight, heads, positions, pos_stride, start, B, N, D, norm, eps,
+                              layout, freqs, nfreq, dtype, wdtype);
+  for (int t = 0; t < count; ++t) {
+    if (!good({y[t]})) return SA_ERR_INVALID;
+    a.y[t] = y[t];
+  }
+  return to_status(sa::rotate_fwd(a, static_cast<hipStream_t>(stream)));
+}
+
+size_t simplicial_norm_rotate_bwd_workspace_size(int32_t count, int64_t B, int64_t N, int64_t D) {
+  if (count < 1 || count > SA_ROTATE_MAX || B <= 0 || N <= 0 || !known_dim(D)) return 0;
+  return sa::rotate_bwd_bytes(count, B, N, D);
+}
+
+int simplicial_norm_rotate_bwd(int32_t count, const void* const* x, const int64_t* strides,
+                               const void* const* weight, const void* const* dy, void* const* dx,
+                               void* const* dweight, const int32_t* heads, const int64_t* positions,
+                               int64_t pos_stride, int64_t start, void* workspace,
+                               size_t workspace_bytes, int64_t B, int64_t N, int64_t D, int32_t norm,
+                               float eps, int32_t layout, const double* freqs, int32_t nfreq,
+                               int32_t dtype, int32_t wdtype, void* stream) {
+  const int rc = check_rotate(count, x, strides, heads, positions, pos_stride, B, N, D, norm, eps, layout, freqs,
+                              nfreq, dtype, wdtype, weight);
+  if (rc != SA_OK) return rc;
+  if (!dy || !dx) return SA_ERR_INVALID;
+  sa::RotArgs a = rotate_args(count, x, strides, weight, heads, positions, pos_stride, start, B, N, D, norm, eps,
+                              layout, freqs, nfreq, dtype, wdtype);
+  bool dw = false;
+  for (int t = 0; t < count; ++t) {
+    if (!good({dy[t], dx[t]})) return SA_ERR_INVALID;
+    a.dy[t] = dy[t];
+    a.y[t] = dx[t];
+    a.dw[t] = dweight ? dweight[t] : nullptr;
+    if (a.dw[t] && (!norm || !aligned(a.dw[t], 4))) return SA_ERR_INVALID;
+    dw = dw || a.dw[t];
+  }
+  if (dw) {
+    if (!good({workspace})) return SA_ERR_INVALID;
+    if (workspace_bytes < sa::rotate_bwd_bytes(count, B, N, D)) return SA_ERR_WORKSPACE;
+  }
+  return to_status(sa::rotate_bwd(a, dw ? static_cast<float*>(workspace) : nullptr, static_cast<hipStream_t>(stream)));
+}
+
+size_t simplicial_dot_attn_fwd_workspace_size(int64_t B, int64_t Nq, int64_t Nk, int64_t H,
+                                              int64_t Hkv, int64_t D, int32_t causal, int32_t window,
+                                              int32_t has_documents, int32_t dtype) {
+  if (check_dot(B, Nq, Nk, H, Hkv, D, window, dtype) != SA_OK) return 0;
+  return sa::dot_fwd_plan(B, Nq, Nk, H, Hkv, D, causal, window, has_documents != 0, dtype).bytes;
+}
+
+int simplicial_dot_attn_fwd(const void* q, const void* k, const void* v, void* out, float* lse,
+                            void* workspace, size_t workspace_bytes, int64_t B, int64_t Nq, int64_t Nk,
+                            int64_t H, int64_t Hkv, int64_t D, int64_t q_sb, int64_t q_sn, int64_t q_sh,
+                            int64_t k_sb, int64_t k_sn, int64_t k_sh, int64_t v_sb, int64_t v_sn,
+                            int64_t v_sh, float scale, float softcap, int32_t causal, int32_t window,
+                            const float* slopes, const int32_t* documents, const int32_t* prefix,
+                            const int32_t* k_lens, int32_t dtype, void* stream) {
+  const DotCall c = {B, Nq, Nk, H, Hkv, D, {q_sb, q_sn, q_sh, k_sb, k_sn, k_sh, v_sb, v_sn, v_sh}, scale, softcap,
+                     causal, window, slopes, documents, prefix, k_lens, dtype};
+  if (!good({q, k, v, out, lse})) return SA_ERR_INVALID;
+  const int rc = check_dot_call(c);
+  if (rc != SA_OK) return rc;
+  const sa::DotPlan p = sa::dot_fwd_plan(B, Nq, Nk, H, Hkv, D, causal, window, documents != nullptr, dtype);
+  if (p.bytes && !good({workspace})) return SA_ERR_INVALID;
+  if (workspace_bytes < p.bytes) return SA_ERR_WORKSPACE;
+  sa::DotArgs a = dot_args(c, q, k, v);
+  a.out = out, a.lse = lse;
+  char* ws = static_cast<char*>(workspace);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  a.nsplit = p.nsplit;
+  a.part = reinterpret_cast<float*>(ws + p.part_off);
+  if (documents) {
+    int2* ranges = reinterpret_cast<int2*>(ws + p.ranges_off);
+    const int r = to_status(sa::dot_ranges(a, ranges, st));
+    if (r != SA_OK) return r;
+    a.ranges = ranges;
+  }
+  return to_status(sa::dot_fwd_f32(a, st));
+}
+
+size_t simplicial_dot_attn_bwd_workspace_size(int64_t B, int64_t Nq, int64_t Nk, int64_t H,
+                                              int64_t Hkv, int64_t D, int32_t causal, int32_t window,
+                                              int32_t has_documents, int32_t dtype) {
+  if (check_dot(B, Nq, Nk, H, Hkv, D, window, dtype) != SA_OK) return 0;
+  return sa::dot_bwd_plan(B, Nq, Nk, H, Hkv, D, causal, window, has_documents != 0, dtype).bytes;
+}
+
+int simplicial_dot_attn_bwd(const void* q, const void* k, const void* v, const void* out,
+                            const void* dout, const float* lse, void* dq, void* dk, void* dv,
+                            void* workspace, size_t workspace_bytes, int64_t B, int64_t Nq, int64_t Nk,
+                            int64_t H, int64_t Hkv, int64_t D, int64_t q_sb, int64_t q_sn, int64_t q_sh,
+                            int64_t k_sb, int64_t k_sn, int64_t k_sh, int64_t v_sb, int64_t v_sn,
+                            int64_t v_sh, float scale, float softcap, int32_t causal, int32_t window,
+                            const float* slopes, const int32_t* documents, const int32_t* prefix,
+                            const int32_t* k_lens, int32_t dtype, void* stream) {
+  const DotCall c = {B, Nq, Nk, H, Hkv, D, {q_sb, q_sn, q_sh, k_sb, k_sn, k_sh, v_sb, v_sn, v_sh}, scale, softcap,
+                     causal, window, slopes, documents, prefix, k_lens, dtype};
+  if (!good({q, k, v, out, dout, lse, dq, dk, dv, workspace})) return SA_ERR_INVALID;
+  const int rc = check_dot_call(c);
+  if (rc != SA_OK) return rc;
+  const sa::DotPlan p = sa::dot_bwd_plan(B, Nq, Nk, H, Hkv, D, causal, window, documents != nullptr, dtype);
+  if (workspace_bytes < p.bytes) return SA_ERR_WORKSPACE;
+  sa::DotArgs a = dot_args(c, q, k, v);
+  a.out_in = out, a.dout = dout, a.lse = const_cast<float*>(lse);
+  a.dq = dq, a.dk = dk, a.dv = dv;
+  char* ws = static_cast<char*>(workspace);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  a.delta = reinterpret_cast<float*>(ws + p.part_off);
+  if (documents) {
+    int2* ranges = reinterpret_cast<int2*>(ws + p.ranges_off);
+    const int r = to_status(sa::dot_ranges(a, ranges, st));
+    if (r != SA_OK) return r;
+    a.ranges = ranges;
+  }
+  return to_status(sa::dot_bwd_f32(a, st));
+}
+
+// A launch holds less than 2^32 threads: at least 64 a row, 1024 logits for every 64 of a long one.
+static bool rows_fit(int64_t R, int64_t V) { return R <= (1 << 25) && product_fits(R, V, 1, int64_t(1) << 35); }
+
+static int check_logprobs(const void* logits, const int64_t* targets, int64_t R, int64_t V, int64_t row_stride,
+                          int32_t dtype) {
+  if (R <= 0 || V <= 0 || row_stride < V || row_stride > kElements) return SA_ERR_INVALID;
+  if (!known(dtype)) return SA_ERR_UNSUPPORTED;
+  if (!logits || !aligned(logits, element_size(dtype)) || !targets || !aligned(targets, 8)) return SA_ERR_INVALID;
+  // (64 slices of a row, workgroups in 32 bits)
+  if (V > 4000000) return SA_ERR_UNSUPPORTED;
+  return rows_fit(R, V) ? SA_OK : SA_ERR_INVALID;
+}
+
+size_t simplicial_logprobs_fwd_workspace_size(int64_t R, int64_t V, int32_t top, int32_t dtype) {
+  if (R <= 0 || V <= 0 || V > 4000000 || !rows_fit(R, V) || !known(dtype) || top < 0 || top > SA_LOGPROBS_MAX_TOP || top > V) return 0;
+  return sa::logprobs_fwd_bytes(R, V, top, dtype);
+}
+
+int simplicial_logprobs_fwd(const void* logits, const int64_t* targets, float* logprob,
+                            float* entropy, float* lse, float* top_logprob, int64_t* top_index,
+                            void* workspace, size_t workspace_bytes, int64_t R, int64_t V,
+                            int64_t row_stride, int32_t top, int32_t dtype, void* stream) {
+  const int rc = check_logprobs(logits, targets, R, V, row_stride, dtype);
+  if (rc != SA_OK) return rc;
+  if (top < 0 || top > SA_LOGPROBS_MAX_TOP || top > V) return SA_ERR_INVALID;
+  if (!logprob || !entropy || !lse || !good_or_null({logprob, entropy, lse, top_logprob}) || !aligned(top_index, 8)) return SA_ERR_INVALID;
+  if (top && (!top_logprob || !top_index)) return SA_ERR_INVALID;
+  const size_t need = sa::logprobs_fwd_bytes(R, V, top, dtype);
+  if (need && !good({workspace})) return SA_ERR_INVALID;
+  if (workspace_bytes < need) return SA_ERR_WORKSPACE;
+  const sa::LogprobArgs a = {logits, targets, logprob, entropy, lse, top_logprob, top_index, R, V, row_stride, top, dtype};
+  return to_status(sa::logprobs_fwd(a, workspace, static_cast<hipStream_t>(stream)));
+}
+
+int simplicial_logprobs_bwd(const void* logits, const int64_t* targets, const float* lse,
+                            const float* entropy, const float* d_logprob, const float* d_entropy,
+                            const float* d_lse, void* dlogits, int64_t R, int64_t V,
+                            int64_t row_stride, int32_t dtype, void* stream) {
+  const int rc = check_logprobs(logits, targets, R, V, row_stride, dtype);
+  if (rc != SA_OK) return rc;
+  if (!lse || !entropy || !good({dlogits}) || !good_or_null({lse, entropy, d_logprob, d_entropy, d_lse})) return SA_ERR_INVALID;
+  const sa::LogprobGrad a = {logits, targets, lse, entropy, d_logprob, d_entropy, d_lse, dlogits, R, V, row_stride, dtype};
+  return to_status(sa::logprobs_bwd(a, static_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"

@@ -1,0 +1,90 @@
+// Internal declarations of the operators of include/simplicial_layers.h (host
+// launchers; layers_api.hip validates their arguments and maps their errors).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace sa {
+
+// ---- norm_rotate.hip ----
+constexpr int kRotTensors = 3;
+constexpr int kRotFreqs = 64;
+struct RotArgs {
+  const void* x[kRotTensors];
+  const void* w[kRotTensors];   // [D] or null
+  const void* dy[kRotTensors];  // backward
+  void* y[kRotTensors];         // forward: y, backward: dx
+  void* dw[kRotTensors];        // backward: [D] or null
+  int64_t sb[kRotTensors], sn[kRotTensors], sh[kRotTensors];
+  int heads[kRotTensors];
+  int count;
+  const int64_t* pos;
+  int64_t pos_stride, start;
+  int B, N, D, norm, nfreq, layout, dtype, wdtype;
+  float eps;
+  double turns[kRotFreqs];  // turns per position: freqs / 2 pi
+};
+hipError_t rotate_fwd(const RotArgs& a, hipStream_t st);
+size_t rotate_bwd_bytes(int count, int64_t B, int64_t N, int64_t D);
+hipError_t rotate_bwd(const RotArgs& a, float* part, hipStream_t st);
+
+// ---- logprobs.hip ----
+struct LogprobArgs {
+  const void* x;
+  const int64_t* targets;
+  float *logprob, *entropy, *lse, *top_logprob;
+  int64_t* top_index;
+  int64_t R, V, stride;
+  int top, dtype;
+};
+size_t logprobs_fwd_bytes(int64_t R, int64_t V, int top, int dtype);
+hipError_t logprobs_fwd(const LogprobArgs& a, void* workspace, hipStream_t st);
+struct LogprobGrad {
+  const void* x;
+  const int64_t* targets;
+  const float *lse, *entropy, *d_logprob, *d_entropy, *d_lse;
+  void* dx;
+  int64_t R, V, stride;
+  int dtype;
+};
+hipError_t logprobs_bwd(const LogprobGrad& a, hipStream_t st);
+
+// ---- dot_f32.hip, dot_mfma.hip ----
+// Dot-product attention. A K-side head's rows are its G = H / Hkv query heads at
+// every position, r = G i + g: one position's heads share their keys.
+struct DotArgs {
+  const void *q, *k, *v, *dout;
+  const void* out_in;  // backward: O
+  void* out;
+  float* lse;  // forward: written, backward: read
+  void *dq, *dk, *dv;
+  int64_t qsb, qsn, qsh, ksb, ksn, ksh, vsb, vsn, vsh;
+  int B, Nq, Nk, H, Hkv, D, G;
+  float scale, cap;
+  int causal, window;  // window 0: none
+  const float* slopes;
+  const int* docs;
+  const int* prefix;
+  const int* lens;
+  // Smallest and largest document number of every 32 positions, [B, ceil(Nk / 32)].
+  const int2* ranges;
+  float* delta;  // backward: Delta [B, H, Nq]
+  int nsplit;    // forward: parts of the key axis
+  float* part;   // forward, nsplit > 1: their partial results
+  int dtype;
+};
+struct DotPlan {
+  int nsplit;
+  size_t ranges_off, part_off, bytes;
+};
+DotPlan dot_fwd_plan(int64_t B, int64_t Nq, int64_t Nk, int64_t H, int64_t Hkv, int64_t D, int causal, int window,
+                     bool docs, int dtype);
+DotPlan dot_bwd_plan(int64_t B, int64_t Nq, int64_t Nk, int64_t H, int64_t Hkv, int64_t D, int causal, int window,
+                     bool docs, int dtype);
+hipError_t dot_ranges(const DotArgs& a, int2* ranges, hipStream_t st);
+hipError_t dot_fwd_f32(const DotArgs& a, hipStream_t st);
+hipError_t dot_bwd_f32(const DotArgs& a, hipStream_t st);
+
+}  // namespace sa

@@ -1,0 +1,370 @@
+"""ctypes binding of the entry points of include/simplicial_layers.h (argument
+marshalling only), in the manner of `binding`: tensors are checked for device,
+dtype, layout and shape, outputs and workspaces are allocated with torch, and the
+raw pointers plus torch's current HIP stream on the tensors' device go to the
+library. There is no fallback implementation.
+"""
+
+import ctypes
+import functools
+
+import torch
+
+from .binding import _DTYPES, SimplicialAttnError, _stream, load_library
+
+__all__ = [
+    "rotary_freqs",
+    "simplicial_norm_rotate_fwd",
+    "simplicial_norm_rotate_bwd",
+    "simplicial_dot_attn_fwd",
+    "simplicial_dot_attn_fwd_workspace_size",
+    "simplicial_dot_attn_bwd",
+    "simplicial_dot_attn_bwd_workspace_size",
+    "simplicial_logprobs_fwd",
+    "simplicial_logprobs_bwd",
+]
+
+ROTATE_LAYOUTS = {"half": 0, "pairs": 1, "axis": 2}
+ROTATE_MAX = 3
+LOGPROBS_MAX_TOP = 32
+
+_lib = None
+
+
+def _library():
+    """The library with this module's entry points declared."""
+    global _lib
+    if _lib is not None:
+        return _lib
+    lib = load_library()
+    vp, i64, i32, f32, size = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_float, ctypes.c_size_t
+    lib.simplicial_norm_rotate_fwd.argtypes = [i32] + [vp] * 5 + [vp, i64, i64, i64, i64, i64, i32, f32, i32, vp, i32,
+                                                                  i32, i32, vp]
+    lib.simplicial_norm_rotate_bwd.argtypes = [i32] + [vp] * 7 + [vp, i64, i64, vp, size, i64, i64, i64, i32, f32, i32,
+                                                                  vp, i32, i32, i32, vp]
+    lib.simplicial_norm_rotate_bwd_workspace_size.argtypes = [i32, i64, i64, i64]
+    dot = [i64] * 15 + [f32, f32, i32, i32] + [vp] * 4 + [i32, vp]
+    lib.simplicial_dot_attn_fwd.argtypes = [vp] * 6 + [size] + dot
+    lib.simplicial_dot_attn_bwd.argtypes = [vp] * 10 + [size] + dot
+    lib.simplicial_logprobs_fwd.argtypes = [vp] * 8 + [size, i64, i64, i64, i32, i32, vp]
+    lib.simplicial_logprobs_bwd.argtypes = [vp] * 8 + [i64, i64, i64, i32, vp]
+    for name in ("norm_rotate_fwd", "norm_rotate_bwd", "dot_attn_fwd", "dot_attn_bwd", "logprobs_fwd", "logprobs_bwd"):
+        getattr(lib, "simplicial_" + name).restype = ctypes.c_int
+    for name in ("dot_attn_fwd", "dot_attn_bwd"):
+        f = getattr(lib, f"simplicial_{name}_workspace_size")
+        f.argtypes = [i64] * 6 + [i32] * 4
+        f.restype = size
+    lib.simplicial_logprobs_fwd_workspace_size.argtypes = [i64, i64, i32, i32]
+    lib.simplicial_logprobs_fwd_workspace_size.restype = size
+    lib.simplicial_norm_rotate_bwd_workspace_size.restype = size
+    _lib = lib
+    return lib
+
+
+def _call(entry, device, *args):
+    """The entry point on the device's current stream, with that device current."""
+    f = getattr(_lib or _library(), entry)
+    if device.index == torch.cuda.current_device():
+        rc = f(*args, _stream(device))
+    else:
+        with torch.cuda.device(device):
+            rc = f(*args, _stream(device))
+    if rc != 0:
+        raise SimplicialAttnError(rc, entry)
+
+
+def _workspace(nbytes, device):
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _check_view(t, name, like=None):
+    """A [B, N, heads, D] GPU tensor of a supported dtype with unit innermost stride."""
+    if t.dim() != 4:
+        raise ValueError(f"{name} must be [B, N, heads, D], got shape {tuple(t.shape)}")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor")
+    if t.dtype not in _DTYPES:
+        raise ValueError(f"{name}: unsupported dtype {t.dtype}; expected float32 or bfloat16")
+    if t.numel() == 0:
+        raise ValueError(f"{name} is empty: shape {tuple(t.shape)}")
+    if t.stride(3) != 1:
+        raise ValueError(f"{name} must be contiguous in its last dimension")
+    if like is not None and (t.dtype != like.dtype or t.device != like.device):
+        raise ValueError(f"{name} has {t.dtype} on {t.device}, expected {like.dtype} on {like.device}")
+
+
+def _strides(t):
+    """Batch, position and head strides; 0 along a dimension of one element, whose stride says nothing."""
+    s, n = t.stride(), t.shape
+    return (s[0] if n[0] > 1 else 0, s[1] if n[1] > 1 else 0, s[2] if n[2] > 1 else 0)
+
+
+def _check_like(t, shape, dtype, device, name):
+    if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, got "
+                         f"{t.dtype} {tuple(t.shape)} on {t.device}")
+
+
+# ---- norm and rotation ----
+
+
+def rotary_freqs(count, base=10000.0):
+    """`count` angles per position, base^(-i / count): the geometric series of a
+    rotation with `count` pairs."""
+    return tuple(float(base) ** (-i / count) for i in range(count))
+
+
+@functools.lru_cache(maxsize=64)
+def _freq_array(freqs):
+    return (ctypes.c_double * max(len(freqs), 1))(*freqs)
+
+
+def _rotate_args(xs, weights, eps, freqs, layout, positions, start):
+    """Checked arguments shared by forward and backward: (count, strides, weights, heads, middle, tail, wdtype)."""
+    n = len(xs)
+    if not 1 <= n <= ROTATE_MAX:
+        raise ValueError(f"1 to {ROTATE_MAX} tensors, got {n}")
+    x0 = xs[0]
+    for t, x in enumerate(xs):
+        _check_view(x, f"x[{t}]", x0)
+        if x.shape[:2] != x0.shape[:2] or x.shape[3] != x0.shape[3]:
+            raise ValueError(f"x[{t}] has shape {tuple(x.shape)}, expected [B, N, heads, D] of {tuple(x0.shape)}")
+    B, N, _, D = x0.shape
+    if layout not in ROTATE_LAYOUTS:
+        raise ValueError(f"layout {layout!r}; expected one of {', '.join(ROTATE_LAYOUTS)}")
+    wdtype = torch.float32
+    if weights is not None:
+        if len(weights) != n:
+            raise ValueError(f"{len(weights)} weights for {n} tensors")
+        given = [w for w in weights if w is not None]
+        if given and eps is None:
+            raise ValueError("weights need a norm (eps is None)")
+        for w in given:
+            if w.dtype not in _DTYPES:
+                raise ValueError(f"unsupported weight dtype {w.dtype}; expected float32 or bfloat16")
+            _check_like(w, (D,), given[0].dtype, x0.device, "a weight")
+        wdtype = given[0].dtype if given else wdtype
+    pos_stride = 0
+    if positions is not None:
+        if positions.dtype != torch.int64 or positions.device != x0.device or positions.shape not in ((N,), (B, N)):
+            raise ValueError(f"positions must be int64 of shape [{N}] or [{B}, {N}] on {x0.device}, got "
+                             f"{positions.dtype} {tuple(positions.shape)} on {positions.device}")
+        if N > 1 and positions.stride(-1) != 1:
+            raise ValueError("positions must be contiguous in their last dimension")
+        if positions.dim() == 2 and B > 1:
+            pos_stride = positions.stride(0)
+    freqs = tuple(freqs) if freqs is not None else ()
+    norm = eps is not None
+    heads = (ctypes.c_int32 * n)(*(x.shape[2] for x in xs))
+    strides = (ctypes.c_int64 * (3 * n))(*(s for x in xs for s in _strides(x)))
+    w = None if weights is None else _pointers(weights)
+    tail = (B, N, D, norm, float(eps) if norm else 0.0, ROTATE_LAYOUTS[layout], _freq_array(freqs), len(freqs),
+            _DTYPES[x0.dtype], _DTYPES[wdtype])
+    return n, strides, w, heads, (_ptr(positions), pos_stride, int(start)), tail, wdtype
+
+
+def _pointers(tensors):
+    return (ctypes.c_void_p * len(tensors))(*(_ptr(t) for t in tensors))
+
+
+def simplicial_norm_rotate_fwd(xs, weights=None, eps=1e-6, freqs=None, layout="half", positions=None, start=0, out=None):
+    """RMS norm of each head and position rotation of one to three tensors (q, k,
+    k') in one launch; returns their results as a list of contiguous tensors.
+
+    xs[t] is [B, N, heads_t, D] (a view with 16-byte aligned rows will do), weights[t]
+    [D] or None; eps None: no norm. `freqs` (numbers, see `rotary_freqs`) are the angles per
+    position of the pairs that `layout` names: "half" (i, n + i), "pairs" (2 i, 2 i + 1)
+    or "axis" (3 i, 3 i + 1: the first two of each 3-component chunk of the determinant
+    logits); None: no rotation. Positions: int64 [N] or [B, N], or start, start + 1, ..."""
+    n, strides, w, heads, pos, tail, _ = _rotate_args(xs, weights, eps, freqs, layout, positions, start)
+    device = xs[0].device
+    if out is None:
+        out = [torch.empty(x.shape, dtype=x.dtype, device=device) for x in xs]
+    else:
+        for x, y in zip(xs, out, strict=True):
+            _check_like(y, x.shape, x.dtype, device, "an output")
+    _call("simplicial_norm_rotate_fwd", device, n, _pointers(xs), strides, w, _pointers(out), heads, *pos, *tail)
+    return list(out)
+
+
+def simplicial_norm_rotate_bwd(xs, dys, weights=None, eps=1e-6, freqs=None, layout="half", positions=None, start=0,
+                               weight_grads=True, grads=None):
+    """(dxs, dweights) of simplicial_norm_rotate_fwd: lists, the latter with None where
+    there is no weight, or all None with weight_grads False."""
+    n, strides, w, heads, pos, tail, wdtype = _rotate_args(xs, weights, eps, freqs, layout, positions, start)
+    device = xs[0].device
+    if len(dys) != n:
+        raise ValueError(f"{len(dys)} gradients for {n} tensors")
+    for x, dy in zip(xs, dys):
+        _check_like(dy, x.shape, x.dtype, device, "an output's gradient")
+    if grads is None:
+        grads = [torch.empty(x.shape, dtype=x.dtype, device=device) for x in xs]
+    else:
+        for x, dx in zip(xs, grads, strict=True):
+            _check_like(dx, x.shape, x.dtype, device, "an input's gradient")
+    dws = [None] * n
+    if weight_grads and weights is not None:
+        dws = [None if t is None else torch.empty_like(t) for t in weights]
+    workspace, nbytes = None, 0
+    if any(t is not None for t in dws):
+        B, N, D = tail[:3]
+        nbytes = (_lib or _library()).simplicial_norm_rotate_bwd_workspace_size(n, B, N, D)
+        workspace = _workspace(nbytes, device)
+    _call("simplicial_norm_rotate_bwd", device, n, _pointers(xs), strides, w, _pointers(dys), _pointers(grads),
+          _pointers(dws), heads, *pos, _ptr(workspace), nbytes, *tail)
+    return list(grads), dws
+
+
+# ---- dot-product attention ----
+
+
+def simplicial_dot_attn_fwd_workspace_size(B, Nq, Nk, H, Hkv, D, causal, window, has_documents, dtype):
+    dt = _DTYPES.get(dtype, dtype)
+    return int(_library().simplicial_dot_attn_fwd_workspace_size(B, Nq, Nk, H, Hkv, D, bool(causal), int(window),
+                                                                 bool(has_documents), int(dt)))
+
+
+def simplicial_dot_attn_bwd_workspace_size(B, Nq, Nk, H, Hkv, D, causal, window, has_documents, dtype):
+    dt = _DTYPES.get(dtype, dtype)
+    return int(_library().simplicial_dot_attn_bwd_workspace_size(B, Nq, Nk, H, Hkv, D, bool(causal), int(window),
+                                                                 bool(has_documents), int(dt)))
+
+
+def _dot_args(q, k, v, scale, causal, window, softcap, slopes, documents, prefix, k_lens):
+    _check_view(q, "q")
+    _check_view(k, "k", q)
+    _check_view(v, "v", q)
+    B, Nq, H, D = q.shape
+    Nk, Hkv = k.shape[1], k.shape[2]
+    if k.shape != v.shape or k.shape[0] != B or k.shape[3] != D:
+        raise ValueError(f"k and v must be [{B}, Nk, Hkv, {D}], got {tuple(k.shape)} and {tuple(v.shape)}")
+    if H % Hkv:
+        raise ValueError(f"{H} query heads are no multiple of {Hkv} heads of k and v")
+    if Nq > Nk:
+        raise ValueError(f"{Nq} queries of {Nk} keys: the queries are the last of the keys' positions")
+    device = q.device
+    if slopes is not None:
+        _check_like(slopes, (H,), torch.float32, device, "slopes")
+    if documents is not None:
+        _check_like(documents, (B, Nk), torch.int32, device, "documents")
+    if prefix is not None:
+        _check_like(prefix, (B,), torch.int32, device, "prefix")
+    if k_lens is not None:
+        _check_like(k_lens, (B,), torch.int32, device, "k_lens")
+    dt = _DTYPES[q.dtype]
+    sizes = (B, Nq, Nk, H, Hkv, D)
+    plan = (*sizes, bool(causal), int(window), documents is not None, dt)
+    args = (*sizes, *_strides(q), *_strides(k), *_strides(v), D ** -0.5 if scale is None else float(scale), float(softcap),
+            bool(causal), int(window), _ptr(slopes), _ptr(documents), _ptr(prefix), _ptr(k_lens), dt)
+    return sizes, plan, args
+
+
+def simplicial_dot_attn_fwd(q, k, v, scale=None, causal=True, window=0, softcap=0.0, slopes=None, documents=None, prefix=None,
+                            k_lens=None, out=None, lse=None):
+    """(O, LSE) of dot-product attention: q [B, Nq, H, D], k and v [B, Nk, Hkv, D] (H a
+    multiple of Hkv), the queries the last Nq of the sequence's positions; LSE is
+    [B, H, Nq] float32. Views with 16-byte aligned rows will do.
+
+    `scale` defaults to 1/sqrt(D); `softcap` > 0 caps scores by softcap * tanh(s / softcap);
+    slopes [H] float32 subtract slope * distance. A query at position p sees keys j <= p
+    (causal) with |p - j| < window (window > 0), and those before prefix[b] ([B] int32); with
+    `documents` ([B, Nk] int32, negative: padding) of its own document alone. k_lens [B]
+    int32: filled lengths of a cache, its last Nq positions the queries. A query that sees
+    no key gives O = 0 and LSE = -inf."""
+    (B, Nq, _, H, _, _), plan, args = _dot_args(q, k, v, scale, causal, window, softcap, slopes, documents, prefix, k_lens)
+    device = q.device
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=device)
+    else:
+        _check_like(out, q.shape, q.dtype, device, "out")
+    if lse is None:
+        lse = torch.empty((B, H, Nq), dtype=torch.float32, device=device)
+    else:
+        _check_like(lse, (B, H, Nq), torch.float32, device, "lse")
+    nbytes = (_lib or _library()).simplicial_dot_attn_fwd_workspace_size(*plan)
+    workspace = _workspace(nbytes, device)
+    _call("simplicial_dot_attn_fwd", device, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(),
+          _ptr(workspace), nbytes, *args)
+    return out, lse
+
+
+def simplicial_dot_attn_bwd(q, k, v, out, dout, lse, scale=None, causal=True, window=0, softcap=0.0, slopes=None,
+                            documents=None, prefix=None, k_lens=None, grads=None):
+    """(dQ, dK, dV) of simplicial_dot_attn_fwd with the same options; `out` and `lse` are
+    its results. The slopes get no gradient."""
+    (B, Nq, _, H, _, _), plan, args = _dot_args(q, k, v, scale, causal, window, softcap, slopes, documents, prefix, k_lens)
+    device = q.device
+    _check_like(out, q.shape, q.dtype, device, "out")
+    _check_like(dout, q.shape, q.dtype, device, "dout")
+    _check_like(lse, (B, H, Nq), torch.float32, device, "lse")
+    if grads is None:
+        grads = tuple(torch.empty(t.shape, dtype=t.dtype, device=device) for t in (q, k, v))
+    else:
+        for t, g, name in zip((q, k, v), grads, ("dq", "dk", "dv"), strict=True):
+            _check_like(g, t.shape, t.dtype, device, name)
+    nbytes = (_lib or _library()).simplicial_dot_attn_bwd_workspace_size(*plan)
+    workspace = _workspace(nbytes, device)
+    _call("simplicial_dot_attn_bwd", device, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), dout.data_ptr(),
+          lse.data_ptr(), *(g.data_ptr() for g in grads), _ptr(workspace), nbytes, *args)
+    return grads
+
+
+# ---- log probabilities ----
+
+
+def _check_logits(logits, targets):
+    if logits.dim() != 2 or logits.numel() == 0:
+        raise ValueError(f"logits must be [R, V], got shape {tuple(logits.shape)}")
+    if not logits.is_cuda:
+        raise ValueError("logits must be a GPU tensor")
+    if logits.dtype not in _DTYPES:
+        raise ValueError(f"unsupported dtype {logits.dtype}; expected float32 or bfloat16")
+    R, V = logits.shape
+    if (V > 1 and logits.stride(1) != 1) or (R > 1 and logits.stride(0) < V):
+        raise ValueError("logits must be contiguous in their last dimension, rows apart")
+    _check_like(targets, (R,), torch.int64, logits.device, "targets")
+    return R, V, logits.stride(0) if R > 1 else V
+
+
+def simplicial_logprobs_fwd(logits, targets, top=0):
+    """(logprob, entropy, lse, top_logprob, top_index) of the rows of logits [R, V]:
+    the log probability of targets [R] (int64; negative: left out, 0), the entropy of
+    the distribution, the log of the sum of exponentials ([R] float32 each), and the `top` (at most
+    32) most probable tokens with their log probabilities ([R, top], equal logits by
+    ascending token)."""
+    R, V, stride = _check_logits(logits, targets)
+    top = int(top)
+    if not 0 <= top <= min(V, LOGPROBS_MAX_TOP):
+        raise ValueError(f"top {top} is not within 0 .. {min(V, LOGPROBS_MAX_TOP)}")
+    device, dt = logits.device, _DTYPES[logits.dtype]
+    logprob, entropy, lse = (torch.empty(R, dtype=torch.float32, device=device) for _ in range(3))
+    top_logprob = torch.empty((R, top), dtype=torch.float32, device=device)
+    top_index = torch.empty((R, top), dtype=torch.int64, device=device)
+    nbytes = (_lib or _library()).simplicial_logprobs_fwd_workspace_size(R, V, top, dt)
+    workspace = _workspace(nbytes, device)
+    _call("simplicial_logprobs_fwd", device, logits.data_ptr(), targets.data_ptr(), logprob.data_ptr(), entropy.data_ptr(),
+          lse.data_ptr(), _ptr(top_logprob) if top else None, _ptr(top_index) if top else None, _ptr(workspace), nbytes, R, V,
+          stride, top, dt)
+    return logprob, entropy, lse, top_logprob, top_index
+
+
+def simplicial_logprobs_bwd(logits, targets, lse, entropy, d_logprob=None, d_entropy=None, d_lse=None, out=None):
+    """Gradient of the logits from those of logprob, entropy and lse ([R] float32; None: zeros)."""
+    R, V, stride = _check_logits(logits, targets)
+    device = logits.device
+    _check_like(lse, (R,), torch.float32, device, "lse")
+    _check_like(entropy, (R,), torch.float32, device, "entropy")
+    for t, name in ((d_logprob, "d_logprob"), (d_entropy, "d_entropy"), (d_lse, "d_lse")):
+        if t is not None:
+            _check_like(t, (R,), torch.float32, device, name)
+    if out is None:
+        out = torch.empty((R, V), dtype=logits.dtype, device=device)
+    else:
+        _check_like(out, (R, V), logits.dtype, device, "out")
+    _call("simplicial_logprobs_bwd", device, logits.data_ptr(), targets.data_ptr(), lse.data_ptr(), entropy.data_ptr(),
+          _ptr(d_logprob), _ptr(d_entropy), _ptr(d_lse), out.data_ptr(), R, V, stride, _DTYPES[logits.dtype])
+    return out

@@ -107,4 +107,56 @@ __device__ __forceinline__ void walk_blocks(int lo, int hi, int off, int step, T
   }
 }
 
+// The same walk as a sequence that a pipelined loop asks for its next block, ahead of
+// the one it works on. test(block, live, mine, full): a block that is `live` comes up;
+// `mine` and `full` are given with it (as when the blocks are a workgroup's and the
+// wavefront's own rows see none, or all, of the block's pairs). blk < 0: no more.
+struct DotBlock {
+  int blk;
+  bool mine, full;
+};
+template <typename Test>
+struct BlockSeq {
+  Test test;
+  int lo, count, step, n0;
+  unsigned long long todo, mine, full;
+  __device__ __forceinline__ BlockSeq(int lo_, int hi, int off, int step_, Test t) : test(t), lo(lo_ + off), step(step_), n0(-64), todo(0), mine(0), full(0) {
+    count = lo < hi ? (hi - lo + step - 1) / step : 0;
+  }
+  __device__ __forceinline__ DotBlock next() {
+    while (todo == 0) {
+      n0 += 64;
+      if (n0 >= count) {
+        n0 = count;  // (stays at the end)
+        return DotBlock{-1, false, false};
+      }
+      const int lane = threadIdx.x & 63;
+      bool l = false, w = false, f = false;
+      if (n0 + lane < count) test(lo + (n0 + lane) * step, l, w, f);
+      todo = __builtin_amdgcn_ballot_w64(l);
+      mine = __builtin_amdgcn_ballot_w64(w);
+      full = __builtin_amdgcn_ballot_w64(f);
+    }
+    const int i = __builtin_ctzll(todo);
+    todo &= todo - 1;
+    return DotBlock{lo + (n0 + i) * step, static_cast<bool>((mine >> i) & 1), static_cast<bool>((full >> i) & 1)};
+  }
+};
+template <typename Test>
+__device__ __forceinline__ BlockSeq<Test> block_seq(int lo, int hi, int off, int step, Test t) {
+  return BlockSeq<Test>(lo, hi, off, step, t);
+}
+
+// r / G for 0 <= r < 2^31, as a product with magic = floor(2^(31 + l) / G) + 1, l =
+// ceil(log2 G), and a shift (G = 1: r).
+__device__ __forceinline__ int div_group(int r, const DotArgs& a) {
+  return a.G == 1 ? r : static_cast<int>(__umulhi(static_cast<unsigned>(r), a.magic) >> a.shift);
+}
+
+// Sum over the wavefront; every lane gets it.
+__device__ __forceinline__ float sum64(float x) {
+  x = reduce32(x, [](float p, float q) { return p + q; });
+  return x + swap_halves(x);
+}
+
 }  // namespace sa

@@ -617,15 +617,16 @@ hipError_t dot_ranges(const DotArgs& a, int2* ranges, hipStream_t st) {
 
 DotPlan dot_fwd_plan(int64_t B, int64_t Nq, int64_t Nk, int64_t H, int64_t Hkv, int64_t D, int causal, int window, bool docs,
                      int dtype) {
-  (void)dtype;
   DotPlan p;
-  const int64_t units = B * Hkv * ((H / Hkv * Nq + kDotBlock - 1) / kDotBlock);
+  const int64_t R = H / Hkv * Nq, units = B * Hkv * ((R + kDotBlock - 1) / kDotBlock);
   // Keys a row block walks: the parts take 256 of them at least.
   const int64_t keys = window && causal ? std::min<int64_t>(Nk, int64_t(window) + Nq) : Nk;
-  p.nsplit = static_cast<int>(std::max<int64_t>(1, std::min(1024 / units, keys / 256)));
+  p.nsplit = static_cast<int>(std::max<int64_t>(1, std::min((dtype == SA_DTYPE_BF16 ? 512 : 1024) / units, keys / 256)));
+  // bf16: workgroups of 128 rows where they fill the chip.
+  if (dtype == SA_DTYPE_BF16 && B * Hkv * ((R + 127) / 128) >= 256) p.nsplit = 0;
   p.ranges_off = 0;
   p.part_off = docs ? up256(static_cast<size_t>(B) * ((Nk + kDotBlock - 1) / kDotBlock) * sizeof(int2)) : 0;
-  p.bytes = p.part_off + (p.nsplit > 1 ? static_cast<size_t>(B) * H * Nq * p.nsplit * (D + 2) * sizeof(float) : 0);
+  p.bytes = p.part_off + (p.nsplit > 1 ? static_cast<size_t>(B) * H * Nq * p.nsplit * (D + 3) * sizeof(float) : 0);
   return p;
 }
 DotPlan dot_bwd_plan(int64_t B, int64_t Nq, int64_t Nk, int64_t H, int64_t Hkv, int64_t D, int causal, int window, bool docs,
@@ -639,9 +640,7 @@ DotPlan dot_bwd_plan(int64_t B, int64_t Nq, int64_t Nk, int64_t H, int64_t Hkv, 
   return p;
 }
 
-hipError_t dot_fwd_f32(const DotArgs& a, hipStream_t st) {
-  return a.dtype == SA_DTYPE_F32 ? launch<float>(a, false, st) : launch<uint16_t>(a, false, st);
-}
+hipError_t dot_fwd_f32(const DotArgs& a, hipStream_t st) { return launch<float>(a, false, st); }
 hipError_t dot_bwd_f32(const DotArgs& a, hipStream_t st) {
   return a.dtype == SA_DTYPE_F32 ? launch<float>(a, true, st) : launch<uint16_t>(a, true, st);
 }

@@ -1,0 +1,629 @@
+// Dot-product attention forward for bf16 data on v_mfma_f32_32x32x16_bf16, float32
+// statistics and accumulators.
+//
+//     S^T = K Q^T,  a = cap tanh(scale S / cap) - slope |p - j|,  O^T += V^T P^T
+//
+// A wavefront owns 32 rows, one in each lane (column c of the products): the running
+// maximum m and sum l of a row are the lane's own, and P^T goes from the accumulator
+// into the second product's operand as it is. K and V come in blocks of 32 keys by
+// loads straight into LDS, swizzled row-major; V^T fragments by the transposing LDS read. Head
+// dimensions 16 and 32 run as 64 with zeros behind them.
+//
+//   dot_fwd_kernel   4 wavefronts, 128 rows, which share the blocks: a ring of 4
+//                    stages, S(n + 1) formed while P(n) is.
+//   dot_few_kernel   32 rows and 4 wavefronts that each take every fourth block (of a
+//                    part of the key axis, where there are few rows) through LDS of
+//                    their own, added at the end: for few queries, a new token's
+//                    above all, where the time is that of reading K and V.
+//
+// The maximum is raised lazily: P is formed with the present m, and only where a
+// row's block sum leaves (0, 2^16] is m raised to the block's maximum and P formed
+// again. The output is divided by the sum of the probabilities as rounded to bf16
+// for the product with V (it is then a weighted mean of V's rows whatever the
+// rounding); LSE takes the sum of the unrounded ones.
+//
+// A block whose pairs are all visible has no mask work; blocks without a visible pair
+// are not visited (walked 64 at a time, a lane each). A masked pair's probability of
+// 0 times an infinity or NaN of V is NaN: rows that come out so are formed again by
+// themselves, over their visible keys alone.
+#include "dot_common.h"
+
+#include "simplicial_layers.h"
+
+#include <algorithm>
+
+namespace sa {
+namespace {
+
+constexpr int kWaves = 4;
+constexpr int kThreads = 64 * kWaves;
+constexpr float kPmax = 65536.f;
+constexpr int kFar = 0x7fffffff;
+
+template <int X>
+using IC = std::integral_constant<int, X>;
+
+template <int N>
+__device__ __forceinline__ void wait_vmcnt() {
+  static_assert(N >= 0 && N < 64, "vmcnt range");
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0F70);
+}
+
+// `n` positions from `p` on, `sn` elements apart, rows of `more` elements.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const uint16_t* p, int n, int64_t sn, int64_t more) {
+  const int64_t bytes = n > 0 ? ((n - 1) * sn + more) * 2 : 0;
+  return make_rsrc(p, static_cast<unsigned>(bytes < kFar ? bytes : kFar));
+}
+
+// What scores need beside the products, in base 2: a = mul s without cap and bias.
+template <bool CAP, bool BIAS>
+struct Scores {
+  float scale2, to_cap, cap2, slope2;
+  __device__ __forceinline__ Scores(const DotArgs& a, int head)
+      : scale2(a.scale * kLog2e), to_cap(CAP ? 2.f * kLog2e * a.scale / a.cap : 0.f), cap2(a.cap * kLog2e),
+        slope2(BIAS ? a.slopes[head] * kLog2e : 0.f) {}
+  // dj: position less key j
+  __device__ __forceinline__ float operator()(float s, float dj) const {
+    float x;
+    if constexpr (CAP)
+      x = cap2 - 2.f * cap2 * __builtin_amdgcn_rcpf(fast_exp2(s * to_cap) + 1.f);  // cap tanh
+    else
+      x = s * scale2;
+    if constexpr (BIAS) x = __builtin_fmaf(-slope2, fabsf(dj), x);
+    return x;
+  }
+};
+
+// A row's running state and the step over one block.
+template <int DP, bool CAP, bool BIAS>
+struct Row {
+  static constexpr int NDT = DP / 32;
+  f32x16_t acc[NDT];
+  float m, l, lr;  // maximum (base 2), sum, sum of the rounded probabilities
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt) acc[dt] = f32x16_t{};
+    m = -1e30f, l = 0.f, lr = 0.f;
+  }
+  // Probabilities of the block at key j0, packed; `masked`: seen(v) says whether the pair is visible.
+  template <typename Seen>
+  __device__ __forceinline__ void step(f32x16_t& s, const Scores<CAP, BIAS>& score, float dj, bool masked, Seen seen,
+                                       u32x4_t (&pf)[2]) {
+    const bf16x2_t ones = {static_cast<__bf16>(1.0f), static_cast<__bf16>(1.0f)};
+    float mul = score.scale2;
+    if (CAP || BIAS || masked) {
+      mul = 1.f;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[v] = score(s[v], dj - static_cast<float>(8 * (v >> 2) + (v & 3)));
+      if (masked) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+          if (!seen(v)) s[v] = -kInf;
+      }
+    }
+    float lb, lrb;
+    auto form = [&]() __attribute__((always_inline)) {
+      lb = 0.f, lrb = 0.f;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float x = fast_exp2(__builtin_fmaf(s[8 * u + 2 * e], mul, -m));
+          const float y = fast_exp2(__builtin_fmaf(s[8 * u + 2 * e + 1], mul, -m));
+          lb += x;
+          lb += y;
+          const unsigned xy = pack_bf16x2(x, y);
+          pf[u][e] = xy;
+          lrb = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, xy), ones, lrb, false);
+        }
+    };
+    form();
+    if (__builtin_amdgcn_ballot_w64(!(lb <= kPmax)) != 0) {
+      float mx = s[0] * mul;
+#pragma unroll
+      for (int v = 1; v < 16; ++v) mx = fmaxf(mx, s[v] * mul);
+      mx = fmaxf(m, fmaxf(mx, swap_halves(mx)));
+      const float down = fast_exp2(m - mx);
+      l *= down, lr *= down;
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt) acc[dt] *= down;
+      m = mx;
+      form();
+    }
+    l += lb, lr += lrb;
+  }
+  // Both halves' sums; m of a row without a visible key is below any score's.
+  __device__ __forceinline__ void finish() {
+    l += swap_halves(l);
+    lr += swap_halves(lr);
+  }
+};
+
+// The 32 rows of a wavefront, one a lane.
+struct Lanes {
+  int i, head, p;
+  bool valid;
+  __device__ __forceinline__ Lanes(const DotArgs& a, const DotMask& m, int hk, int r) {
+    valid = r < a.G * a.Nq;
+    const int rr = valid ? r : 0;
+    i = div_group(rr, a);
+    head = hk * a.G + rr - i * a.G;
+    p = valid ? m.first + i : -1;
+  }
+};
+__device__ __forceinline__ DotSpan rows_span(const DotArgs& a, const DotMask& m, int r0, int n) {
+  return DotSpan(m, m.first + r0 / a.G, m.first + (min(r0 + n, a.G * a.Nq) - 1) / a.G);
+}
+
+// Q's rows as the products' B operand.
+template <int DP>
+__device__ __forceinline__ void load_q(u32x4_t (&qf)[DP / 16], const DotArgs& a, const Lanes& w, int b, int h) {
+  const uint16_t* p = static_cast<const uint16_t*>(a.q) + b * a.qsb + w.i * a.qsn + w.head * a.qsh + 8 * h;
+#pragma unroll
+  for (int t = 0; t < DP / 16; ++t) qf[t] = w.valid && 16 * t + 8 * h < a.D ? ldg128(p + 16 * t) : u32x4_t{0, 0, 0, 0};
+}
+
+// O of one row by itself, over its visible keys (LSE is not touched by masked pairs), a
+// wavefront's 64 lanes along the columns: for rows whose products met an infinity or NaN.
+__device__ __forceinline__ void single_row(const DotArgs& a, const DotMask& m, int b, int i, int head, float lse) {
+  const int lane = threadIdx.x & 63, hk = head / a.G, p = m.first + i, dq = m.doc(p);
+  const bool d0 = lane < a.D, d1 = lane + 64 < a.D;
+  const uint16_t* q = static_cast<const uint16_t*>(a.q) + b * a.qsb + i * a.qsn + head * a.qsh + lane;
+  const uint16_t* k = static_cast<const uint16_t*>(a.k) + b * a.ksb + hk * a.ksh + lane;
+  const uint16_t* v = static_cast<const uint16_t*>(a.v) + b * a.vsb + hk * a.vsh + lane;
+  const float q0 = d0 ? bf16_to_f32(q[0]) : 0.f, q1 = d1 ? bf16_to_f32(q[64]) : 0.f;
+  const float slope = a.slopes ? a.slopes[head] : 0.f;
+  float o0 = 0.f, o1 = 0.f;
+  for (int j = 0; j < m.L; ++j) {
+    if (!m.sees(p, j, dq, m.doc(j))) continue;
+    const int64_t kj = j * a.ksn, vj = j * a.vsn;
+    float s = (d0 ? q0 * bf16_to_f32(k[kj]) : 0.f) + (d1 ? q1 * bf16_to_f32(k[kj + 64]) : 0.f);
+    s = sum64(s) * a.scale;
+    if (a.cap > 0.f) s = a.cap * tanhf(s / a.cap);
+    const float w = fast_exp2((s - slope * static_cast<float>(abs(p - j)) - lse) * kLog2e);
+    o0 += d0 ? w * bf16_to_f32(v[vj]) : 0.f;
+    o1 += d1 ? w * bf16_to_f32(v[vj + 64]) : 0.f;
+    if (__builtin_amdgcn_ballot_w64((d0 && o0 == o0) || (d1 && o1 == o1)) == 0) break;  // all NaN
+  }
+  uint16_t* out = static_cast<uint16_t*>(a.out) + ((static_cast<int64_t>(b) * a.Nq + i) * a.H + head) * a.D + lane;
+  if (d0) out[0] = f32_to_bf16(o0);
+  if (d1) out[64] = f32_to_bf16(o1);
+}
+__device__ __forceinline__ bool has_mask(const DotArgs& a) { return a.causal || a.window || a.prefix || a.docs || a.lens; }
+// The rows of `bad` (a bit for each of the wavefront's 32), one after another.
+__device__ __forceinline__ void single_rows(const DotArgs& a, const DotMask& m, int b, const Lanes& w, float lse, unsigned bad) {
+  while (bad) {
+    const int c = __builtin_ctz(bad);
+    bad &= bad - 1;
+    single_row(a, m, b, __builtin_amdgcn_readlane(w.i, c), __builtin_amdgcn_readlane(w.head, c),
+               __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(lse), c)));
+  }
+}
+
+// Workgroup order: every XCD takes a contiguous run of (sequence, K-side head), whose
+// keys its L2 holds; the row blocks that see most keys come first.
+__device__ __forceinline__ bool unit_of(int64_t total, int64_t& unit) {
+  const int64_t per = (total + 7) / 8;
+  unit = static_cast<int64_t>(blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  return unit < total;
+}
+unsigned unit_grid(int64_t total) { return static_cast<unsigned>((total + 7) / 8 * 8); }
+
+// Per-lane LDS offsets of a tile's fragments.
+template <int DP>
+struct Frags {
+  using T = SwzTile<DP>;
+  int ko[DP / 16], vo[DP / 32][2];
+  __device__ __forceinline__ Frags(int lane, int base) {
+    const int c = lane & 31, h = lane >> 5, grp = lane >> 4, sl = lane & 15;
+#pragma unroll
+    for (int t = 0; t < DP / 16; ++t) ko[t] = base + T::off(c, 2 * t + h);
+    const int r0 = 4 * (grp >> 1) + (sl >> 2);
+#pragma unroll
+    for (int dt = 0; dt < DP / 32; ++dt) {
+      const int col = 32 * dt + 16 * (grp & 1) + 4 * (sl & 3), ch = col >> 3, within = (col & 7) * 2;
+      vo[dt][0] = base + T::off(r0, ch) + within;
+      vo[dt][1] = base + T::off(r0 + 8, ch) + within;
+    }
+  }
+  __device__ __forceinline__ u32x4_t row(const lds_char* tile, int t) const { return lds_ld<u32x4_t>(tile + ko[t]); }
+  __device__ __forceinline__ u32x4_t tr(const lds_char* tile, int dt, int u) const {
+    const lds_char* p = tile + 2 * DP * 16 * u;
+    const u32x2_t x = lds_tr16(p + vo[dt][0]), y = lds_tr16(p + vo[dt][1]);
+    return u32x4_t{x[0], x[1], y[0], y[1]};
+  }
+};
+
+// Rows c of O: 4 consecutive columns of each accumulator quad.
+template <int DP>
+__device__ __forceinline__ void store_row(const DotArgs& a, int b, const Lanes& w, const f32x16_t (&acc)[DP / 32], float inv, int h) {
+  uint16_t* out = static_cast<uint16_t*>(a.out) + ((static_cast<int64_t>(b) * a.Nq + w.i) * a.H + w.head) * a.D + 4 * h;
+#pragma unroll
+  for (int dt = 0; dt < DP / 32; ++dt)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (32 * dt + 8 * q < a.D)
+        *reinterpret_cast<u32x2_t*>(out + 32 * dt + 8 * q) =
+            u32x2_t{pack_bf16x2(acc[dt][4 * q] * inv, acc[dt][4 * q + 1] * inv), pack_bf16x2(acc[dt][4 * q + 2] * inv, acc[dt][4 * q + 3] * inv)};
+}
+
+template <int DP, bool CAP, bool BIAS>
+__global__ __launch_bounds__(kThreads, 2) void dot_fwd_kernel(DotArgs a) {
+  using T = SwzTile<DP>;
+  constexpr int NT = DP / 16, NDT = DP / 32, SPW = T::instrs / kWaves, kStages = 4, kRows = 32 * kWaves;
+  static_assert(T::instrs % kWaves == 0, "every wavefront issues as many loads of a tile");
+  __shared__ __attribute__((aligned(16))) char kst0[T::bytes], kst1[T::bytes], kst2[T::bytes], kst3[T::bytes];
+  __shared__ __attribute__((aligned(16))) char vst0[T::bytes], vst1[T::bytes], vst2[T::bytes], vst3[T::bytes];
+  auto kst = [&](auto SC) __attribute__((always_inline)) {
+    constexpr int X = decltype(SC)::value;
+    return to_lds(X == 0 ? kst0 : X == 1 ? kst1 : X == 2 ? kst2 : kst3);
+  };
+  auto vst = [&](auto SC) __attribute__((always_inline)) {
+    constexpr int X = decltype(SC)::value;
+    return to_lds(X == 0 ? vst0 : X == 1 ? vst1 : X == 2 ? vst2 : vst3);
+  };
+  const int R = a.G * a.Nq, nrb = (R + kRows - 1) / kRows;
+  int64_t unit;
+  if (!unit_of(static_cast<int64_t>(a.B) * a.Hkv * nrb, unit)) return;
+  const int block = nrb - 1 - static_cast<int>(unit % nrb), bh = static_cast<int>(unit / nrb);
+  const int b = bh / a.Hkv, hk = bh - b * a.Hkv;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 31, h = lane >> 5;
+  const DotMask m(a, b);
+  const int r0 = block * kRows + 32 * wave;
+  const Lanes w(a, m, hk, r0 + c);
+  const DotSpan all = rows_span(a, m, block * kRows, kRows), own = rows_span(a, m, min(r0, R - 1), 32);
+  const int dq = m.doc(w.p);
+  const Scores<CAP, BIAS> score(a, w.head);
+  const int pos = w.p - 4 * h;
+  int lo, hi;
+  key_blocks(m, all, lo, hi);
+  const bool some = r0 < R;
+  auto seq = block_seq(lo, hi, 0, 1, [&](int blk, bool& live, bool& mine, bool& full) {
+    const DotSpan k(m, blk * kDotBlock, blk * kDotBlock + kDotBlock - 1);
+    live = dot_live(m, all, k);
+    mine = some && dot_live(m, own, k);
+    full = dot_full(m, own, k);
+  });
+
+  // Loads of a tile: wavefront x-th share is 1 KB, lane l the 16-byte chunk at 16 l.
+  int kvoff[SPW], vvoff[SPW];
+#pragma unroll
+  for (int x = 0; x < SPW; ++x) {
+    const int p = 64 * (x * kWaves + wave) + lane, row = p / T::CH, ch = (p % T::CH) ^ T::swz(row);
+    kvoff[x] = 8 * ch < a.D ? static_cast<int>(row * a.ksn * 2) + 16 * ch : kFar;
+    vvoff[x] = 8 * ch < a.D ? static_cast<int>(row * a.vsn * 2) + 16 * ch : kFar;
+  }
+  const uint16_t* kb = static_cast<const uint16_t*>(a.k) + b * a.ksb + hk * a.ksh;
+  const uint16_t* vb = static_cast<const uint16_t*>(a.v) + b * a.vsb + hk * a.vsh;
+  // (past the last block: loads of nothing, so that every iteration issues as many)
+  auto load_k = [&](lds_char* dst, int blk) __attribute__((always_inline)) {
+    const int64_t j0 = max(blk, 0) * kDotBlock;
+    const auto r = rows_of(kb + j0 * a.ksn, blk < 0 ? 0 : min(m.L - static_cast<int>(j0), kDotBlock), a.ksn, a.D);
+#pragma unroll
+    for (int x = 0; x < SPW; ++x) load_lds16(r, dst + 1024 * (x * kWaves + wave), kvoff[x]);
+  };
+  auto load_v = [&](lds_char* dst, int blk) __attribute__((always_inline)) {
+    const int64_t j0 = max(blk, 0) * kDotBlock;
+    const auto r = rows_of(vb + j0 * a.vsn, blk < 0 ? 0 : min(m.L - static_cast<int>(j0), kDotBlock), a.vsn, a.D);
+#pragma unroll
+    for (int x = 0; x < SPW; ++x) load_lds16(r, dst + 1024 * (x * kWaves + wave), vvoff[x]);
+  };
+  u32x4_t qf[NT];
+  load_q<DP>(qf, a, w, b, h);
+  const Frags<DP> frag(lane, 0);
+  DotBlock bq[kStages];
+  bq[0] = seq.next();
+  load_k(kst(IC<0>{}), bq[0].blk);
+  bq[1] = seq.next();
+  load_k(kst(IC<1>{}), bq[1].blk);
+  load_v(vst(IC<0>{}), bq[0].blk);
+  bq[2] = seq.next();
+  load_k(kst(IC<2>{}), bq[2].blk);
+  load_v(vst(IC<1>{}), bq[1].blk);
+  bq[3] = seq.next();
+  load_k(kst(IC<3>{}), bq[3].blk);
+  load_v(vst(IC<2>{}), bq[2].blk);
+
+  Row<DP, CAP, BIAS> row;
+  row.clear();
+  f32x16_t sc[2];
+  u32x4_t kf[NT];
+  auto products = [&](f32x16_t& dst) __attribute__((always_inline)) {
+    dst = mfma32(kf[0], qf[0], f32x16_t{});
+#pragma unroll
+    for (int t = 1; t < NT; ++t) dst = mfma32(kf[t], qf[t], dst);
+  };
+  wait_vmcnt<5 * SPW>();  // K(0), K(1)
+  lds_barrier_tracked();
+#pragma unroll
+  for (int t = 0; t < NT; ++t) kf[t] = frag.row(kst(IC<0>{}), t);
+  __builtin_amdgcn_sched_barrier(0);
+  products(sc[0]);
+#pragma unroll
+  for (int t = 0; t < NT; ++t) kf[t] = frag.row(kst(IC<1>{}), t);
+
+  // Iteration n: S(n + 1) and P(n), O += P V(n). K(n + 2) and V(n) have to be in LDS: of the loads
+  // issued after them V(n + 1), K(n + 3) and V(n + 2) may be in flight.
+  auto iteration = [&](auto SC) __attribute__((always_inline)) {
+    constexpr int S = decltype(SC)::value, cur = S & 1, nxt = cur ^ 1;
+    const DotBlock at = bq[S];
+    if (at.blk < 0) return false;
+    wait_vmcnt<3 * SPW>();
+    lds_barrier_tracked();
+    bq[S] = seq.next();
+    load_k(kst(IC<S>{}), bq[S].blk);                            // K(n) was read in iteration n - 2
+    load_v(vst(IC<(S + 3) % kStages>{}), bq[(S + 3) % kStages].blk);  // V(n - 1) in iteration n - 1
+    if (at.mine) {
+      u32x4_t vf[2][NDT];
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt) vf[u][dt] = frag.tr(vst(IC<S>{}), dt, u);
+      __builtin_amdgcn_s_setprio(1);
+      products(sc[nxt]);
+      u32x4_t pf[2];
+      const int j0 = at.blk * kDotBlock;
+      row.step(sc[cur], score, static_cast<float>(pos - j0), !at.full,
+               [&](int v) {
+                 const int j = j0 + acc_row(v, h);
+                 return m.sees(w.p, j, dq, m.doc(j));
+               },
+               pf);
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt) row.acc[dt] = mfma32(vf[u][dt], pf[u], row.acc[dt]);
+      __builtin_amdgcn_s_setprio(0);
+    } else {
+      products(sc[nxt]);
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) kf[t] = frag.row(kst(IC<(S + 2) % kStages>{}), t);
+    return true;
+  };
+  while (iteration(IC<0>{}) && iteration(IC<1>{}) && iteration(IC<2>{}) && iteration(IC<3>{})) {
+  }
+  wait_vmcnt<0>();
+  row.finish();
+  const bool empty = row.l == 0.f;
+  const float inv = empty ? 0.f : 1.f / row.lr;
+  const float lse = empty ? -kInf : row.m * kLn2 + logf(row.l);
+  float check = 0.f;
+#pragma unroll
+  for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) check += row.acc[dt][v] * 0.f;
+  unsigned bad = 0;
+  if (has_mask(a)) {
+    const unsigned long long x = __builtin_amdgcn_ballot_w64(w.valid && fabsf(row.l) < kInf && check != check);
+    bad = static_cast<unsigned>(x) | static_cast<unsigned>(x >> 32);
+  }
+  if (w.valid) {
+    if (!((bad >> c) & 1)) store_row<DP>(a, b, w, row.acc, inv, h);
+    if (h == 0) a.lse[(static_cast<int64_t>(b) * a.H + w.head) * a.Nq + w.i] = lse;
+  }
+  single_rows(a, m, b, w, lse, bad);
+}
+
+template <int DP, bool CAP, bool BIAS>
+__global__ __launch_bounds__(kThreads, 1) void dot_few_kernel(DotArgs a) {
+  using T = SwzTile<DP>;
+  constexpr int NT = DP / 16, NDT = DP / 32, SPW = T::instrs;
+  __shared__ __attribute__((aligned(16))) char kst0[kWaves * T::bytes], kst1[kWaves * T::bytes];
+  __shared__ __attribute__((aligned(16))) char vst0[kWaves * T::bytes], vst1[kWaves * T::bytes];
+  __shared__ float stat[3][kWaves][32];
+  auto kst = [&](auto SC) __attribute__((always_inline)) { return to_lds(decltype(SC)::value == 0 ? kst0 : kst1); };
+  auto vst = [&](auto SC) __attribute__((always_inline)) { return to_lds(decltype(SC)::value == 0 ? vst0 : vst1); };
+  const int R = a.G * a.Nq, nrb = (R + 31) / 32;
+  int64_t unit;
+  if (!unit_of(static_cast<int64_t>(a.B) * a.Hkv * nrb * a.nsplit, unit)) return;
+  const int part = static_cast<int>(unit % a.nsplit);
+  unit /= a.nsplit;
+  const int block = nrb - 1 - static_cast<int>(unit % nrb), bh = static_cast<int>(unit / nrb);
+  const int b = bh / a.Hkv, hk = bh - b * a.Hkv;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 31, h = lane >> 5;
+  const DotMask m(a, b);
+  const Lanes w(a, m, hk, block * 32 + c);
+  const DotSpan own = rows_span(a, m, block * 32, 32);
+  const int dq = m.doc(w.p);
+  const Scores<CAP, BIAS> score(a, w.head);
+  const int pos = w.p - 4 * h;
+  int lo, hi;
+  key_blocks(m, own, lo, hi);
+  auto seq = block_seq(lo, hi, part * kWaves + wave, kWaves * a.nsplit, [&](int blk, bool& live, bool& mine, bool& full) {
+    const DotSpan k(m, blk * kDotBlock, blk * kDotBlock + kDotBlock - 1);
+    live = dot_live(m, own, k);
+    mine = live;
+    full = dot_full(m, own, k);
+  });
+  int kvoff[SPW], vvoff[SPW];
+#pragma unroll
+  for (int x = 0; x < SPW; ++x) {
+    const int p = 64 * x + lane, row = p / T::CH, ch = (p % T::CH) ^ T::swz(row);
+    kvoff[x] = 8 * ch < a.D ? static_cast<int>(row * a.ksn * 2) + 16 * ch : kFar;
+    vvoff[x] = 8 * ch < a.D ? static_cast<int>(row * a.vsn * 2) + 16 * ch : kFar;
+  }
+  const uint16_t* kb = static_cast<const uint16_t*>(a.k) + b * a.ksb + hk * a.ksh;
+  const uint16_t* vb = static_cast<const uint16_t*>(a.v) + b * a.vsb + hk * a.vsh;
+  auto load = [&](auto SC, int blk) __attribute__((always_inline)) {
+    const int64_t j0 = max(blk, 0) * kDotBlock;
+    const int n = blk < 0 ? 0 : min(m.L - static_cast<int>(j0), kDotBlock);
+    const auto rk = rows_of(kb + j0 * a.ksn, n, a.ksn, a.D), rv = rows_of(vb + j0 * a.vsn, n, a.vsn, a.D);
+#pragma unroll
+    for (int x = 0; x < SPW; ++x) load_lds16(rk, kst(SC) + wave * T::bytes + 1024 * x, kvoff[x]);
+#pragma unroll
+    for (int x = 0; x < SPW; ++x) load_lds16(rv, vst(SC) + wave * T::bytes + 1024 * x, vvoff[x]);
+  };
+  u32x4_t qf[NT];
+  load_q<DP>(qf, a, w, b, h);
+  const Frags<DP> frag(lane, wave * T::bytes);
+  DotBlock bq[2];
+  bq[0] = seq.next();
+  load(IC<0>{}, bq[0].blk);
+  bq[1] = seq.next();
+  load(IC<1>{}, bq[1].blk);
+  Row<DP, CAP, BIAS> row;
+  row.clear();
+  // (the wavefronts' blocks are their own: no barriers)
+  auto iteration = [&](auto SC) __attribute__((always_inline)) {
+    constexpr int S = decltype(SC)::value;
+    const DotBlock at = bq[S];
+    if (at.blk < 0) return false;
+    wait_vmcnt<2 * SPW>();
+    asm volatile("" ::: "memory");
+    f32x16_t s = mfma32(frag.row(kst(SC), 0), qf[0], f32x16_t{});
+#pragma unroll
+    for (int t = 1; t < NT; ++t) s = mfma32(frag.row(kst(SC), t), qf[t], s);
+    u32x4_t vf[2][NDT];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt) vf[u][dt] = frag.tr(vst(SC), dt, u);
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // the stage is read: its next block may come
+    asm volatile("" ::: "memory");
+    bq[S] = seq.next();
+    load(SC, bq[S].blk);
+    u32x4_t pf[2];
+    const int j0 = at.blk * kDotBlock;
+    row.step(s, score, static_cast<float>(pos - j0), !at.full,
+             [&](int v) {
+               const int j = j0 + acc_row(v, h);
+               return m.sees(w.p, j, dq, m.doc(j));
+             },
+             pf);
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt) row.acc[dt] = mfma32(vf[u][dt], pf[u], row.acc[dt]);
+    return true;
+  };
+  while (iteration(IC<0>{}) && iteration(IC<1>{})) {
+  }
+  wait_vmcnt<0>();
+  row.finish();
+  // The wavefronts' states joined: their accumulators, scaled to the common maximum, through
+  // the tiles' LDS (one array a tile, 4 KB a wavefront).
+  auto joined = [&](int dt) { return reinterpret_cast<float*>(dt == 0 ? kst0 : dt == 1 ? kst1 : dt == 2 ? vst0 : vst1) + lane; };
+  if (h == 0) stat[0][wave][c] = row.m, stat[1][wave][c] = row.l, stat[2][wave][c] = row.lr;
+  __syncthreads();
+  float top = stat[0][0][c];
+#pragma unroll
+  for (int x = 1; x < kWaves; ++x) top = fmaxf(top, stat[0][x][c]);
+  float l = 0.f, lr = 0.f;
+#pragma unroll
+  for (int x = 0; x < kWaves; ++x) {
+    const float f = fast_exp2(stat[0][x][c] - top);
+    l += f * stat[1][x][c];
+    lr += f * stat[2][x][c];
+  }
+  const float down = fast_exp2(row.m - top);
+#pragma unroll
+  for (int dt = 0; dt < NDT; ++dt) {
+    float* x = joined(dt) + wave * 1024;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) x[64 * v] = row.acc[dt][v] * down;
+  }
+  __syncthreads();
+  const bool empty = l == 0.f;
+  const float inv = a.nsplit > 1 ? 1.f : empty ? 0.f : 1.f / lr;
+  const int64_t rr = static_cast<int64_t>(bh) * R + block * 32 + c;
+  float* pr = a.part + (rr * a.nsplit + part) * a.D + 4 * h;
+  uint16_t* out = static_cast<uint16_t*>(a.out) + ((static_cast<int64_t>(b) * a.Nq + w.i) * a.H + w.head) * a.D + 4 * h;
+  float check = 0.f;
+  const float lse = empty ? -kInf : top * kLn2 + logf(l);
+  // Each wavefront takes quad `wave` of every tile.
+#pragma unroll
+  for (int dt = 0; dt < NDT; ++dt) {
+    const float* x = joined(dt);
+    float y[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      y[e] = 0.f;
+#pragma unroll
+      for (int z = 0; z < kWaves; ++z) y[e] += x[z * 1024 + 64 * (4 * wave + e)];
+      check += y[e] * 0.f;
+      y[e] *= inv;
+    }
+    if (w.valid && 32 * dt + 8 * wave < a.D) {
+      if (a.nsplit > 1)
+        *reinterpret_cast<u32x4_t*>(pr + 32 * dt + 8 * wave) =
+            u32x4_t{__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3])};
+      else
+        *reinterpret_cast<u32x2_t*>(out + 32 * dt + 8 * wave) = u32x2_t{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
+    }
+  }
+  if (wave == 0 && h == 0 && w.valid) {
+    if (a.nsplit > 1) {
+      float* st = a.part + static_cast<int64_t>(a.B) * a.H * a.Nq * a.nsplit * a.D + (rr * a.nsplit + part) * 3;
+      st[0] = l == 0.f ? -kInf : top, st[1] = l, st[2] = lr;
+    } else {
+      a.lse[(static_cast<int64_t>(b) * a.H + w.head) * a.Nq + w.i] = lse;
+    }
+  }
+  if (a.nsplit > 1 || !has_mask(a)) return;
+  // (a row is not finite if any wavefront's columns of it are not)
+  __shared__ unsigned flags[kWaves];
+  const unsigned long long x = __builtin_amdgcn_ballot_w64(w.valid && fabsf(l) < kInf && check != check);
+  if (lane == 0) flags[wave] = static_cast<unsigned>(x) | static_cast<unsigned>(x >> 32);
+  __syncthreads();
+  if (wave == 0) single_rows(a, m, b, w, lse, flags[0] | flags[1] | flags[2] | flags[3]);
+}
+
+// Joins the parts of a row, four rows a workgroup, a wavefront each.
+__global__ __launch_bounds__(kThreads) void dot_join_kernel(DotArgs a) {
+  const int64_t all = static_cast<int64_t>(a.B) * a.H * a.Nq, r = static_cast<int64_t>(blockIdx.x) * kWaves + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  if (r >= all) return;
+  const float* st = a.part + all * a.nsplit * a.D + r * a.nsplit * 3;
+  float top = -kInf;
+  for (int s = lane; s < a.nsplit; s += 64) top = fmaxf(top, st[3 * s]);
+  top = reduce32(top, [](float x, float y) { return fmaxf(x, y); });
+  top = fmaxf(top, swap_halves(top));
+  const float base = top == -kInf ? 0.f : top;
+  float l = 0.f, lr = 0.f, x0 = 0.f, x1 = 0.f;
+  for (int s = 0; s < a.nsplit; ++s) {
+    const float f = fast_exp2(st[3 * s] - base);
+    l += f * st[3 * s + 1];
+    lr += f * st[3 * s + 2];
+    const float* p = a.part + (r * a.nsplit + s) * a.D;
+    x0 += lane < a.D ? f * p[lane] : 0.f;
+    x1 += lane + 64 < a.D ? f * p[lane + 64] : 0.f;
+  }
+  const int64_t rh = static_cast<int64_t>(a.G) * a.Nq;
+  const int bh = static_cast<int>(r / rh), rr = static_cast<int>(r - bh * rh), i = rr / a.G;
+  const int b = bh / a.Hkv, head = (bh - b * a.Hkv) * a.G + rr - i * a.G;
+  const float lse = l == 0.f ? -kInf : top * kLn2 + logf(l);
+  if (lane == 0) a.lse[(static_cast<int64_t>(b) * a.H + head) * a.Nq + i] = lse;
+  const float check = x0 * 0.f + x1 * 0.f;
+  if (has_mask(a) && fabsf(l) < kInf && __builtin_amdgcn_ballot_w64(check != check) != 0) {
+    single_row(a, DotMask(a, b), b, i, head, lse);
+    return;
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / lr;
+  uint16_t* out = static_cast<uint16_t*>(a.out) + ((static_cast<int64_t>(b) * a.Nq + i) * a.H + head) * a.D;
+  if (lane < a.D) out[lane] = f32_to_bf16(x0 * inv);
+  if (lane + 64 < a.D) out[lane + 64] = f32_to_bf16(x1 * inv);
+}
+
+template <int DP, bool CAP, bool BIAS>
+hipError_t launch(const DotArgs& a, hipStream_t st) {
+  const int64_t R = static_cast<int64_t>(a.G) * a.Nq, heads = static_cast<int64_t>(a.B) * a.Hkv;
+  if (a.nsplit == 0) {
+    dot_fwd_kernel<DP, CAP, BIAS><<<unit_grid(heads * ((R + 127) / 128)), kThreads, 0, st>>>(a);
+    return hipGetLastError();
+  }
+  dot_few_kernel<DP, CAP, BIAS><<<unit_grid(heads * ((R + 31) / 32) * a.nsplit), kThreads, 0, st>>>(a);
+  if (a.nsplit > 1) dot_join_kernel<<<static_cast<unsigned>((heads * R + kWaves - 1) / kWaves), kThreads, 0, st>>>(a);
+  return hipGetLastError();
+}
+template <int DP>
+hipError_t launch(const DotArgs& a, hipStream_t st) {
+  if (a.cap > 0.f) return a.slopes ? launch<DP, true, true>(a, st) : launch<DP, true, false>(a, st);
+  return a.slopes ? launch<DP, false, true>(a, st) : launch<DP, false, false>(a, st);
+}
+
+}  // namespace
+
+hipError_t dot_fwd_bf16(const DotArgs& a, hipStream_t st) { return a.D <= 64 ? launch<64>(a, st) : launch<128>(a, st); }
+
+}  // namespace sa

@@ -131,6 +131,12 @@ sa::DotArgs dot_args(const DotCall& c, const void* q, const void* k, const void*
   a.vsb = c.st[6], a.vsn = c.st[7], a.vsh = c.st[8];
   a.B = static_cast<int>(c.B), a.Nq = static_cast<int>(c.Nq), a.Nk = static_cast<int>(c.Nk), a.H = static_cast<int>(c.H);
   a.Hkv = static_cast<int>(c.Hkv), a.D = static_cast<int>(c.D), a.G = a.H / a.Hkv;
+  if (a.G > 1) {
+    int l = 0;
+    while ((int64_t(1) << l) < a.G) ++l;
+    a.magic = static_cast<unsigned>((uint64_t(1) << (31 + l)) / static_cast<uint64_t>(a.G) + 1);
+    a.shift = l - 1;
+  }
   a.scale = c.scale, a.cap = c.softcap, a.causal = c.causal != 0;
   a.window = c.window >= c.Nk ? 0 : c.window;  // (no distance reaches Nk)
   a.slopes = c.slopes, a.docs = c.documents, a.prefix = c.prefix, a.lens = c.k_lens;
@@ -229,7 +235,7 @@ int simplicial_dot_attn_fwd(const void* q, const void* k, const void* v, void* o
     if (r != SA_OK) return r;
     a.ranges = ranges;
   }
-  return to_status(sa::dot_fwd_f32(a, st));
+  return to_status(dtype == SA_DTYPE_BF16 ? sa::dot_fwd_bf16(a, st) : sa::dot_fwd_f32(a, st));
 }
 
 size_t simplicial_dot_attn_bwd_workspace_size(int64_t B, int64_t Nq, int64_t Nk, int64_t H,

@@ -62,6 +62,8 @@ struct DotArgs {
   void *dq, *dk, *dv;
   int64_t qsb, qsn, qsh, ksb, ksn, ksh, vsb, vsn, vsh;
   int B, Nq, Nk, H, Hkv, D, G;
+  unsigned magic;  // of the division by G (dot_common.h)
+  int shift;
   float scale, cap;
   int causal, window;  // window 0: none
   const float* slopes;
@@ -71,7 +73,7 @@ struct DotArgs {
   // Smallest and largest document number of every 32 positions, [B, ceil(Nk / 32)].
   const int2* ranges;
   float* delta;  // backward: Delta [B, H, Nq]
-  int nsplit;    // forward: parts of the key axis
+  int nsplit;    // forward: parts of the key axis (bf16, 0: workgroups of 128 rows)
   float* part;   // forward, nsplit > 1: their partial results
   int dtype;
 };
@@ -86,5 +88,6 @@ DotPlan dot_bwd_plan(int64_t B, int64_t Nq, int64_t Nk, int64_t H, int64_t Hkv, 
 hipError_t dot_ranges(const DotArgs& a, int2* ranges, hipStream_t st);
 hipError_t dot_fwd_f32(const DotArgs& a, hipStream_t st);
 hipError_t dot_bwd_f32(const DotArgs& a, hipStream_t st);
+hipError_t dot_fwd_bf16(const DotArgs& a, hipStream_t st);
 
 }  // namespace sa

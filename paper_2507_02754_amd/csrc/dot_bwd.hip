@@ -1,0 +1,567 @@
+// Dot-product attention backward for bf16 data on v_mfma_f32_32x32x16_bf16, float32
+// sums.
+//
+//     P = exp(a - LSE),  dS = P (dO V^T - Delta) (1 - tanh^2)
+//     dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO
+//
+// Two kernels without atomics. The query side owns rows: S^T = K Q^T and dP^T = V dO^T
+// put one row in each lane, dQ^T += K^T dS^T; it also forms Delta = <dO, O> and leaves
+// what the key side needs of a block of 32 rows (Stat) in the workspace. The key side
+// owns keys: S = Q K^T, dP = dO V^T with one key in each lane, dV^T += dO^T P and
+// dK^T += Q^T dS over all rows of the head's group, which sums the gradients of a
+// shared head in float32. 7 matrix products where 5 would do with S and dP formed
+// once, against atomics or partial sums of dQ for every block of keys.
+//
+// As in the forward, a workgroup's 4 wavefronts own 32 rows (keys) each and share the
+// blocks of the other side through a ring in LDS, or (PRIV, where there are few rows
+// or keys) own the same 32 and take every fourth block through LDS of their own, their
+// sums added at the end in a fixed order.
+//
+// P and dS are rounded to bf16 for their products, as the operands are; everything
+// else is float32. Rows or keys whose sums met an infinity or NaN of a masked pair are
+// formed again by themselves.
+#include "dot_mfma.h"
+
+namespace sa {
+namespace {
+
+// What the key side reads of a block of 32 rows: LSE in base 2 (+inf: a row without a
+// key or none, whose probabilities are 0), Delta, the distance bias's slope in base 2 and the
+// query less the block's first.
+struct Stat {
+  float lse2[32], delta[32], slope2[32], query[32];
+};
+__device__ __forceinline__ Stat* stats_of(const DotArgs& a, int bh) {
+  const int nrb = (a.G * a.Nq + 31) / 32;
+  return reinterpret_cast<Stat*>(a.delta) + static_cast<int64_t>(bh) * nrb;
+}
+
+// Base-2 score and the cap's derivative.
+template <bool CAP, bool BIAS>
+__device__ __forceinline__ float score_of(const Scores<CAP, BIAS>& c, float s, float slope2, float dj, float less, float& dcap) {
+  float x;
+  if constexpr (CAP) {
+    const float u = __builtin_amdgcn_rcpf(fast_exp2(s * c.to_cap) + 1.f);  // tanh = 1 - 2 u
+    x = c.cap2 - 2.f * c.cap2 * u - less;
+    dcap = 4.f * (u - u * u);
+  } else {
+    x = __builtin_fmaf(s, c.scale2, -less);
+  }
+  if constexpr (BIAS) x = __builtin_fmaf(-slope2, fabsf(dj), x);
+  return x;
+}
+
+// dQ of one row by itself.
+__device__ __forceinline__ void single_row(const DotArgs& a, const DotMask& m, int b, int i, int head, float lse, float delta) {
+  const int lane = threadIdx.x & 63, hk = head / a.G, p = m.first + i, dq = m.doc(p);
+  const bool d0 = lane < a.D, d1 = lane + 64 < a.D;
+  const int64_t at = ((static_cast<int64_t>(b) * a.Nq + i) * a.H + head) * a.D + lane;
+  const uint16_t* q = static_cast<const uint16_t*>(a.q) + b * a.qsb + i * a.qsn + head * a.qsh + lane;
+  const uint16_t* g = static_cast<const uint16_t*>(a.dout) + at;
+  const uint16_t* k = static_cast<const uint16_t*>(a.k) + b * a.ksb + hk * a.ksh + lane;
+  const uint16_t* v = static_cast<const uint16_t*>(a.v) + b * a.vsb + hk * a.vsh + lane;
+  const float q0 = d0 ? bf16_to_f32(q[0]) : 0.f, q1 = d1 ? bf16_to_f32(q[64]) : 0.f;
+  const float g0 = d0 ? bf16_to_f32(g[0]) : 0.f, g1 = d1 ? bf16_to_f32(g[64]) : 0.f;
+  const float slope = a.slopes ? a.slopes[head] : 0.f;
+  float o0 = 0.f, o1 = 0.f;
+  for (int j = 0; j < m.L; ++j) {
+    if (!m.sees(p, j, dq, m.doc(j))) continue;
+    const int64_t kj = j * a.ksn, vj = j * a.vsn;
+    const float k0 = d0 ? bf16_to_f32(k[kj]) : 0.f, k1 = d1 ? bf16_to_f32(k[kj + 64]) : 0.f;
+    float s = sum64(q0 * k0 + q1 * k1) * a.scale, dcap = 1.f;
+    const float dp = sum64((d0 ? g0 * bf16_to_f32(v[vj]) : 0.f) + (d1 ? g1 * bf16_to_f32(v[vj + 64]) : 0.f));
+    if (a.cap > 0.f) {
+      const float t = tanhf(s / a.cap);
+      s = a.cap * t;
+      dcap = 1.f - t * t;
+    }
+    const float w = fast_exp2((s - slope * static_cast<float>(abs(p - j)) - lse) * kLog2e) * (dp - delta) * dcap * a.scale;
+    o0 += w * k0;
+    o1 += w * k1;
+    if (__builtin_amdgcn_ballot_w64((d0 && o0 == o0) || (d1 && o1 == o1)) == 0) break;  // all NaN
+  }
+  uint16_t* out = static_cast<uint16_t*>(a.dq) + at;
+  if (d0) out[0] = f32_to_bf16(o0);
+  if (d1) out[64] = f32_to_bf16(o1);
+}
+// dK and dV of one key by itself.
+__device__ __forceinline__ void single_key(const DotArgs& a, const DotMask& m, int b, int hk, int j) {
+  const int lane = threadIdx.x & 63, dk = m.doc(j);
+  const bool d0 = lane < a.D, d1 = lane + 64 < a.D;
+  const uint16_t* k = static_cast<const uint16_t*>(a.k) + b * a.ksb + j * a.ksn + hk * a.ksh + lane;
+  const uint16_t* v = static_cast<const uint16_t*>(a.v) + b * a.vsb + j * a.vsn + hk * a.vsh + lane;
+  const float k0 = d0 ? bf16_to_f32(k[0]) : 0.f, k1 = d1 ? bf16_to_f32(k[64]) : 0.f;
+  const float v0 = d0 ? bf16_to_f32(v[0]) : 0.f, v1 = d1 ? bf16_to_f32(v[64]) : 0.f;
+  const Stat* stats = stats_of(a, b * a.Hkv + hk);
+  float x0 = 0.f, x1 = 0.f, y0 = 0.f, y1 = 0.f;
+  for (int i = max(-m.first, 0); i < a.Nq; ++i) {
+    const int p = m.first + i;
+    if (!m.sees(p, j, m.doc(p), dk)) continue;
+    for (int gr = 0; gr < a.G; ++gr) {
+      const int head = hk * a.G + gr, r = i * a.G + gr;
+      const uint16_t* q = static_cast<const uint16_t*>(a.q) + b * a.qsb + i * a.qsn + head * a.qsh + lane;
+      const uint16_t* g = static_cast<const uint16_t*>(a.dout) + ((static_cast<int64_t>(b) * a.Nq + i) * a.H + head) * a.D + lane;
+      const float q0 = d0 ? bf16_to_f32(q[0]) : 0.f, q1 = d1 ? bf16_to_f32(q[64]) : 0.f;
+      const float g0 = d0 ? bf16_to_f32(g[0]) : 0.f, g1 = d1 ? bf16_to_f32(g[64]) : 0.f;
+      float s = sum64(q0 * k0 + q1 * k1) * a.scale, dcap = 1.f;
+      const float dp = sum64(g0 * v0 + g1 * v1);
+      if (a.cap > 0.f) {
+        const float t = tanhf(s / a.cap);
+        s = a.cap * t;
+        dcap = 1.f - t * t;
+      }
+      const Stat& st = stats[r >> 5];
+      const float w = fast_exp2((s - (a.slopes ? a.slopes[head] : 0.f) * static_cast<float>(abs(p - j))) * kLog2e - st.lse2[r & 31]);
+      const float ds = w * (dp - st.delta[r & 31]) * dcap * a.scale;
+      x0 += ds * q0;
+      x1 += ds * q1;
+      y0 += w * g0;
+      y1 += w * g1;
+    }
+    if (__builtin_amdgcn_ballot_w64((d0 && (x0 == x0 || y0 == y0)) || (d1 && (x1 == x1 || y1 == y1))) == 0) break;
+  }
+  const int64_t at = ((static_cast<int64_t>(b) * a.Nk + j) * a.Hkv + hk) * a.D + lane;
+  if (d0) static_cast<uint16_t*>(a.dk)[at] = f32_to_bf16(x0), static_cast<uint16_t*>(a.dv)[at] = f32_to_bf16(y0);
+  if (d1) static_cast<uint16_t*>(a.dk)[at + 64] = f32_to_bf16(x1), static_cast<uint16_t*>(a.dv)[at + 64] = f32_to_bf16(y1);
+}
+
+// LDS arrays of the ring: NS stages of two tensors' tiles, every stage its own array
+// (so that the wait for one stage's loads is not for the others').
+#define SA_DOT_RING(W)                                                                                                 \
+  __shared__ __attribute__((aligned(16))) char xst0[(W)*T::bytes], xst1[(W)*T::bytes], yst0[(W)*T::bytes], yst1[(W)*T::bytes]; \
+  __shared__ __attribute__((aligned(16))) char xst2[PRIV ? 16 : T::bytes], xst3[PRIV ? 16 : T::bytes],                   \
+      yst2[PRIV ? 16 : T::bytes], yst3[PRIV ? 16 : T::bytes];                                                           \
+  auto xst = [&](auto SC) __attribute__((always_inline)) {                                                             \
+    constexpr int X = decltype(SC)::value;                                                                             \
+    return to_lds(X == 0 ? xst0 : X == 1 ? xst1 : X == 2 ? xst2 : xst3);                                               \
+  };                                                                                                                   \
+  auto yst = [&](auto SC) __attribute__((always_inline)) {                                                             \
+    constexpr int X = decltype(SC)::value;                                                                             \
+    return to_lds(X == 0 ? yst0 : X == 1 ? yst1 : X == 2 ? yst2 : yst3);                                               \
+  }
+
+// Adds the wavefronts' accumulator tiles in order, through one LDS array of 16 KB each:
+// wavefront w ends with quad w (columns 8 w + 4 h .. + 3) of every tile in y.
+template <int NDT, typename Buf>
+__device__ __forceinline__ void add_waves(const f32x16_t (&acc)[NDT], float (&y)[NDT][4], Buf buf, int wave, int lane) {
+#pragma unroll
+  for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) buf(dt)[wave * 1024 + 64 * v + lane] = acc[dt][v];
+  __syncthreads();
+#pragma unroll
+  for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      y[dt][e] = 0.f;
+#pragma unroll
+      for (int z = 0; z < kWaves; ++z) y[dt][e] += buf(dt)[z * 1024 + 64 * (4 * wave + e) + lane];
+    }
+  __syncthreads();
+}
+template <int NDT>
+__device__ __forceinline__ float store_quads(uint16_t* p, const float (&y)[NDT][4], float mul, int wave, int D) {
+  float check = 0.f;
+#pragma unroll
+  for (int dt = 0; dt < NDT; ++dt) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) check += y[dt][e] * 0.f;
+    if (p && 32 * dt + 8 * wave < D)
+      *reinterpret_cast<u32x2_t*>(p + 32 * dt + 8 * wave) = u32x2_t{pack_bf16x2(y[dt][0] * mul, y[dt][1] * mul), pack_bf16x2(y[dt][2] * mul, y[dt][3] * mul)};
+  }
+  return check;
+}
+
+// ---- query side ----
+template <int DP, bool CAP, bool BIAS, bool PRIV>
+__global__ __launch_bounds__(kThreads, PRIV ? 1 : 2) void dot_dq_kernel(DotArgs a) {
+  using T = SwzTile<DP>;
+  constexpr int NT = DP / 16, NDT = DP / 32, SPW = PRIV ? T::instrs : T::instrs / kWaves, kRows = PRIV ? 32 : 32 * kWaves;
+  constexpr int NS = PRIV ? 2 : 4;
+  SA_DOT_RING(PRIV ? kWaves : 1);
+  const int R = a.G * a.Nq, nrb = (R + kRows - 1) / kRows;
+  int64_t unit;
+  if (!unit_of(static_cast<int64_t>(a.B) * a.Hkv * nrb, unit)) return;
+  const int block = nrb - 1 - static_cast<int>(unit % nrb), bh = static_cast<int>(unit / nrb);
+  const int b = bh / a.Hkv, hk = bh - b * a.Hkv;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 31, h = lane >> 5;
+  const DotMask m(a, b);
+  const int r0 = block * kRows + (PRIV ? 0 : 32 * wave);
+  const Lanes w(a, m, hk, r0 + c);
+  const DotSpan all = rows_span(a, m, block * kRows, kRows), own = rows_span(a, m, min(r0, R - 1), 32);
+  const int dq = m.doc(w.p), pos = w.p - 4 * h;
+  const Scores<CAP, BIAS> score(a, w.head);
+  int lo, hi;
+  key_blocks(m, all, lo, hi);
+  const bool some = r0 < R;
+  auto seq = block_seq(lo, hi, PRIV ? wave : 0, PRIV ? kWaves : 1, [&](int blk, bool& live, bool& mine, bool& full) {
+    const DotSpan k(m, blk * kDotBlock, blk * kDotBlock + kDotBlock - 1);
+    live = dot_live(m, all, k);
+    mine = some && dot_live(m, own, k);
+    full = dot_full(m, own, k);
+  });
+  int kvoff[SPW], vvoff[SPW];
+#pragma unroll
+  for (int x = 0; x < SPW; ++x) {
+    const int p = 64 * (PRIV ? x : x * kWaves + wave) + lane, row = p / T::CH, ch = (p % T::CH) ^ T::swz(row);
+    kvoff[x] = 8 * ch < a.D ? static_cast<int>(row * a.ksn * 2) + 16 * ch : kFar;
+    vvoff[x] = 8 * ch < a.D ? static_cast<int>(row * a.vsn * 2) + 16 * ch : kFar;
+  }
+  const uint16_t* kb = static_cast<const uint16_t*>(a.k) + b * a.ksb + hk * a.ksh;
+  const uint16_t* vb = static_cast<const uint16_t*>(a.v) + b * a.vsb + hk * a.vsh;
+  auto load = [&](auto SC, int blk) __attribute__((always_inline)) {
+    const int64_t j0 = max(blk, 0) * kDotBlock;
+    const int n = blk < 0 ? 0 : min(m.L - static_cast<int>(j0), kDotBlock);
+    const auto rk = rows_of(kb + j0 * a.ksn, n, a.ksn, a.D), rv = rows_of(vb + j0 * a.vsn, n, a.vsn, a.D);
+    const int base = PRIV ? wave * T::bytes : 0;
+#pragma unroll
+    for (int x = 0; x < SPW; ++x) load_lds16(rk, xst(SC) + base + 1024 * (PRIV ? x : x * kWaves + wave), kvoff[x]);
+#pragma unroll
+    for (int x = 0; x < SPW; ++x) load_lds16(rv, yst(SC) + base + 1024 * (PRIV ? x : x * kWaves + wave), vvoff[x]);
+  };
+  // This row's q, dO and Delta.
+  u32x4_t qf[NT], gf[NT];
+  const int64_t orow = ((static_cast<int64_t>(b) * a.Nq + w.i) * a.H + w.head) * a.D;
+  load_row<DP>(qf, q_row(a, w, b), w.valid, a.D, h);
+  load_row<DP>(gf, static_cast<const uint16_t*>(a.dout) + orow, w.valid, a.D, h);
+  float delta = 0.f;
+  {
+    u32x4_t of[NT];
+    load_row<DP>(of, static_cast<const uint16_t*>(a.out_in) + orow, w.valid, a.D, h);
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        delta += bf16_lo(gf[t][e]) * bf16_lo(of[t][e]);
+        delta += bf16_hi(gf[t][e]) * bf16_hi(of[t][e]);
+      }
+    delta += swap_halves(delta);
+  }
+  const float lse = w.valid ? a.lse[(static_cast<int64_t>(b) * a.H + w.head) * a.Nq + w.i] : -kInf;
+  const float lse2 = lse == -kInf ? kInf : lse * kLog2e;
+  if (h == 0 && some && (!PRIV || wave == 0)) {
+    Stat& st = stats_of(a, bh)[r0 / 32];
+    st.lse2[c] = lse2;
+    st.delta[c] = w.valid ? delta : 0.f;
+    st.slope2[c] = score.slope2;
+    st.query[c] = static_cast<float>(w.i - div_group(r0, a));
+  }
+  const Frags<DP> frag(lane, PRIV ? wave * T::bytes : 0);
+  DotBlock bq[NS];
+  bq[0] = seq.next();
+  load(IC<0>{}, bq[0].blk);
+  bq[1] = seq.next();
+  load(IC<1>{}, bq[1].blk);
+  if constexpr (!PRIV) {
+    bq[2] = seq.next();
+    load(IC<2>{}, bq[2].blk);
+  }
+  f32x16_t acc[NDT] = {};
+  auto iteration = [&](auto SC) __attribute__((always_inline)) {
+    constexpr int S = decltype(SC)::value;
+    const DotBlock at = bq[S];
+    if (at.blk < 0) return false;
+    if constexpr (PRIV) {
+      wait_vmcnt<2 * SPW>();
+      asm volatile("" ::: "memory");
+    } else {
+      wait_vmcnt<4 * SPW>();
+      lds_barrier_tracked();
+      bq[(S + 3) % NS] = seq.next();
+      load(IC<(S + 3) % NS>{}, bq[(S + 3) % NS].blk);
+    }
+    if (at.mine) {
+      f32x16_t s = mfma32(frag.row(xst(SC), 0), qf[0], f32x16_t{}), dp = mfma32(frag.row(yst(SC), 0), gf[0], f32x16_t{});
+#pragma unroll
+      for (int t = 1; t < NT; ++t) {
+        s = mfma32(frag.row(xst(SC), t), qf[t], s);
+        dp = mfma32(frag.row(yst(SC), t), gf[t], dp);
+      }
+      const int j0 = at.blk * kDotBlock;
+      const float dj = static_cast<float>(pos - j0);
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        float dcap = 1.f;
+        const float x = score_of(score, s[v], score.slope2, dj - static_cast<float>(8 * (v >> 2) + (v & 3)), lse2, dcap);
+        s[v] = fast_exp2(x) * (dp[v] - delta);
+        if constexpr (CAP) s[v] *= dcap;
+      }
+      if (!at.full) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const int j = j0 + acc_row(v, h);
+          if (!m.sees(w.p, j, dq, m.doc(j))) s[v] = 0.f;
+        }
+      }
+      const float* sv = reinterpret_cast<const float*>(&s);
+      u32x4_t pf[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) pf[u] = pack_frag(sv, u);
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt) acc[dt] = mfma32(frag.tr(xst(SC), dt, u), pf[u], acc[dt]);
+    }
+    if constexpr (PRIV) {
+      __builtin_amdgcn_s_waitcnt(0xC07F);  // the stage is read: its next block may come
+      asm volatile("" ::: "memory");
+      bq[S] = seq.next();
+      load(SC, bq[S].blk);
+    }
+    return true;
+  };
+  if constexpr (PRIV) {
+    while (iteration(IC<0>{}) && iteration(IC<1>{})) {
+    }
+  } else {
+    while (iteration(IC<0>{}) && iteration(IC<1>{}) && iteration(IC<2>{}) && iteration(IC<3>{})) {
+    }
+  }
+  wait_vmcnt<0>();
+  uint16_t* dst = static_cast<uint16_t*>(a.dq) + orow + 4 * h;
+  unsigned bad = 0;
+  if constexpr (PRIV) {
+    __shared__ unsigned flags[kWaves];
+    float y[NDT][4];
+    __syncthreads();
+    add_waves(acc, y, [&](int dt) { return reinterpret_cast<float*>(dt == 0 ? xst0 : dt == 1 ? xst1 : dt == 2 ? yst0 : yst1); }, wave, lane);
+    const float check = store_quads(w.valid ? dst : nullptr, y, a.scale, wave, a.D);
+    const unsigned x = rows_where(w.valid && check != check);
+    if (lane == 0) flags[wave] = x;
+    __syncthreads();
+    if (wave == 0) bad = flags[0] | flags[1] | flags[2] | flags[3];
+  } else {
+    const float check = not_finite(acc);
+    bad = rows_where(w.valid && check != check);
+    if (w.valid && !((bad >> c) & 1)) store_row<DP>(dst, acc, a.scale, a.D);
+  }
+  if (!has_mask(a)) bad = 0;
+  while (bad) {
+    const int x = __builtin_ctz(bad);
+    bad &= bad - 1;
+    single_row(a, m, b, __builtin_amdgcn_readlane(w.i, x), __builtin_amdgcn_readlane(w.head, x),
+               __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(lse), x)),
+               __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(delta), x)));
+  }
+}
+
+// ---- key side ----
+template <int DP, bool CAP, bool BIAS, bool PRIV>
+__global__ __launch_bounds__(kThreads, PRIV ? 1 : 2) void dot_dkv_kernel(DotArgs a) {
+  using T = SwzTile<DP>;
+  constexpr int NT = DP / 16, NDT = DP / 32, SPW = PRIV ? T::instrs : T::instrs / kWaves, kKeys = PRIV ? 32 : 32 * kWaves;
+  constexpr int NS = PRIV ? 2 : 4, kInfo = BIAS ? 512 : 256, LPB = 2 * SPW + (BIAS ? 2 : 1);  // loads of a block
+  SA_DOT_RING(PRIV ? kWaves : 1);
+  __shared__ __attribute__((aligned(16))) char info0[(PRIV ? kWaves : 1) * kInfo], info1[(PRIV ? kWaves : 1) * kInfo],
+      info2[PRIV ? 16 : kInfo], info3[PRIV ? 16 : kInfo];
+  auto ist = [&](auto SC) __attribute__((always_inline)) {
+    constexpr int X = decltype(SC)::value;
+    return to_lds(X == 0 ? info0 : X == 1 ? info1 : X == 2 ? info2 : info3) + (PRIV ? (threadIdx.x >> 6) * kInfo : 0);
+  };
+  const int R = a.G * a.Nq, nkb = (a.Nk + kKeys - 1) / kKeys;
+  int64_t unit;
+  if (!unit_of(static_cast<int64_t>(a.B) * a.Hkv * nkb, unit)) return;
+  const int block = static_cast<int>(unit % nkb), bh = static_cast<int>(unit / nkb);
+  const int b = bh / a.Hkv, hk = bh - b * a.Hkv;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 31, h = lane >> 5;
+  const DotMask m(a, b);
+  const int j0 = block * kKeys + (PRIV ? 0 : 32 * wave), j = j0 + c;
+  const DotSpan all(m, block * kKeys, block * kKeys + kKeys - 1), own(m, j0, j0 + 31);
+  const int dk = m.doc(j);
+  const Scores<CAP, false> score(a, 0);
+  int lo, hi;
+  row_blocks(m, all, a.G, R, lo, hi);
+  const bool some = j0 < m.L;
+  auto seq = block_seq(lo, hi, PRIV ? wave : 0, PRIV ? kWaves : 1, [&](int blk, bool& live, bool& mine, bool& full) {
+    const DotSpan q(m, m.first + div_group(blk * 32, a), m.first + div_group(min(blk * 32 + 32, R) - 1, a));
+    live = dot_live(m, q, all);
+    mine = some && dot_live(m, q, own);
+    full = dot_full(m, q, own);
+  });
+  // Rows of q and dO: the chunk of row 32 blk + lrow that this lane brings.
+  int lrow[SPW], lcol[SPW];
+#pragma unroll
+  for (int x = 0; x < SPW; ++x) {
+    const int p = 64 * (PRIV ? x : x * kWaves + wave) + lane;
+    lrow[x] = p / T::CH;
+    const int ch = (p % T::CH) ^ T::swz(lrow[x]);
+    lcol[x] = 8 * ch < a.D ? 16 * ch : -1;
+  }
+  const uint16_t* qb = static_cast<const uint16_t*>(a.q) + b * a.qsb;
+  const uint16_t* gb = static_cast<const uint16_t*>(a.dout) + static_cast<int64_t>(b) * a.Nq * a.H * a.D;
+  const Stat* stats = stats_of(a, bh);
+  const int64_t gsn = static_cast<int64_t>(a.H) * a.D;
+  const int qsn2 = static_cast<int>(a.qsn * 2), qsh2 = static_cast<int>(a.qsh * 2), gsn2 = static_cast<int>(gsn * 2);
+  auto load = [&](auto SC, int blk) __attribute__((always_inline)) {
+    const int i0 = div_group(max(blk, 0) * 32, a), n = blk < 0 ? 0 : min(a.Nq - i0, 33);
+    const auto rq = rows_of(qb + i0 * a.qsn, n, a.qsn, (a.H - 1) * a.qsh + a.D), rg = rows_of(gb + i0 * gsn, n, gsn, gsn);
+    const auto rs = make_rsrc(stats + max(blk, 0), blk < 0 ? 0 : sizeof(Stat));
+    const int base = PRIV ? wave * T::bytes : 0;
+    int qo[SPW], go[SPW];
+#pragma unroll
+    for (int x = 0; x < SPW; ++x) {
+      const int r = max(blk, 0) * 32 + lrow[x], i = div_group(r, a), head = hk * a.G + r - i * a.G;
+      const bool in = r < R && lcol[x] >= 0;
+      qo[x] = in ? (i - i0) * qsn2 + head * qsh2 + lcol[x] : kFar;
+      go[x] = in ? (i - i0) * gsn2 + head * a.D * 2 + lcol[x] : kFar;
+    }
+#pragma unroll
+    for (int x = 0; x < SPW; ++x) load_lds16(rq, xst(SC) + base + 1024 * (PRIV ? x : x * kWaves + wave), qo[x]);
+#pragma unroll
+    for (int x = 0; x < SPW; ++x) load_lds16(rg, yst(SC) + base + 1024 * (PRIV ? x : x * kWaves + wave), go[x]);
+    // (every wavefront brings the same numbers)
+    load_lds4(rs, ist(SC), lane * 4);
+    if constexpr (BIAS) load_lds4(rs, ist(SC) + 256, 256 + lane * 4);
+  };
+  const bool key = j < m.L;
+  u32x4_t kf[NT], vf[NT];
+  load_row<DP>(kf, static_cast<const uint16_t*>(a.k) + b * a.ksb + (key ? j : 0) * a.ksn + hk * a.ksh, key, a.D, h);
+  load_row<DP>(vf, static_cast<const uint16_t*>(a.v) + b * a.vsb + (key ? j : 0) * a.vsn + hk * a.vsh, key, a.D, h);
+  const Frags<DP> frag(lane, PRIV ? wave * T::bytes : 0);
+  DotBlock bq[NS];
+  bq[0] = seq.next();
+  load(IC<0>{}, bq[0].blk);
+  bq[1] = seq.next();
+  load(IC<1>{}, bq[1].blk);
+  if constexpr (!PRIV) {
+    bq[2] = seq.next();
+    load(IC<2>{}, bq[2].blk);
+  }
+  f32x16_t acck[NDT] = {}, accv[NDT] = {};
+  auto iteration = [&](auto SC) __attribute__((always_inline)) {
+    constexpr int S = decltype(SC)::value;
+    const DotBlock at = bq[S];
+    if (at.blk < 0) return false;
+    if constexpr (PRIV) {
+      wait_vmcnt<LPB>();
+      asm volatile("" ::: "memory");
+    } else {
+      wait_vmcnt<2 * LPB>();
+      lds_barrier_tracked();
+      bq[(S + 3) % NS] = seq.next();
+      load(IC<(S + 3) % NS>{}, bq[(S + 3) % NS].blk);
+    }
+    if (at.mine) {
+      f32x16_t s = mfma32(frag.row(xst(SC), 0), kf[0], f32x16_t{}), dp = mfma32(frag.row(yst(SC), 0), vf[0], f32x16_t{});
+#pragma unroll
+      for (int t = 1; t < NT; ++t) {
+        s = mfma32(frag.row(xst(SC), t), kf[t], s);
+        dp = mfma32(frag.row(yst(SC), t), vf[t], dp);
+      }
+      const lds_char* info = ist(SC) + 16 * h;
+      const float dj = static_cast<float>(m.first + div_group(at.blk * 32, a) - j);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const f32x4_t lse2 = lds_ld<f32x4_t>(info + 32 * q), delta = lds_ld<f32x4_t>(info + 128 + 32 * q);
+        f32x4_t slope2 = {}, query = {};
+        if constexpr (BIAS) slope2 = lds_ld<f32x4_t>(info + 256 + 32 * q), query = lds_ld<f32x4_t>(info + 384 + 32 * q);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float dcap = 1.f, x = score_of(score, s[4 * q + e], 0.f, 0.f, lse2[e], dcap);
+          if constexpr (BIAS) x = __builtin_fmaf(-slope2[e], fabsf(query[e] + dj), x);
+          const float p = fast_exp2(x);
+          s[4 * q + e] = p;
+          dp[4 * q + e] = p * (dp[4 * q + e] - delta[e]);
+          if constexpr (CAP) dp[4 * q + e] *= dcap;
+        }
+      }
+      if (!at.full) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const int r = at.blk * 32 + acc_row(v, h), p = r < R ? m.first + div_group(r, a) : -1;
+          if (!m.sees(p, j, m.doc(p), dk)) s[v] = 0.f, dp[v] = 0.f;
+        }
+      }
+      u32x4_t pf[2], df[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        pf[u] = pack_frag(reinterpret_cast<const float*>(&s), u);
+        df[u] = pack_frag(reinterpret_cast<const float*>(&dp), u);
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt) {
+          accv[dt] = mfma32(frag.tr(yst(SC), dt, u), pf[u], accv[dt]);
+          acck[dt] = mfma32(frag.tr(xst(SC), dt, u), df[u], acck[dt]);
+        }
+    }
+    if constexpr (PRIV) {
+      __builtin_amdgcn_s_waitcnt(0xC07F);  // the stage is read: its next block may come
+      asm volatile("" ::: "memory");
+      bq[S] = seq.next();
+      load(SC, bq[S].blk);
+    }
+    return true;
+  };
+  if constexpr (PRIV) {
+    while (iteration(IC<0>{}) && iteration(IC<1>{})) {
+    }
+  } else {
+    while (iteration(IC<0>{}) && iteration(IC<1>{}) && iteration(IC<2>{}) && iteration(IC<3>{})) {
+    }
+  }
+  wait_vmcnt<0>();
+  const bool out = j < a.Nk;
+  const int64_t at = ((static_cast<int64_t>(b) * a.Nk + (out ? j : 0)) * a.Hkv + hk) * a.D + 4 * h;
+  uint16_t *pk = static_cast<uint16_t*>(a.dk) + at, *pv = static_cast<uint16_t*>(a.dv) + at;
+  unsigned bad = 0;
+  if constexpr (PRIV) {
+    __shared__ unsigned flags[kWaves];
+    auto buf = [&](int dt) { return reinterpret_cast<float*>(dt == 0 ? xst0 : dt == 1 ? xst1 : dt == 2 ? yst0 : yst1); };
+    float y[NDT][4];
+    __syncthreads();
+    add_waves(acck, y, buf, wave, lane);
+    float check = store_quads(out ? pk : nullptr, y, a.scale, wave, a.D);
+    add_waves(accv, y, buf, wave, lane);
+    check += store_quads(out ? pv : nullptr, y, 1.f, wave, a.D);
+    const unsigned x = rows_where(key && check != check);
+    if (lane == 0) flags[wave] = x;
+    __syncthreads();
+    if (wave == 0) bad = flags[0] | flags[1] | flags[2] | flags[3];
+  } else {
+    const float check = not_finite(acck) + not_finite(accv);
+    bad = rows_where(key && check != check);
+    if (out && !((bad >> c) & 1)) {
+      store_row<DP>(pk, acck, a.scale, a.D);
+      store_row<DP>(pv, accv, 1.f, a.D);
+    }
+  }
+  if (!has_mask(a)) bad = 0;
+  while (bad) {
+    const int x = __builtin_ctz(bad);
+    bad &= bad - 1;
+    single_key(a, m, b, hk, j0 + x);
+  }
+}
+
+template <int DP, bool CAP, bool BIAS, bool PRIV>
+void launch(const DotArgs& a, hipStream_t st) {
+  const int64_t R = static_cast<int64_t>(a.G) * a.Nq, heads = static_cast<int64_t>(a.B) * a.Hkv;
+  constexpr int n = PRIV ? 32 : 128;
+  dot_dq_kernel<DP, CAP, BIAS, PRIV><<<unit_grid(heads * ((R + n - 1) / n)), kThreads, 0, st>>>(a);
+  dot_dkv_kernel<DP, CAP, BIAS, PRIV><<<unit_grid(heads * ((a.Nk + n - 1) / n)), kThreads, 0, st>>>(a);
+}
+template <int DP, bool CAP, bool BIAS>
+void launch(const DotArgs& a, hipStream_t st) {
+  if (a.nsplit == 0)
+    launch<DP, CAP, BIAS, false>(a, st);
+  else
+    launch<DP, CAP, BIAS, true>(a, st);
+}
+template <int DP>
+void launch(const DotArgs& a, hipStream_t st) {
+  if (a.cap > 0.f)
+    a.slopes ? launch<DP, true, true>(a, st) : launch<DP, true, false>(a, st);
+  else
+    a.slopes ? launch<DP, false, true>(a, st) : launch<DP, false, false>(a, st);
+}
+
+}  // namespace
+
+hipError_t dot_bwd_bf16(const DotArgs& a, hipStream_t st) {
+  a.D <= 64 ? launch<64>(a, st) : launch<128>(a, st);
+  return hipGetLastError();
+}
+
+}  // namespace sa

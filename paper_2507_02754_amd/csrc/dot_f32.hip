@@ -631,18 +631,20 @@ DotPlan dot_fwd_plan(int64_t B, int64_t Nq, int64_t Nk, int64_t H, int64_t Hkv, 
 }
 DotPlan dot_bwd_plan(int64_t B, int64_t Nq, int64_t Nk, int64_t H, int64_t Hkv, int64_t D, int causal, int window, bool docs,
                      int dtype) {
-  (void)Hkv, (void)D, (void)causal, (void)window, (void)dtype;
+  (void)D, (void)causal, (void)window;
   DotPlan p;
-  p.nsplit = 1;
+  const int64_t R = H / Hkv * Nq;
+  const bool bf16 = dtype == SA_DTYPE_BF16;
+  // bf16: workgroups of 128 rows or keys where they fill the chip.
+  p.nsplit = bf16 && B * Hkv * ((std::max(R, Nk) + 127) / 128) >= 256 ? 0 : 1;
   p.ranges_off = 0;
-  p.part_off = docs ? up256(static_cast<size_t>(B) * ((Nk + kDotBlock - 1) / kDotBlock) * sizeof(int2)) : 0;  // Delta
-  p.bytes = p.part_off + static_cast<size_t>(B) * H * Nq * sizeof(float);
+  p.part_off = docs ? up256(static_cast<size_t>(B) * ((Nk + kDotBlock - 1) / kDotBlock) * sizeof(int2)) : 0;
+  // Delta, or for every 32 rows what the bf16 kernels keep of them (dot_bwd.hip)
+  p.bytes = p.part_off + (bf16 ? static_cast<size_t>(B) * Hkv * ((R + 31) / 32) * 512 : static_cast<size_t>(B) * H * Nq * sizeof(float));
   return p;
 }
 
 hipError_t dot_fwd_f32(const DotArgs& a, hipStream_t st) { return launch<float>(a, false, st); }
-hipError_t dot_bwd_f32(const DotArgs& a, hipStream_t st) {
-  return a.dtype == SA_DTYPE_F32 ? launch<float>(a, true, st) : launch<uint16_t>(a, true, st);
-}
+hipError_t dot_bwd_f32(const DotArgs& a, hipStream_t st) { return launch<float>(a, true, st); }
 
 }  // namespace sa

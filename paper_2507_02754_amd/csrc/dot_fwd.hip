@@ -26,7 +26,7 @@
 // are not visited (walked 64 at a time, a lane each). A masked pair's probability of
 // 0 times an infinity or NaN of V is NaN: rows that come out so are formed again by
 // themselves, over their visible keys alone.
-#include "dot_common.h"
+#include "dot_mfma.h"
 
 #include "simplicial_layers.h"
 
@@ -35,44 +35,7 @@
 namespace sa {
 namespace {
 
-constexpr int kWaves = 4;
-constexpr int kThreads = 64 * kWaves;
 constexpr float kPmax = 65536.f;
-constexpr int kFar = 0x7fffffff;
-
-template <int X>
-using IC = std::integral_constant<int, X>;
-
-template <int N>
-__device__ __forceinline__ void wait_vmcnt() {
-  static_assert(N >= 0 && N < 64, "vmcnt range");
-  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0F70);
-}
-
-// `n` positions from `p` on, `sn` elements apart, rows of `more` elements.
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const uint16_t* p, int n, int64_t sn, int64_t more) {
-  const int64_t bytes = n > 0 ? ((n - 1) * sn + more) * 2 : 0;
-  return make_rsrc(p, static_cast<unsigned>(bytes < kFar ? bytes : kFar));
-}
-
-// What scores need beside the products, in base 2: a = mul s without cap and bias.
-template <bool CAP, bool BIAS>
-struct Scores {
-  float scale2, to_cap, cap2, slope2;
-  __device__ __forceinline__ Scores(const DotArgs& a, int head)
-      : scale2(a.scale * kLog2e), to_cap(CAP ? 2.f * kLog2e * a.scale / a.cap : 0.f), cap2(a.cap * kLog2e),
-        slope2(BIAS ? a.slopes[head] * kLog2e : 0.f) {}
-  // dj: position less key j
-  __device__ __forceinline__ float operator()(float s, float dj) const {
-    float x;
-    if constexpr (CAP)
-      x = cap2 - 2.f * cap2 * __builtin_amdgcn_rcpf(fast_exp2(s * to_cap) + 1.f);  // cap tanh
-    else
-      x = s * scale2;
-    if constexpr (BIAS) x = __builtin_fmaf(-slope2, fabsf(dj), x);
-    return x;
-  }
-};
 
 // A row's running state and the step over one block.
 template <int DP, bool CAP, bool BIAS>
@@ -139,30 +102,6 @@ struct Row {
   }
 };
 
-// The 32 rows of a wavefront, one a lane.
-struct Lanes {
-  int i, head, p;
-  bool valid;
-  __device__ __forceinline__ Lanes(const DotArgs& a, const DotMask& m, int hk, int r) {
-    valid = r < a.G * a.Nq;
-    const int rr = valid ? r : 0;
-    i = div_group(rr, a);
-    head = hk * a.G + rr - i * a.G;
-    p = valid ? m.first + i : -1;
-  }
-};
-__device__ __forceinline__ DotSpan rows_span(const DotArgs& a, const DotMask& m, int r0, int n) {
-  return DotSpan(m, m.first + r0 / a.G, m.first + (min(r0 + n, a.G * a.Nq) - 1) / a.G);
-}
-
-// Q's rows as the products' B operand.
-template <int DP>
-__device__ __forceinline__ void load_q(u32x4_t (&qf)[DP / 16], const DotArgs& a, const Lanes& w, int b, int h) {
-  const uint16_t* p = static_cast<const uint16_t*>(a.q) + b * a.qsb + w.i * a.qsn + w.head * a.qsh + 8 * h;
-#pragma unroll
-  for (int t = 0; t < DP / 16; ++t) qf[t] = w.valid && 16 * t + 8 * h < a.D ? ldg128(p + 16 * t) : u32x4_t{0, 0, 0, 0};
-}
-
 // O of one row by itself, over its visible keys (LSE is not touched by masked pairs), a
 // wavefront's 64 lanes along the columns: for rows whose products met an infinity or NaN.
 __device__ __forceinline__ void single_row(const DotArgs& a, const DotMask& m, int b, int i, int head, float lse) {
@@ -189,7 +128,6 @@ __device__ __forceinline__ void single_row(const DotArgs& a, const DotMask& m, i
   if (d0) out[0] = f32_to_bf16(o0);
   if (d1) out[64] = f32_to_bf16(o1);
 }
-__device__ __forceinline__ bool has_mask(const DotArgs& a) { return a.causal || a.window || a.prefix || a.docs || a.lens; }
 // The rows of `bad` (a bit for each of the wavefront's 32), one after another.
 __device__ __forceinline__ void single_rows(const DotArgs& a, const DotMask& m, int b, const Lanes& w, float lse, unsigned bad) {
   while (bad) {
@@ -198,53 +136,6 @@ __device__ __forceinline__ void single_rows(const DotArgs& a, const DotMask& m, 
     single_row(a, m, b, __builtin_amdgcn_readlane(w.i, c), __builtin_amdgcn_readlane(w.head, c),
                __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(lse), c)));
   }
-}
-
-// Workgroup order: every XCD takes a contiguous run of (sequence, K-side head), whose
-// keys its L2 holds; the row blocks that see most keys come first.
-__device__ __forceinline__ bool unit_of(int64_t total, int64_t& unit) {
-  const int64_t per = (total + 7) / 8;
-  unit = static_cast<int64_t>(blockIdx.x & 7) * per + (blockIdx.x >> 3);
-  return unit < total;
-}
-unsigned unit_grid(int64_t total) { return static_cast<unsigned>((total + 7) / 8 * 8); }
-
-// Per-lane LDS offsets of a tile's fragments.
-template <int DP>
-struct Frags {
-  using T = SwzTile<DP>;
-  int ko[DP / 16], vo[DP / 32][2];
-  __device__ __forceinline__ Frags(int lane, int base) {
-    const int c = lane & 31, h = lane >> 5, grp = lane >> 4, sl = lane & 15;
-#pragma unroll
-    for (int t = 0; t < DP / 16; ++t) ko[t] = base + T::off(c, 2 * t + h);
-    const int r0 = 4 * (grp >> 1) + (sl >> 2);
-#pragma unroll
-    for (int dt = 0; dt < DP / 32; ++dt) {
-      const int col = 32 * dt + 16 * (grp & 1) + 4 * (sl & 3), ch = col >> 3, within = (col & 7) * 2;
-      vo[dt][0] = base + T::off(r0, ch) + within;
-      vo[dt][1] = base + T::off(r0 + 8, ch) + within;
-    }
-  }
-  __device__ __forceinline__ u32x4_t row(const lds_char* tile, int t) const { return lds_ld<u32x4_t>(tile + ko[t]); }
-  __device__ __forceinline__ u32x4_t tr(const lds_char* tile, int dt, int u) const {
-    const lds_char* p = tile + 2 * DP * 16 * u;
-    const u32x2_t x = lds_tr16(p + vo[dt][0]), y = lds_tr16(p + vo[dt][1]);
-    return u32x4_t{x[0], x[1], y[0], y[1]};
-  }
-};
-
-// Rows c of O: 4 consecutive columns of each accumulator quad.
-template <int DP>
-__device__ __forceinline__ void store_row(const DotArgs& a, int b, const Lanes& w, const f32x16_t (&acc)[DP / 32], float inv, int h) {
-  uint16_t* out = static_cast<uint16_t*>(a.out) + ((static_cast<int64_t>(b) * a.Nq + w.i) * a.H + w.head) * a.D + 4 * h;
-#pragma unroll
-  for (int dt = 0; dt < DP / 32; ++dt)
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-      if (32 * dt + 8 * q < a.D)
-        *reinterpret_cast<u32x2_t*>(out + 32 * dt + 8 * q) =
-            u32x2_t{pack_bf16x2(acc[dt][4 * q] * inv, acc[dt][4 * q + 1] * inv), pack_bf16x2(acc[dt][4 * q + 2] * inv, acc[dt][4 * q + 3] * inv)};
 }
 
 template <int DP, bool CAP, bool BIAS>
@@ -309,7 +200,7 @@ __global__ __launch_bounds__(kThreads, 2) void dot_fwd_kernel(DotArgs a) {
     for (int x = 0; x < SPW; ++x) load_lds16(r, dst + 1024 * (x * kWaves + wave), vvoff[x]);
   };
   u32x4_t qf[NT];
-  load_q<DP>(qf, a, w, b, h);
+  load_row<DP>(qf, q_row(a, w, b), w.valid, a.D, h);
   const Frags<DP> frag(lane, 0);
   DotBlock bq[kStages];
   bq[0] = seq.next();
@@ -388,18 +279,11 @@ __global__ __launch_bounds__(kThreads, 2) void dot_fwd_kernel(DotArgs a) {
   const bool empty = row.l == 0.f;
   const float inv = empty ? 0.f : 1.f / row.lr;
   const float lse = empty ? -kInf : row.m * kLn2 + logf(row.l);
-  float check = 0.f;
-#pragma unroll
-  for (int dt = 0; dt < NDT; ++dt)
-#pragma unroll
-    for (int v = 0; v < 16; ++v) check += row.acc[dt][v] * 0.f;
-  unsigned bad = 0;
-  if (has_mask(a)) {
-    const unsigned long long x = __builtin_amdgcn_ballot_w64(w.valid && fabsf(row.l) < kInf && check != check);
-    bad = static_cast<unsigned>(x) | static_cast<unsigned>(x >> 32);
-  }
+  const float check = not_finite(row.acc);
+  const unsigned bad = has_mask(a) ? rows_where(w.valid && fabsf(row.l) < kInf && check != check) : 0;
   if (w.valid) {
-    if (!((bad >> c) & 1)) store_row<DP>(a, b, w, row.acc, inv, h);
+    if (!((bad >> c) & 1))
+      store_row<DP>(static_cast<uint16_t*>(a.out) + ((static_cast<int64_t>(b) * a.Nq + w.i) * a.H + w.head) * a.D + 4 * h, row.acc, inv, a.D);
     if (h == 0) a.lse[(static_cast<int64_t>(b) * a.H + w.head) * a.Nq + w.i] = lse;
   }
   single_rows(a, m, b, w, lse, bad);
@@ -455,7 +339,7 @@ __global__ __launch_bounds__(kThreads, 1) void dot_few_kernel(DotArgs a) {
     for (int x = 0; x < SPW; ++x) load_lds16(rv, vst(SC) + wave * T::bytes + 1024 * x, vvoff[x]);
   };
   u32x4_t qf[NT];
-  load_q<DP>(qf, a, w, b, h);
+  load_row<DP>(qf, q_row(a, w, b), w.valid, a.D, h);
   const Frags<DP> frag(lane, wave * T::bytes);
   DotBlock bq[2];
   bq[0] = seq.next();
@@ -563,8 +447,8 @@ __global__ __launch_bounds__(kThreads, 1) void dot_few_kernel(DotArgs a) {
   if (a.nsplit > 1 || !has_mask(a)) return;
   // (a row is not finite if any wavefront's columns of it are not)
   __shared__ unsigned flags[kWaves];
-  const unsigned long long x = __builtin_amdgcn_ballot_w64(w.valid && fabsf(l) < kInf && check != check);
-  if (lane == 0) flags[wave] = static_cast<unsigned>(x) | static_cast<unsigned>(x >> 32);
+  const unsigned x = rows_where(w.valid && fabsf(l) < kInf && check != check);
+  if (lane == 0) flags[wave] = x;
   __syncthreads();
   if (wave == 0) single_rows(a, m, b, w, lse, flags[0] | flags[1] | flags[2] | flags[3]);
 }

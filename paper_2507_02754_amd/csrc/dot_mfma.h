@@ -1,0 +1,143 @@
+// What the bf16 dot-product attention kernels share: tiles of 32 rows in LDS and their
+// fragments, scores, and the order of the workgroups.
+#pragma once
+
+#include "dot_common.h"
+
+#include "simplicial_layers.h"
+
+#include <algorithm>
+
+namespace sa {
+namespace {
+
+constexpr int kWaves = 4;
+constexpr int kThreads = 64 * kWaves;
+constexpr int kFar = 0x7fffffff;
+
+template <int X>
+using IC = std::integral_constant<int, X>;
+
+template <int N>
+__device__ __forceinline__ void wait_vmcnt() {
+  static_assert(N >= 0 && N < 64, "vmcnt range");
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0F70);
+}
+
+// `n` positions from `p` on, `sn` elements apart, rows of `more` elements.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const uint16_t* p, int n, int64_t sn, int64_t more) {
+  const int64_t bytes = n > 0 ? ((n - 1) * sn + more) * 2 : 0;
+  return make_rsrc(p, static_cast<unsigned>(bytes < kFar ? bytes : kFar));
+}
+
+// What scores need beside the products, in base 2: a = mul s without cap and bias.
+template <bool CAP, bool BIAS>
+struct Scores {
+  float scale2, to_cap, cap2, slope2;
+  __device__ __forceinline__ Scores(const DotArgs& a, int head)
+      : scale2(a.scale * kLog2e), to_cap(CAP ? 2.f * kLog2e * a.scale / a.cap : 0.f), cap2(a.cap * kLog2e),
+        slope2(BIAS ? a.slopes[head] * kLog2e : 0.f) {}
+  // dj: position less key j
+  __device__ __forceinline__ float operator()(float s, float dj) const {
+    float x;
+    if constexpr (CAP)
+      x = cap2 - 2.f * cap2 * __builtin_amdgcn_rcpf(fast_exp2(s * to_cap) + 1.f);  // cap tanh
+    else
+      x = s * scale2;
+    if constexpr (BIAS) x = __builtin_fmaf(-slope2, fabsf(dj), x);
+    return x;
+  }
+};
+
+// The 32 rows of a wavefront, one a lane.
+struct Lanes {
+  int i, head, p;
+  bool valid;
+  __device__ __forceinline__ Lanes(const DotArgs& a, const DotMask& m, int hk, int r) {
+    valid = r < a.G * a.Nq;
+    const int rr = valid ? r : 0;
+    i = div_group(rr, a);
+    head = hk * a.G + rr - i * a.G;
+    p = valid ? m.first + i : -1;
+  }
+};
+__device__ __forceinline__ DotSpan rows_span(const DotArgs& a, const DotMask& m, int r0, int n) {
+  return DotSpan(m, m.first + r0 / a.G, m.first + (min(r0 + n, a.G * a.Nq) - 1) / a.G);
+}
+
+// A row (of D columns from p on; none: zeros) as a product's operand.
+template <int DP>
+__device__ __forceinline__ void load_row(u32x4_t (&f)[DP / 16], const uint16_t* p, bool valid, int D, int h) {
+#pragma unroll
+  for (int t = 0; t < DP / 16; ++t) f[t] = valid && 16 * t + 8 * h < D ? ldg128(p + 16 * t + 8 * h) : u32x4_t{0, 0, 0, 0};
+}
+__device__ __forceinline__ const uint16_t* q_row(const DotArgs& a, const Lanes& w, int b) {
+  return static_cast<const uint16_t*>(a.q) + b * a.qsb + w.i * a.qsn + w.head * a.qsh;
+}
+
+// Writes an accumulator's row c times `mul`: 4 consecutive columns of each quad, from
+// p on (already + 4 h).
+template <int DP>
+__device__ __forceinline__ void store_row(uint16_t* p, const f32x16_t (&acc)[DP / 32], float mul, int D) {
+#pragma unroll
+  for (int dt = 0; dt < DP / 32; ++dt)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (32 * dt + 8 * q < D)
+        *reinterpret_cast<u32x2_t*>(p + 32 * dt + 8 * q) =
+            u32x2_t{pack_bf16x2(acc[dt][4 * q] * mul, acc[dt][4 * q + 1] * mul), pack_bf16x2(acc[dt][4 * q + 2] * mul, acc[dt][4 * q + 3] * mul)};
+}
+// NaN if any of a lane's accumulators is an infinity or NaN, else 0.
+template <int NDT>
+__device__ __forceinline__ float not_finite(const f32x16_t (&acc)[NDT]) {
+  float x = 0.f;
+#pragma unroll
+  for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) x += acc[dt][v] * 0.f;
+  return x;
+}
+// The rows (bits 0 .. 31) for which either half's lane says so.
+__device__ __forceinline__ unsigned rows_where(bool x) {
+  const unsigned long long b = __builtin_amdgcn_ballot_w64(x);
+  return static_cast<unsigned>(b) | static_cast<unsigned>(b >> 32);
+}
+
+__device__ __forceinline__ bool has_mask(const DotArgs& a) { return a.causal || a.window || a.prefix || a.docs || a.lens; }
+
+// Workgroup order: every XCD takes a contiguous run of (sequence, K-side head), whose
+// keys its L2 holds; the row blocks that see most keys come first.
+__device__ __forceinline__ bool unit_of(int64_t total, int64_t& unit) {
+  const int64_t per = (total + 7) / 8;
+  unit = static_cast<int64_t>(blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  return unit < total;
+}
+unsigned unit_grid(int64_t total) { return static_cast<unsigned>((total + 7) / 8 * 8); }
+
+// Per-lane LDS offsets of a tile's fragments.
+template <int DP>
+struct Frags {
+  using T = SwzTile<DP>;
+  int ko[DP / 16], vo[DP / 32][2];
+  __device__ __forceinline__ Frags(int lane, int base) {
+    const int c = lane & 31, h = lane >> 5, grp = lane >> 4, sl = lane & 15;
+#pragma unroll
+    for (int t = 0; t < DP / 16; ++t) ko[t] = base + T::off(c, 2 * t + h);
+    const int r0 = 4 * (grp >> 1) + (sl >> 2);
+#pragma unroll
+    for (int dt = 0; dt < DP / 32; ++dt) {
+      const int col = 32 * dt + 16 * (grp & 1) + 4 * (sl & 3), ch = col >> 3, within = (col & 7) * 2;
+      vo[dt][0] = base + T::off(r0, ch) + within;
+      vo[dt][1] = base + T::off(r0 + 8, ch) + within;
+    }
+  }
+  __device__ __forceinline__ u32x4_t row(const lds_char* tile, int t) const { return lds_ld<u32x4_t>(tile + ko[t]); }
+  __device__ __forceinline__ u32x4_t tr(const lds_char* tile, int dt, int u) const {
+    const lds_char* p = tile + 2 * DP * 16 * u;
+    const u32x2_t x = lds_tr16(p + vo[dt][0]), y = lds_tr16(p + vo[dt][1]);
+    return u32x4_t{x[0], x[1], y[0], y[1]};
+  }
+};
+
+}  // namespace
+}  // namespace sa

@@ -272,7 +272,8 @@ int simplicial_dot_attn_bwd(const void* q, const void* k, const void* v, const v
     if (r != SA_OK) return r;
     a.ranges = ranges;
   }
-  return to_status(sa::dot_bwd_f32(a, st));
+  a.nsplit = p.nsplit;
+  return to_status(dtype == SA_DTYPE_BF16 ? sa::dot_bwd_bf16(a, st) : sa::dot_bwd_f32(a, st));
 }
 
 // A launch holds less than 2^32 threads: at least 64 a row, 1024 logits for every 64 of a long one.

@@ -72,8 +72,8 @@ struct DotArgs {
   const int* lens;
   // Smallest and largest document number of every 32 positions, [B, ceil(Nk / 32)].
   const int2* ranges;
-  float* delta;  // backward: Delta [B, H, Nq]
-  int nsplit;    // forward: parts of the key axis (bf16, 0: workgroups of 128 rows)
+  float* delta;  // backward: Delta [B, H, Nq] (bf16: what dot_bwd.hip keeps of the rows)
+  int nsplit;    // forward: parts of the key axis (bf16, 0: workgroups of 128 rows or keys)
   float* part;   // forward, nsplit > 1: their partial results
   int dtype;
 };
@@ -89,5 +89,6 @@ hipError_t dot_ranges(const DotArgs& a, int2* ranges, hipStream_t st);
 hipError_t dot_fwd_f32(const DotArgs& a, hipStream_t st);
 hipError_t dot_bwd_f32(const DotArgs& a, hipStream_t st);
 hipError_t dot_fwd_bf16(const DotArgs& a, hipStream_t st);
+hipError_t dot_bwd_bf16(const DotArgs& a, hipStream_t st);
 
 }  // namespace sa

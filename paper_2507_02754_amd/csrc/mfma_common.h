@@ -21,6 +21,7 @@ typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef unsigned u32x4_t __attribute__((ext_vector_type(4)));
 typedef unsigned u32x2_t __attribute__((ext_vector_type(2)));
 
@@ -195,6 +196,12 @@ __device__ __forceinline__ void lds_st(lds_char* p, V v) {
 __device__ __forceinline__ void load_lds16(__amdgpu_buffer_rsrc_t r, lds_char* dst, int voff, int soff = 0) {
 #if defined(__HIP_DEVICE_COMPILE__)
   __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(dst), 16, voff, soff, 0, 0);
+#endif
+}
+// The same of 4 bytes per lane, to dst + 4 l.
+__device__ __forceinline__ void load_lds4(__amdgpu_buffer_rsrc_t r, lds_char* dst, int voff) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(dst), 4, voff, 0, 0, 0);
 #endif
 }
 __device__ __forceinline__ u32x2_t lds_tr16(const lds_char* p) {

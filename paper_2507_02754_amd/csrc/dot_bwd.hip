@@ -181,7 +181,7 @@ __global__ __launch_bounds__(kThreads, PRIV ? 1 : 2) void dot_dq_kernel(DotArgs 
   SA_DOT_RING(PRIV ? kWaves : 1);
   const int R = a.G * a.Nq, nrb = (R + kRows - 1) / kRows;
   int64_t unit;
-  if (!unit_of(static_cast<int64_t>(a.B) * a.Hkv * nrb, unit)) return;
+  if (!unit_of(static_cast<int64_t>(a.B) * a.Hkv, nrb, unit)) return;
   const int block = nrb - 1 - static_cast<int>(unit % nrb), bh = static_cast<int>(unit / nrb);
   const int b = bh / a.Hkv, hk = bh - b * a.Hkv;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 31, h = lane >> 5;
@@ -360,7 +360,7 @@ __global__ __launch_bounds__(kThreads, PRIV ? 1 : 2) void dot_dkv_kernel(DotArgs
   };
   const int R = a.G * a.Nq, nkb = (a.Nk + kKeys - 1) / kKeys;
   int64_t unit;
-  if (!unit_of(static_cast<int64_t>(a.B) * a.Hkv * nkb, unit)) return;
+  if (!unit_of(static_cast<int64_t>(a.B) * a.Hkv, nkb, unit)) return;
   const int block = static_cast<int>(unit % nkb), bh = static_cast<int>(unit / nkb);
   const int b = bh / a.Hkv, hk = bh - b * a.Hkv;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 31, h = lane >> 5;
@@ -539,8 +539,8 @@ template <int DP, bool CAP, bool BIAS, bool PRIV>
 void launch(const DotArgs& a, hipStream_t st) {
   const int64_t R = static_cast<int64_t>(a.G) * a.Nq, heads = static_cast<int64_t>(a.B) * a.Hkv;
   constexpr int n = PRIV ? 32 : 128;
-  dot_dq_kernel<DP, CAP, BIAS, PRIV><<<unit_grid(heads * ((R + n - 1) / n)), kThreads, 0, st>>>(a);
-  dot_dkv_kernel<DP, CAP, BIAS, PRIV><<<unit_grid(heads * ((a.Nk + n - 1) / n)), kThreads, 0, st>>>(a);
+  dot_dq_kernel<DP, CAP, BIAS, PRIV><<<unit_grid(heads, ((R + n - 1) / n)), kThreads, 0, st>>>(a);
+  dot_dkv_kernel<DP, CAP, BIAS, PRIV><<<unit_grid(heads, ((a.Nk + n - 1) / n)), kThreads, 0, st>>>(a);
 }
 template <int DP, bool CAP, bool BIAS>
 void launch(const DotArgs& a, hipStream_t st) {

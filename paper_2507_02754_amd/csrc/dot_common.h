@@ -147,6 +147,23 @@ __device__ __forceinline__ BlockSeq<Test> block_seq(int lo, int hi, int off, int
   return BlockSeq<Test>(lo, hi, off, step, t);
 }
 
+// Workgroup order. Workgroups go to the 8 XCDs in turn. `heads` (sequence, K-side head) pairs of
+// `per` units each: gcd(heads, 8) groups of XCDs take an equal share of the heads, so that
+// a head's keys stay in few L2s, and the XCDs of a group take its units in turn, so that
+// long and short ones (the first and last rows of a causal sequence) spread evenly: a
+// contiguous run for each XCD instead left half of them with the short rows.
+__device__ __forceinline__ bool unit_of(int64_t heads, int64_t per, int64_t& unit) {
+  const int groups = heads % 8 == 0 ? 8 : heads % 4 == 0 ? 4 : heads % 2 == 0 ? 2 : 1, share = 8 / groups;
+  const int x = blockIdx.x & 7, group = x / share;
+  const int64_t all = heads / groups * per, k = static_cast<int64_t>(blockIdx.x >> 3) * share + x % share;
+  unit = group * all + k;
+  return k < all;
+}
+inline unsigned unit_grid(int64_t heads, int64_t per) {
+  const int64_t groups = heads % 8 == 0 ? 8 : heads % 4 == 0 ? 4 : heads % 2 == 0 ? 2 : 1, share = 8 / groups;
+  return static_cast<unsigned>((heads / groups * per + share - 1) / share * 8);
+}
+
 // r / G for 0 <= r < 2^31, as a product with magic = floor(2^(31 + l) / G) + 1, l =
 // ceil(log2 G), and a shift (G = 1: r).
 __device__ __forceinline__ int div_group(int r, const DotArgs& a) {

@@ -213,15 +213,6 @@ struct Rows {
   }
 };
 
-// Workgroup order: every XCD takes a contiguous run of (sequence, K-side head), whose
-// keys its L2 holds; the row blocks that see most keys come first.
-__device__ __forceinline__ bool unit_of(int64_t total, int64_t& unit) {
-  const int64_t per = (total + 7) / 8;
-  unit = static_cast<int64_t>(blockIdx.x & 7) * per + (blockIdx.x >> 3);
-  return unit < total;
-}
-unsigned unit_grid(int64_t total) { return static_cast<unsigned>((total + 7) / 8 * 8); }
-
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads, 1) void dot_fwd_f32_kernel(DotArgs a) {
   constexpr int NDT = Geo<D>::NDT, S = sizeof(T);
@@ -229,7 +220,7 @@ __global__ __launch_bounds__(kThreads, 1) void dot_fwd_f32_kernel(DotArgs a) {
   __shared__ float stat[2][kWaves][32];
   const int nrb = (a.G * a.Nq + kDotBlock - 1) / kDotBlock;
   int64_t unit;
-  if (!unit_of(static_cast<int64_t>(a.B) * a.Hkv * nrb * a.nsplit, unit)) return;
+  if (!unit_of(static_cast<int64_t>(a.B) * a.Hkv, static_cast<int64_t>(nrb) * a.nsplit, unit)) return;
   const int part = static_cast<int>(unit % a.nsplit);
   unit /= a.nsplit;
   const int block = nrb - 1 - static_cast<int>(unit % nrb), bh = static_cast<int>(unit / nrb);
@@ -378,7 +369,7 @@ __global__ __launch_bounds__(kThreads, 1) void dot_dq_f32_kernel(DotArgs a) {
   __shared__ float lds[kWaves * NDT * 1024 > kWaves * kScratch ? kWaves * NDT * 1024 : kWaves * kScratch];
   const int nrb = (a.G * a.Nq + kDotBlock - 1) / kDotBlock;
   int64_t unit;
-  if (!unit_of(static_cast<int64_t>(a.B) * a.Hkv * nrb, unit)) return;
+  if (!unit_of(static_cast<int64_t>(a.B) * a.Hkv, nrb, unit)) return;
   const int block = nrb - 1 - static_cast<int>(unit % nrb), bh = static_cast<int>(unit / nrb);
   const int b = bh / a.Hkv, hk = bh - b * a.Hkv;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 31, h = lane >> 5;
@@ -475,7 +466,7 @@ __global__ __launch_bounds__(kThreads, 1) void dot_dkv_f32_kernel(DotArgs a) {
   __shared__ RowInfo infos[kWaves];
   const int nkb = (a.Nk + kDotBlock - 1) / kDotBlock;
   int64_t unit;
-  if (!unit_of(static_cast<int64_t>(a.B) * a.Hkv * nkb, unit)) return;
+  if (!unit_of(static_cast<int64_t>(a.B) * a.Hkv, nkb, unit)) return;
   const int block = static_cast<int>(unit % nkb), bh = static_cast<int>(unit / nkb);
   const int b = bh / a.Hkv, hk = bh - b * a.Hkv;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 31, h = lane >> 5;
@@ -580,7 +571,7 @@ __global__ void dot_ranges_kernel(const int* docs, int2* ranges, int B, int Nk) 
 template <typename T, int D>
 hipError_t launch_fwd(const DotArgs& a, hipStream_t st) {
   const int64_t nrb = (static_cast<int64_t>(a.G) * a.Nq + kDotBlock - 1) / kDotBlock;
-  dot_fwd_f32_kernel<T, D><<<unit_grid(a.B * nrb * a.Hkv * a.nsplit), kThreads, 0, st>>>(a);
+  dot_fwd_f32_kernel<T, D><<<unit_grid(static_cast<int64_t>(a.B) * a.Hkv, nrb * a.nsplit), kThreads, 0, st>>>(a);
   if (a.nsplit > 1) {
     const int64_t rows = static_cast<int64_t>(a.B) * a.H * a.Nq;
     dot_join_kernel<T><<<static_cast<unsigned>((rows + 256 / D - 1) / (256 / D)), 256, 0, st>>>(a);
@@ -591,8 +582,8 @@ template <typename T, int D>
 hipError_t launch_bwd(const DotArgs& a, hipStream_t st) {
   const int64_t nrb = (static_cast<int64_t>(a.G) * a.Nq + kDotBlock - 1) / kDotBlock;
   const int64_t nkb = (a.Nk + kDotBlock - 1) / kDotBlock;
-  dot_dq_f32_kernel<T, D><<<unit_grid(a.B * nrb * a.Hkv), kThreads, 0, st>>>(a);
-  dot_dkv_f32_kernel<T, D><<<unit_grid(a.B * nkb * a.Hkv), kThreads, 0, st>>>(a);
+  dot_dq_f32_kernel<T, D><<<unit_grid(static_cast<int64_t>(a.B) * a.Hkv, nrb), kThreads, 0, st>>>(a);
+  dot_dkv_f32_kernel<T, D><<<unit_grid(static_cast<int64_t>(a.B) * a.Hkv, nkb), kThreads, 0, st>>>(a);
   return hipGetLastError();
 }
 template <typename T>

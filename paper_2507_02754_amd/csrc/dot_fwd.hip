@@ -155,7 +155,7 @@ __global__ __launch_bounds__(kThreads, 2) void dot_fwd_kernel(DotArgs a) {
   };
   const int R = a.G * a.Nq, nrb = (R + kRows - 1) / kRows;
   int64_t unit;
-  if (!unit_of(static_cast<int64_t>(a.B) * a.Hkv * nrb, unit)) return;
+  if (!unit_of(static_cast<int64_t>(a.B) * a.Hkv, nrb, unit)) return;
   const int block = nrb - 1 - static_cast<int>(unit % nrb), bh = static_cast<int>(unit / nrb);
   const int b = bh / a.Hkv, hk = bh - b * a.Hkv;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 31, h = lane >> 5;
@@ -300,7 +300,7 @@ __global__ __launch_bounds__(kThreads, 1) void dot_few_kernel(DotArgs a) {
   auto vst = [&](auto SC) __attribute__((always_inline)) { return to_lds(decltype(SC)::value == 0 ? vst0 : vst1); };
   const int R = a.G * a.Nq, nrb = (R + 31) / 32;
   int64_t unit;
-  if (!unit_of(static_cast<int64_t>(a.B) * a.Hkv * nrb * a.nsplit, unit)) return;
+  if (!unit_of(static_cast<int64_t>(a.B) * a.Hkv, static_cast<int64_t>(nrb) * a.nsplit, unit)) return;
   const int part = static_cast<int>(unit % a.nsplit);
   unit /= a.nsplit;
   const int block = nrb - 1 - static_cast<int>(unit % nrb), bh = static_cast<int>(unit / nrb);
@@ -493,10 +493,10 @@ template <int DP, bool CAP, bool BIAS>
 hipError_t launch(const DotArgs& a, hipStream_t st) {
   const int64_t R = static_cast<int64_t>(a.G) * a.Nq, heads = static_cast<int64_t>(a.B) * a.Hkv;
   if (a.nsplit == 0) {
-    dot_fwd_kernel<DP, CAP, BIAS><<<unit_grid(heads * ((R + 127) / 128)), kThreads, 0, st>>>(a);
+    dot_fwd_kernel<DP, CAP, BIAS><<<unit_grid(heads, ((R + 127) / 128)), kThreads, 0, st>>>(a);
     return hipGetLastError();
   }
-  dot_few_kernel<DP, CAP, BIAS><<<unit_grid(heads * ((R + 31) / 32) * a.nsplit), kThreads, 0, st>>>(a);
+  dot_few_kernel<DP, CAP, BIAS><<<unit_grid(heads, ((R + 31) / 32) * a.nsplit), kThreads, 0, st>>>(a);
   if (a.nsplit > 1) dot_join_kernel<<<static_cast<unsigned>((heads * R + kWaves - 1) / kWaves), kThreads, 0, st>>>(a);
   return hipGetLastError();
 }

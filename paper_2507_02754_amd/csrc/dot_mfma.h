@@ -105,15 +105,6 @@ __device__ __forceinline__ unsigned rows_where(bool x) {
 
 __device__ __forceinline__ bool has_mask(const DotArgs& a) { return a.causal || a.window || a.prefix || a.docs || a.lens; }
 
-// Workgroup order: every XCD takes a contiguous run of (sequence, K-side head), whose
-// keys its L2 holds; the row blocks that see most keys come first.
-__device__ __forceinline__ bool unit_of(int64_t total, int64_t& unit) {
-  const int64_t per = (total + 7) / 8;
-  unit = static_cast<int64_t>(blockIdx.x & 7) * per + (blockIdx.x >> 3);
-  return unit < total;
-}
-unsigned unit_grid(int64_t total) { return static_cast<unsigned>((total + 7) / 8 * 8); }
-
 // Per-lane LDS offsets of a tile's fragments.
 template <int DP>
 struct Frags {

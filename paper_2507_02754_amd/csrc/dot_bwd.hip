@@ -189,7 +189,8 @@ __global__ __launch_bounds__(kThreads, PRIV ? 1 : 2) void dot_dq_kernel(DotArgs 
   const int r0 = block * kRows + (PRIV ? 0 : 32 * wave);
   const Lanes w(a, m, hk, r0 + c);
   const DotSpan all = rows_span(a, m, block * kRows, kRows), own = rows_span(a, m, min(r0, R - 1), 32);
-  const int dq = m.doc(w.p), pos = w.p - 4 * h;
+  const KeysSeen seen(m, w.p);
+  const int pos = w.p - 4 * h;
   const Scores<CAP, BIAS> score(a, w.head);
   int lo, hi;
   key_blocks(m, all, lo, hi);
@@ -286,13 +287,8 @@ __global__ __launch_bounds__(kThreads, PRIV ? 1 : 2) void dot_dq_kernel(DotArgs 
         s[v] = fast_exp2(x) * (dp[v] - delta);
         if constexpr (CAP) s[v] *= dcap;
       }
-      if (!at.full) {
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const int j = j0 + acc_row(v, h);
-          if (!m.sees(w.p, j, dq, m.doc(j))) s[v] = 0.f;
-        }
-      }
+      if (!at.full)
+        each_pair(m, seen, c, h, [&](int x) { return j0 + x; }, [&](int v, bool see) { s[v] = see ? s[v] : 0.f; });
       const float* sv = reinterpret_cast<const float*>(&s);
       u32x4_t pf[2];
 #pragma unroll
@@ -367,7 +363,7 @@ __global__ __launch_bounds__(kThreads, PRIV ? 1 : 2) void dot_dkv_kernel(DotArgs
   const DotMask m(a, b);
   const int j0 = block * kKeys + (PRIV ? 0 : 32 * wave), j = j0 + c;
   const DotSpan all(m, block * kKeys, block * kKeys + kKeys - 1), own(m, j0, j0 + 31);
-  const int dk = m.doc(j);
+  const QueriesSeeing seen(m, j);
   const Scores<CAP, false> score(a, 0);
   int lo, hi;
   row_blocks(m, all, a.G, R, lo, hi);
@@ -465,13 +461,10 @@ __global__ __launch_bounds__(kThreads, PRIV ? 1 : 2) void dot_dkv_kernel(DotArgs
           if constexpr (CAP) dp[4 * q + e] *= dcap;
         }
       }
-      if (!at.full) {
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const int r = at.blk * 32 + acc_row(v, h), p = r < R ? m.first + div_group(r, a) : -1;
-          if (!m.sees(p, j, m.doc(p), dk)) s[v] = 0.f, dp[v] = 0.f;
-        }
-      }
+      // (rows past the last one have probabilities of 0 as they are)
+      if (!at.full)
+        each_pair(m, seen, c, h, [&](int x) { return m.first + div_group(at.blk * 32 + x, a); },
+                  [&](int v, bool see) { s[v] = see ? s[v] : 0.f, dp[v] = see ? dp[v] : 0.f; });
       u32x4_t pf[2], df[2];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {

@@ -87,6 +87,51 @@ __device__ __forceinline__ void row_blocks(const DotMask& m, const DotSpan& k, i
   hi = k.p0 >= m.L || to <= from ? lo : static_cast<int>((static_cast<int64_t>(to) * G + kDotBlock - 1) / kDotBlock);
 }
 
+// The keys j that a query at p sees, as ranges: a0 <= j < a0 + n or j < pre, and of its
+// document; a query that sees nothing has n = pre = 0.
+struct KeysSeen {
+  int a0, pre, doc;
+  unsigned n;
+  __device__ __forceinline__ KeysSeen(const DotMask& m, int p) : a0(0), pre(0), doc(m.doc(p)), n(0) {
+    if (p < 0 || doc < 0) return;
+    a0 = m.window ? max(p - m.window + 1, 0) : 0;
+    const int end = m.causal ? p + 1 : m.window ? static_cast<int>(min(static_cast<int64_t>(p) + m.window, static_cast<int64_t>(m.L))) : m.L;
+    n = static_cast<unsigned>(max(min(end, m.L) - a0, 0));
+    pre = m.prefix;
+  }
+  __device__ __forceinline__ bool operator()(int j) const { return (static_cast<unsigned>(j - a0) < n) | (j < pre); }
+};
+// The positions p of the queries that see key j, likewise: b0 <= p < b0 + n.
+struct QueriesSeeing {
+  int b0, doc;
+  unsigned n;
+  __device__ __forceinline__ QueriesSeeing(const DotMask& m, int j) : b0(0), doc(m.doc(j)), n(0) {
+    if (j >= m.L || doc < 0) return;
+    n = 0x7fffffff;
+    if (j < m.prefix) return;
+    b0 = m.causal ? j : m.window ? max(j - m.window + 1, 0) : 0;
+    if (m.window) n = static_cast<unsigned>(j - b0 + m.window);
+  }
+  __device__ __forceinline__ bool operator()(int p) const { return static_cast<unsigned>(p - b0) < n; }
+};
+// Calls f(v, visible) for the accumulator registers of a block whose 32 rows (keys or
+// queries) are at position at(x), x = 0 .. 31, against the lane's own query or key `seen`.
+// Document numbers are loaded once, a lane each, and read across lanes.
+template <typename Seen, typename At, typename F>
+__device__ __forceinline__ void each_pair(const DotMask& m, const Seen& seen, int c, int h, At at, F f) {
+  if (m.docs) {
+    const int mine = m.doc(at(c));
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      const int lo = __builtin_amdgcn_readlane(mine, acc_row(v, 0)), hi = __builtin_amdgcn_readlane(mine, acc_row(v, 1));
+      f(v, seen(at(acc_row(v, h))) & ((h ? hi : lo) == seen.doc));
+    }
+  } else {
+#pragma unroll
+    for (int v = 0; v < 16; ++v) f(v, seen(at(acc_row(v, h))));
+  }
+}
+
 // Walks the blocks lo + off, lo + off + step, .. < hi that are live: 64 at a time are
 // looked at, one a lane. test(block, live, full) and body(block, full), all wavefront-uniform
 // but for test's block.

@@ -228,7 +228,7 @@ __global__ __launch_bounds__(kThreads, 1) void dot_fwd_f32_kernel(DotArgs a) {
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 31, h = lane >> 5;
   const DotMask m(a, b);
   const Rows row(a, m, hk, block, c);
-  const int dq = m.doc(row.p);
+  const KeysSeen sees(m, row.p);
   const float slope = a.slopes ? a.slopes[row.valid ? row.head : 0] : 0.f;
   const Score score(a);
   RowOp<T, D> q;
@@ -261,14 +261,14 @@ __global__ __launch_bounds__(kThreads, 1) void dot_fwd_f32_kernel(DotArgs a) {
           const int j = j0 + acc_row(v, h);
           float unused;
           x[v] = score(s[v], slope, abs(row.p - j), unused);
-          if (!full) {
-            if (m.sees(row.p, j, dq, m.doc(j)))
-              seen |= 1u << v;
-            else
-              x[v] = -kInf;
-          }
-          top = fmaxf(top, x[v]);
         }
+        if (!full)
+          each_pair(m, sees, c, h, [&](int y) { return j0 + y; }, [&](int v, bool see) {
+            seen |= static_cast<unsigned>(see) << v;
+            x[v] = see ? x[v] : -kInf;
+          });
+#pragma unroll
+        for (int v = 0; v < 16; ++v) top = fmaxf(top, x[v]);
         top = fmaxf(mx, fmaxf(top, swap_halves(top)));
         const float base = top == -kInf ? 0.f : top, down = fast_exp2((mx - base) * kLog2e);
         mx = top;
@@ -375,7 +375,7 @@ __global__ __launch_bounds__(kThreads, 1) void dot_dq_f32_kernel(DotArgs a) {
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 31, h = lane >> 5;
   const DotMask m(a, b);
   const Rows row(a, m, hk, block, c);
-  const int dq = m.doc(row.p);
+  const KeysSeen sees(m, row.p);
   const float slope = a.slopes ? a.slopes[row.valid ? row.head : 0] : 0.f;
   const Score score(a);
   RowOp<T, D> q, g;
@@ -426,13 +426,12 @@ __global__ __launch_bounds__(kThreads, 1) void dot_dq_f32_kernel(DotArgs a) {
           float dcap;
           const float p = prob(score(s[v], slope, abs(row.p - j), dcap), lse);
           x[v] = p * (dp[v] - delta) * dcap * a.scale;
-          if (!full) {
-            if (m.sees(row.p, j, dq, m.doc(j)))
-              seen |= 1u << v;
-            else
-              x[v] = 0.f;
-          }
         }
+        if (!full)
+          each_pair(m, sees, c, h, [&](int y) { return j0 + y; }, [&](int v, bool see) {
+            seen |= static_cast<unsigned>(see) << v;
+            x[v] = see ? x[v] : 0.f;
+          });
         weighted_rows<T, D>(acc, x, rk, [&](int y) { return static_cast<int>(y * a.ksn * S); }, c, h, !full, seen,
                             lds + wave * kScratch);
       });
@@ -455,7 +454,7 @@ __global__ __launch_bounds__(kThreads, 1) void dot_dq_f32_kernel(DotArgs a) {
 
 // What a row block's 32 rows are, one wavefront's copy in LDS.
 struct RowInfo {
-  int p[32], doc[32], qoff[32], goff[32];
+  int p[32], qoff[32], goff[32];
   float lse[32], delta[32], slope[32];
 };
 
@@ -475,7 +474,7 @@ __global__ __launch_bounds__(kThreads, 1) void dot_dkv_f32_kernel(DotArgs a) {
   RowInfo& info = infos[wave];
   const int j0 = block * kDotBlock, j = j0 + c, R = a.G * a.Nq;
   const DotSpan span(m, j0, j0 + kDotBlock - 1);
-  const int dk = m.doc(j);
+  const QueriesSeeing sees(m, j);
   RowOp<T, D> k, v;
   k.load(rows_of(static_cast<const T*>(a.k) + b * a.ksb + hk * a.ksh + j0 * a.ksn, m.L - j0, a.ksn, D), static_cast<int>(c * a.ksn * S), h);
   v.load(rows_of(static_cast<const T*>(a.v) + b * a.vsb + hk * a.vsh + j0 * a.vsn, m.L - j0, a.vsn, D), static_cast<int>(c * a.vsn * S), h);
@@ -501,7 +500,6 @@ __global__ __launch_bounds__(kThreads, 1) void dot_dkv_f32_kernel(DotArgs a) {
         const int goff = valid ? static_cast<int>(((i - i0) * orow + head * D) * S) : kFar;
         if (h == 0) {
           info.p[c] = p;
-          info.doc[c] = m.doc(p);
           info.qoff[c] = qoff;
           info.goff[c] = goff;
           info.lse[c] = valid ? a.lse[srow] : -kInf;
@@ -525,13 +523,13 @@ __global__ __launch_bounds__(kThreads, 1) void dot_dkv_f32_kernel(DotArgs a) {
           float dcap;
           w[e] = prob(score(s[e], info.slope[y], abs(info.p[y] - j), dcap), info.lse[y]);
           x[e] = w[e] * (dp[e] - info.delta[y]) * dcap * a.scale;
-          if (!full) {
-            if (m.sees(info.p[y], j, info.doc[y], dk))
-              seen |= 1u << e;
-            else
-              w[e] = 0.f, x[e] = 0.f;
-          }
         }
+        if (!full)
+          each_pair(m, sees, c, h, [&](int y) { return info.p[y]; }, [&](int e, bool see) {
+            seen |= static_cast<unsigned>(see) << e;
+            w[e] = see ? w[e] : 0.f;
+            x[e] = see ? x[e] : 0.f;
+          });
         // (rows past the last query load as zeros, with probabilities of 0)
         weighted_rows<T, D>(accv, w, rg, [&](int y) { return info.goff[y]; }, c, h, !full, seen, lds + wave * kScratch);
         weighted_rows<T, D>(acck, x, rq, [&](int y) { return info.qoff[y]; }, c, h, !full, seen, lds + wave * kScratch);

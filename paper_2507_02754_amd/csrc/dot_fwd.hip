@@ -48,9 +48,10 @@ struct Row {
     for (int dt = 0; dt < NDT; ++dt) acc[dt] = f32x16_t{};
     m = -1e30f, l = 0.f, lr = 0.f;
   }
-  // Probabilities of the block at key j0, packed; `masked`: seen(v) says whether the pair is visible.
-  template <typename Seen>
-  __device__ __forceinline__ void step(f32x16_t& s, const Scores<CAP, BIAS>& score, float dj, bool masked, Seen seen,
+  // Probabilities of a block, packed; `masked`: hide(s) sets the scores of pairs that are not
+  // visible to -inf.
+  template <typename Hide>
+  __device__ __forceinline__ void step(f32x16_t& s, const Scores<CAP, BIAS>& score, float dj, bool masked, Hide hide,
                                        u32x4_t (&pf)[2]) {
     const bf16x2_t ones = {static_cast<__bf16>(1.0f), static_cast<__bf16>(1.0f)};
     float mul = score.scale2;
@@ -58,11 +59,7 @@ struct Row {
       mul = 1.f;
 #pragma unroll
       for (int v = 0; v < 16; ++v) s[v] = score(s[v], dj - static_cast<float>(8 * (v >> 2) + (v & 3)));
-      if (masked) {
-#pragma unroll
-        for (int v = 0; v < 16; ++v)
-          if (!seen(v)) s[v] = -kInf;
-      }
+      if (masked) hide(s);
     }
     float lb, lrb;
     auto form = [&]() __attribute__((always_inline)) {
@@ -163,7 +160,7 @@ __global__ __launch_bounds__(kThreads, 2) void dot_fwd_kernel(DotArgs a) {
   const int r0 = block * kRows + 32 * wave;
   const Lanes w(a, m, hk, r0 + c);
   const DotSpan all = rows_span(a, m, block * kRows, kRows), own = rows_span(a, m, min(r0, R - 1), 32);
-  const int dq = m.doc(w.p);
+  const KeysSeen seen(m, w.p);
   const Scores<CAP, BIAS> score(a, w.head);
   const int pos = w.p - 4 * h;
   int lo, hi;
@@ -255,9 +252,8 @@ __global__ __launch_bounds__(kThreads, 2) void dot_fwd_kernel(DotArgs a) {
       u32x4_t pf[2];
       const int j0 = at.blk * kDotBlock;
       row.step(sc[cur], score, static_cast<float>(pos - j0), !at.full,
-               [&](int v) {
-                 const int j = j0 + acc_row(v, h);
-                 return m.sees(w.p, j, dq, m.doc(j));
+               [&](f32x16_t& s) __attribute__((always_inline)) {
+                 each_pair(m, seen, c, h, [&](int x) { return j0 + x; }, [&](int v, bool see) { s[v] = see ? s[v] : -kInf; });
                },
                pf);
 #pragma unroll
@@ -309,7 +305,7 @@ __global__ __launch_bounds__(kThreads, 1) void dot_few_kernel(DotArgs a) {
   const DotMask m(a, b);
   const Lanes w(a, m, hk, block * 32 + c);
   const DotSpan own = rows_span(a, m, block * 32, 32);
-  const int dq = m.doc(w.p);
+  const KeysSeen seen(m, w.p);
   const Scores<CAP, BIAS> score(a, w.head);
   const int pos = w.p - 4 * h;
   int lo, hi;
@@ -370,9 +366,8 @@ __global__ __launch_bounds__(kThreads, 1) void dot_few_kernel(DotArgs a) {
     u32x4_t pf[2];
     const int j0 = at.blk * kDotBlock;
     row.step(s, score, static_cast<float>(pos - j0), !at.full,
-             [&](int v) {
-               const int j = j0 + acc_row(v, h);
-               return m.sees(w.p, j, dq, m.doc(j));
+             [&](f32x16_t& s) __attribute__((always_inline)) {
+               each_pair(m, seen, c, h, [&](int x) { return j0 + x; }, [&](int v, bool see) { s[v] = see ? s[v] : -kInf; });
              },
              pf);
 #pragma unroll

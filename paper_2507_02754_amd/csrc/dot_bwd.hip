@@ -262,6 +262,7 @@ __global__ __launch_bounds__(kThreads, PRIV ? 1 : 2) void dot_dq_kernel(DotArgs 
     constexpr int S = decltype(SC)::value;
     const DotBlock at = bq[S];
     if (at.blk < 0) return false;
+    const Frags<DP> f = frag.fresh();
     if constexpr (PRIV) {
       wait_vmcnt<2 * SPW>();
       asm volatile("" ::: "memory");
@@ -272,11 +273,11 @@ __global__ __launch_bounds__(kThreads, PRIV ? 1 : 2) void dot_dq_kernel(DotArgs 
       load(IC<(S + 3) % NS>{}, bq[(S + 3) % NS].blk);
     }
     if (at.mine) {
-      f32x16_t s = mfma32(frag.row(xst(SC), 0), qf[0], f32x16_t{}), dp = mfma32(frag.row(yst(SC), 0), gf[0], f32x16_t{});
+      f32x16_t s = mfma32(f.row(xst(SC), 0), qf[0], f32x16_t{}), dp = mfma32(f.row(yst(SC), 0), gf[0], f32x16_t{});
 #pragma unroll
       for (int t = 1; t < NT; ++t) {
-        s = mfma32(frag.row(xst(SC), t), qf[t], s);
-        dp = mfma32(frag.row(yst(SC), t), gf[t], dp);
+        s = mfma32(f.row(xst(SC), t), qf[t], s);
+        dp = mfma32(f.row(yst(SC), t), gf[t], dp);
       }
       const int j0 = at.blk * kDotBlock;
       const float dj = static_cast<float>(pos - j0);
@@ -296,7 +297,7 @@ __global__ __launch_bounds__(kThreads, PRIV ? 1 : 2) void dot_dq_kernel(DotArgs 
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int dt = 0; dt < NDT; ++dt) acc[dt] = mfma32(frag.tr(xst(SC), dt, u), pf[u], acc[dt]);
+        for (int dt = 0; dt < NDT; ++dt) acc[dt] = mfma32(f.tr(xst(SC), dt, u), pf[u], acc[dt]);
     }
     if constexpr (PRIV) {
       __builtin_amdgcn_s_waitcnt(0xC07F);  // the stage is read: its next block may come
@@ -363,7 +364,6 @@ __global__ __launch_bounds__(kThreads, PRIV ? 1 : 2) void dot_dkv_kernel(DotArgs
   const DotMask m(a, b);
   const int j0 = block * kKeys + (PRIV ? 0 : 32 * wave), j = j0 + c;
   const DotSpan all(m, block * kKeys, block * kKeys + kKeys - 1), own(m, j0, j0 + 31);
-  const QueriesSeeing seen(m, j);
   const Scores<CAP, false> score(a, 0);
   int lo, hi;
   row_blocks(m, all, a.G, R, lo, hi);
@@ -374,15 +374,14 @@ __global__ __launch_bounds__(kThreads, PRIV ? 1 : 2) void dot_dkv_kernel(DotArgs
     mine = some && dot_live(m, q, own);
     full = dot_full(m, q, own);
   });
-  // Rows of q and dO: the chunk of row 32 blk + lrow that this lane brings.
-  int lrow[SPW], lcol[SPW];
-#pragma unroll
-  for (int x = 0; x < SPW; ++x) {
-    const int p = 64 * (PRIV ? x : x * kWaves + wave) + lane;
-    lrow[x] = p / T::CH;
-    const int ch = (p % T::CH) ^ T::swz(lrow[x]);
-    lcol[x] = 8 * ch < a.D ? 16 * ch : -1;
-  }
+  // What depends on the lane alone is formed anew in every block: the accumulators and
+  // the keys' operands leave no registers for it, and a reload from scratch memory would
+  // wait for the block loads issued before it.
+  auto lane_anew = [&]() __attribute__((always_inline)) {
+    int x = lane;
+    asm volatile("" : "+v"(x));
+    return x;
+  };
   const uint16_t* qb = static_cast<const uint16_t*>(a.q) + b * a.qsb;
   const uint16_t* gb = static_cast<const uint16_t*>(a.dout) + static_cast<int64_t>(b) * a.Nq * a.H * a.D;
   const Stat* stats = stats_of(a, bh);
@@ -393,21 +392,19 @@ __global__ __launch_bounds__(kThreads, PRIV ? 1 : 2) void dot_dkv_kernel(DotArgs
     const auto rq = rows_of(qb + i0 * a.qsn, n, a.qsn, (a.H - 1) * a.qsh + a.D), rg = rows_of(gb + i0 * gsn, n, gsn, gsn);
     const auto rs = make_rsrc(stats + max(blk, 0), blk < 0 ? 0 : sizeof(Stat));
     const int base = PRIV ? wave * T::bytes : 0;
-    int qo[SPW], go[SPW];
+    const int ln = lane_anew();
+    // Rows of q and dO: the chunk of row 32 blk + p / CH that this lane brings.
 #pragma unroll
     for (int x = 0; x < SPW; ++x) {
-      const int r = max(blk, 0) * 32 + lrow[x], i = div_group(r, a), head = hk * a.G + r - i * a.G;
-      const bool in = r < R && lcol[x] >= 0;
-      qo[x] = in ? (i - i0) * qsn2 + head * qsh2 + lcol[x] : kFar;
-      go[x] = in ? (i - i0) * gsn2 + head * a.D * 2 + lcol[x] : kFar;
+      const int at = PRIV ? x : x * kWaves + wave, p = 64 * at + ln, row = p / T::CH, ch = (p % T::CH) ^ T::swz(row);
+      const int r = max(blk, 0) * 32 + row, i = div_group(r, a), head = hk * a.G + r - i * a.G;
+      const bool in = r < R && 8 * ch < a.D;
+      load_lds16(rq, xst(SC) + base + 1024 * at, in ? (i - i0) * qsn2 + head * qsh2 + 16 * ch : kFar);
+      load_lds16(rg, yst(SC) + base + 1024 * at, in ? (i - i0) * gsn2 + head * a.D * 2 + 16 * ch : kFar);
     }
-#pragma unroll
-    for (int x = 0; x < SPW; ++x) load_lds16(rq, xst(SC) + base + 1024 * (PRIV ? x : x * kWaves + wave), qo[x]);
-#pragma unroll
-    for (int x = 0; x < SPW; ++x) load_lds16(rg, yst(SC) + base + 1024 * (PRIV ? x : x * kWaves + wave), go[x]);
     // (every wavefront brings the same numbers)
-    load_lds4(rs, ist(SC), lane * 4);
-    if constexpr (BIAS) load_lds4(rs, ist(SC) + 256, 256 + lane * 4);
+    load_lds4(rs, ist(SC), ln * 4);
+    if constexpr (BIAS) load_lds4(rs, ist(SC) + 256, 256 + ln * 4);
   };
   const bool key = j < m.L;
   u32x4_t kf[NT], vf[NT];
@@ -428,6 +425,7 @@ __global__ __launch_bounds__(kThreads, PRIV ? 1 : 2) void dot_dkv_kernel(DotArgs
     constexpr int S = decltype(SC)::value;
     const DotBlock at = bq[S];
     if (at.blk < 0) return false;
+    const Frags<DP> f = frag.fresh();
     if constexpr (PRIV) {
       wait_vmcnt<LPB>();
       asm volatile("" ::: "memory");
@@ -438,14 +436,20 @@ __global__ __launch_bounds__(kThreads, PRIV ? 1 : 2) void dot_dkv_kernel(DotArgs
       load(IC<(S + 3) % NS>{}, bq[(S + 3) % NS].blk);
     }
     if (at.mine) {
-      f32x16_t s = mfma32(frag.row(xst(SC), 0), kf[0], f32x16_t{}), dp = mfma32(frag.row(yst(SC), 0), vf[0], f32x16_t{});
+      const int ln = lane_anew(), jn = j0 + (ln & 31);
+      // Bit v: whether the pair of accumulator register v is visible (before the products,
+      // where registers are free; rows past the last one have probabilities of 0 as they are).
+      const unsigned seen = at.full ? 0xffffu : pairs_seen(m, QueriesSeeing(m, jn), ln & 31, ln >> 5, [&](int x) {
+        return m.first + div_group(at.blk * 32 + x, a);
+      });
+      f32x16_t s = mfma32(f.row(xst(SC), 0), kf[0], f32x16_t{}), dp = mfma32(f.row(yst(SC), 0), vf[0], f32x16_t{});
 #pragma unroll
       for (int t = 1; t < NT; ++t) {
-        s = mfma32(frag.row(xst(SC), t), kf[t], s);
-        dp = mfma32(frag.row(yst(SC), t), vf[t], dp);
+        s = mfma32(f.row(xst(SC), t), kf[t], s);
+        dp = mfma32(f.row(yst(SC), t), vf[t], dp);
       }
-      const lds_char* info = ist(SC) + 16 * h;
-      const float dj = static_cast<float>(m.first + div_group(at.blk * 32, a) - j);
+      const lds_char* info = ist(SC) + 16 * (ln >> 5);
+      const float dj = static_cast<float>(m.first + div_group(at.blk * 32, a) - jn);
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const f32x4_t lse2 = lds_ld<f32x4_t>(info + 32 * q), delta = lds_ld<f32x4_t>(info + 128 + 32 * q);
@@ -461,22 +465,29 @@ __global__ __launch_bounds__(kThreads, PRIV ? 1 : 2) void dot_dkv_kernel(DotArgs
           if constexpr (CAP) dp[4 * q + e] *= dcap;
         }
       }
-      // (rows past the last one have probabilities of 0 as they are)
-      if (!at.full)
-        each_pair(m, seen, c, h, [&](int x) { return m.first + div_group(at.blk * 32 + x, a); },
-                  [&](int v, bool see) { s[v] = see ? s[v] : 0.f, dp[v] = see ? dp[v] : 0.f; });
       u32x4_t pf[2], df[2];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         pf[u] = pack_frag(reinterpret_cast<const float*>(&s), u);
         df[u] = pack_frag(reinterpret_cast<const float*>(&dp), u);
       }
+      if (!at.full) {  // masked pairs out of the packed values (fewer registers than before packing)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int v = 8 * u + 2 * e, lo = __builtin_amdgcn_sbfe(seen, v, 1), hi = __builtin_amdgcn_sbfe(seen, v + 1, 1);
+            const unsigned keep = (lo & 0xffffu) | (hi & 0xffff0000u);
+            pf[u][e] &= keep;
+            df[u][e] &= keep;
+          }
+      }
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int dt = 0; dt < NDT; ++dt) {
-          accv[dt] = mfma32(frag.tr(yst(SC), dt, u), pf[u], accv[dt]);
-          acck[dt] = mfma32(frag.tr(xst(SC), dt, u), df[u], acck[dt]);
+          accv[dt] = mfma32(f.tr(yst(SC), dt, u), pf[u], accv[dt]);
+          acck[dt] = mfma32(f.tr(xst(SC), dt, u), df[u], acck[dt]);
         }
     }
     if constexpr (PRIV) {

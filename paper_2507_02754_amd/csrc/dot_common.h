@@ -132,6 +132,23 @@ __device__ __forceinline__ void each_pair(const DotMask& m, const Seen& seen, in
   }
 }
 
+// The same as bits v, in a loop that takes few registers.
+template <typename Seen, typename At>
+__device__ __forceinline__ unsigned pairs_seen(const DotMask& m, const Seen& seen, int c, int h, At at) {
+  const int mine = m.docs ? m.doc(at(c)) : 0;
+  unsigned bits = 0;
+#pragma unroll 1
+  for (int v = 0; v < 16; ++v) {
+    bool see = seen(at(acc_row(v, h)));
+    if (m.docs) {
+      const int lo = __builtin_amdgcn_readlane(mine, acc_row(v, 0)), hi = __builtin_amdgcn_readlane(mine, acc_row(v, 1));
+      see = see & ((h ? hi : lo) == seen.doc);
+    }
+    bits |= static_cast<unsigned>(see) << v;
+  }
+  return bits;
+}
+
 // Walks the blocks lo + off, lo + off + step, .. < hi that are live: 64 at a time are
 // looked at, one a lane. test(block, live, full) and body(block, full), all wavefront-uniform
 // but for test's block.

@@ -236,6 +236,7 @@ __global__ __launch_bounds__(kThreads, 2) void dot_fwd_kernel(DotArgs a) {
     constexpr int S = decltype(SC)::value, cur = S & 1, nxt = cur ^ 1;
     const DotBlock at = bq[S];
     if (at.blk < 0) return false;
+    const Frags<DP> f = frag.fresh();
     wait_vmcnt<3 * SPW>();
     lds_barrier_tracked();
     bq[S] = seq.next();
@@ -246,7 +247,7 @@ __global__ __launch_bounds__(kThreads, 2) void dot_fwd_kernel(DotArgs a) {
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int dt = 0; dt < NDT; ++dt) vf[u][dt] = frag.tr(vst(IC<S>{}), dt, u);
+        for (int dt = 0; dt < NDT; ++dt) vf[u][dt] = f.tr(vst(IC<S>{}), dt, u);
       __builtin_amdgcn_s_setprio(1);
       products(sc[nxt]);
       u32x4_t pf[2];
@@ -265,7 +266,7 @@ __global__ __launch_bounds__(kThreads, 2) void dot_fwd_kernel(DotArgs a) {
       products(sc[nxt]);
     }
 #pragma unroll
-    for (int t = 0; t < NT; ++t) kf[t] = frag.row(kst(IC<(S + 2) % kStages>{}), t);
+    for (int t = 0; t < NT; ++t) kf[t] = f.row(kst(IC<(S + 2) % kStages>{}), t);
     return true;
   };
   while (iteration(IC<0>{}) && iteration(IC<1>{}) && iteration(IC<2>{}) && iteration(IC<3>{})) {
@@ -349,16 +350,17 @@ __global__ __launch_bounds__(kThreads, 1) void dot_few_kernel(DotArgs a) {
     constexpr int S = decltype(SC)::value;
     const DotBlock at = bq[S];
     if (at.blk < 0) return false;
+    const Frags<DP> f = frag.fresh();
     wait_vmcnt<2 * SPW>();
     asm volatile("" ::: "memory");
-    f32x16_t s = mfma32(frag.row(kst(SC), 0), qf[0], f32x16_t{});
+    f32x16_t s = mfma32(f.row(kst(SC), 0), qf[0], f32x16_t{});
 #pragma unroll
-    for (int t = 1; t < NT; ++t) s = mfma32(frag.row(kst(SC), t), qf[t], s);
+    for (int t = 1; t < NT; ++t) s = mfma32(f.row(kst(SC), t), qf[t], s);
     u32x4_t vf[2][NDT];
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int dt = 0; dt < NDT; ++dt) vf[u][dt] = frag.tr(vst(SC), dt, u);
+      for (int dt = 0; dt < NDT; ++dt) vf[u][dt] = f.tr(vst(SC), dt, u);
     __builtin_amdgcn_s_waitcnt(0xC07F);  // the stage is read: its next block may come
     asm volatile("" ::: "memory");
     bq[S] = seq.next();

@@ -105,27 +105,31 @@ __device__ __forceinline__ unsigned rows_where(bool x) {
 
 __device__ __forceinline__ bool has_mask(const DotArgs& a) { return a.causal || a.window || a.prefix || a.docs || a.lens; }
 
-// Per-lane LDS offsets of a tile's fragments.
+// A tile's fragments. Row fragment t of lane (h, c) is chunk 2 t + h of row c, at slot
+// (2 t + h) ^ swz(c): the offset of t = 0 with 32 t exclusive-or'ed in. A transposed
+// fragment's two reads are at rows r and r + 8 (whose swz differ by 2), columns 32 dt
+// on: one offset with 64 dt, and with 32 besides, exclusive-or'ed in. So two registers
+// hold them all; fresh() is called once a block and keeps them from being expanded
+// into sixteen that live through the loop.
 template <int DP>
 struct Frags {
   using T = SwzTile<DP>;
-  int ko[DP / 16], vo[DP / 32][2];
+  int ko, vo;
   __device__ __forceinline__ Frags(int lane, int base) {
     const int c = lane & 31, h = lane >> 5, grp = lane >> 4, sl = lane & 15;
-#pragma unroll
-    for (int t = 0; t < DP / 16; ++t) ko[t] = base + T::off(c, 2 * t + h);
-    const int r0 = 4 * (grp >> 1) + (sl >> 2);
-#pragma unroll
-    for (int dt = 0; dt < DP / 32; ++dt) {
-      const int col = 32 * dt + 16 * (grp & 1) + 4 * (sl & 3), ch = col >> 3, within = (col & 7) * 2;
-      vo[dt][0] = base + T::off(r0, ch) + within;
-      vo[dt][1] = base + T::off(r0 + 8, ch) + within;
-    }
+    ko = base + T::off(c, h);
+    const int col = 16 * (grp & 1) + 4 * (sl & 3);
+    vo = base + T::off(4 * (grp >> 1) + (sl >> 2), col >> 3) + (col & 7) * 2;
   }
-  __device__ __forceinline__ u32x4_t row(const lds_char* tile, int t) const { return lds_ld<u32x4_t>(tile + ko[t]); }
+  __device__ __forceinline__ Frags fresh() const {
+    Frags f = *this;
+    asm volatile("" : "+v"(f.ko), "+v"(f.vo));
+    return f;
+  }
+  __device__ __forceinline__ u32x4_t row(const lds_char* tile, int t) const { return lds_ld<u32x4_t>(tile + (ko ^ (32 * t))); }
   __device__ __forceinline__ u32x4_t tr(const lds_char* tile, int dt, int u) const {
     const lds_char* p = tile + 2 * DP * 16 * u;
-    const u32x2_t x = lds_tr16(p + vo[dt][0]), y = lds_tr16(p + vo[dt][1]);
+    const u32x2_t x = lds_tr16(p + (vo ^ (64 * dt))), y = lds_tr16(p + 16 * DP + (vo ^ (64 * dt) ^ 32));
     return u32x4_t{x[0], x[1], y[0], y[1]};
   }
 };

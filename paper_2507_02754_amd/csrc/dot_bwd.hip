@@ -125,20 +125,36 @@ __device__ __forceinline__ void single_key(const DotArgs& a, const DotMask& m, i
   if (d1) static_cast<uint16_t*>(a.dk)[at + 64] = f32_to_bf16(x1), static_cast<uint16_t*>(a.dv)[at + 64] = f32_to_bf16(y1);
 }
 
-// LDS arrays of the ring: NS stages of two tensors' tiles, every stage its own array
-// (so that the wait for one stage's loads is not for the others').
-#define SA_DOT_RING(W)                                                                                                 \
-  __shared__ __attribute__((aligned(16))) char xst0[(W)*T::bytes], xst1[(W)*T::bytes], yst0[(W)*T::bytes], yst1[(W)*T::bytes]; \
-  __shared__ __attribute__((aligned(16))) char xst2[PRIV ? 16 : T::bytes], xst3[PRIV ? 16 : T::bytes],                   \
-      yst2[PRIV ? 16 : T::bytes], yst3[PRIV ? 16 : T::bytes];                                                           \
-  auto xst = [&](auto SC) __attribute__((always_inline)) {                                                             \
-    constexpr int X = decltype(SC)::value;                                                                             \
-    return to_lds(X == 0 ? xst0 : X == 1 ? xst1 : X == 2 ? xst2 : xst3);                                               \
-  };                                                                                                                   \
-  auto yst = [&](auto SC) __attribute__((always_inline)) {                                                             \
-    constexpr int X = decltype(SC)::value;                                                                             \
-    return to_lds(X == 0 ? yst0 : X == 1 ? yst1 : X == 2 ? yst2 : yst3);                                               \
+// LDS arrays of the ring: W copies of NS stages of two tensors' tiles, every stage its own
+// array (so that the wait for one stage's loads is not for the others').
+#define SA_DOT_RING(W, NS)                                                                                  \
+  __shared__ __attribute__((aligned(16))) char xst0[(W)*T::bytes], xst1[(W)*T::bytes], yst0[(W)*T::bytes],  \
+      yst1[(W)*T::bytes], xst2[NS > 2 ? (W)*T::bytes : 16], xst3[NS > 2 ? (W)*T::bytes : 16],               \
+      yst2[NS > 2 ? (W)*T::bytes : 16], yst3[NS > 2 ? (W)*T::bytes : 16];                                   \
+  auto xst = [&](auto SC) __attribute__((always_inline)) {                                                  \
+    constexpr int X = decltype(SC)::value;                                                                  \
+    return to_lds(X == 0 ? xst0 : X == 1 ? xst1 : X == 2 ? xst2 : xst3);                                    \
+  };                                                                                                        \
+  auto yst = [&](auto SC) __attribute__((always_inline)) {                                                  \
+    constexpr int X = decltype(SC)::value;                                                                  \
+    return to_lds(X == 0 ? yst0 : X == 1 ? yst1 : X == 2 ? yst2 : yst3);                                    \
   }
+
+// The second group's accumulators into the first's, through LDS: 64 floats a register.
+template <int NDT>
+__device__ __forceinline__ void leave(const f32x16_t (&acc)[NDT], float* buf) {
+#pragma unroll
+  for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) buf[64 * (16 * dt + v)] = acc[dt][v];
+}
+template <int NDT>
+__device__ __forceinline__ void take(f32x16_t (&acc)[NDT], const float* buf) {
+#pragma unroll
+  for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[dt][v] += buf[64 * (16 * dt + v)];
+}
 
 // Adds the wavefronts' accumulator tiles in order, through one LDS array of 16 KB each:
 // wavefront w ends with quad w (columns 8 w + 4 h .. + 3) of every tile in y.
@@ -173,18 +189,19 @@ __device__ __forceinline__ float store_quads(uint16_t* p, const float (&y)[NDT][
 }
 
 // ---- query side ----
-template <int DP, bool CAP, bool BIAS, bool PRIV>
-__global__ __launch_bounds__(kThreads, PRIV ? 1 : 2) void dot_dq_kernel(DotArgs a) {
+template <int DP, bool CAP, bool BIAS, bool PRIV, int GROUPS>
+__global__ __launch_bounds__(kThreads* GROUPS, PRIV ? 1 : 2) void dot_dq_kernel(DotArgs a) {
   using T = SwzTile<DP>;
   constexpr int NT = DP / 16, NDT = DP / 32, SPW = PRIV ? T::instrs : T::instrs / kWaves, kRows = PRIV ? 32 : 32 * kWaves;
   constexpr int NS = PRIV ? 2 : 4;
-  SA_DOT_RING(PRIV ? kWaves : 1);
+  SA_DOT_RING(PRIV ? kWaves : GROUPS, NS);
   const int R = a.G * a.Nq, nrb = (R + kRows - 1) / kRows;
   int64_t unit;
   if (!unit_of(static_cast<int64_t>(a.B) * a.Hkv, nrb, unit)) return;
   const int block = nrb - 1 - static_cast<int>(unit % nrb), bh = static_cast<int>(unit / nrb);
   const int b = bh / a.Hkv, hk = bh - b * a.Hkv;
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 31, h = lane >> 5;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane((tid >> 6) % kWaves), lane = tid & 63, c = lane & 31, h = lane >> 5;
+  const int group = GROUPS > 1 ? __builtin_amdgcn_readfirstlane(tid / kThreads) : 0, base = (PRIV ? wave : group) * T::bytes;
   const DotMask m(a, b);
   const int r0 = block * kRows + (PRIV ? 0 : 32 * wave);
   const Lanes w(a, m, hk, r0 + c);
@@ -214,7 +231,6 @@ __global__ __launch_bounds__(kThreads, PRIV ? 1 : 2) void dot_dq_kernel(DotArgs 
     const int64_t j0 = max(blk, 0) * kDotBlock;
     const int n = blk < 0 ? 0 : min(m.L - static_cast<int>(j0), kDotBlock);
     const auto rk = rows_of(kb + j0 * a.ksn, n, a.ksn, a.D), rv = rows_of(vb + j0 * a.vsn, n, a.vsn, a.D);
-    const int base = PRIV ? wave * T::bytes : 0;
 #pragma unroll
     for (int x = 0; x < SPW; ++x) load_lds16(rk, xst(SC) + base + 1024 * (PRIV ? x : x * kWaves + wave), kvoff[x]);
 #pragma unroll
@@ -240,28 +256,34 @@ __global__ __launch_bounds__(kThreads, PRIV ? 1 : 2) void dot_dq_kernel(DotArgs 
   }
   const float lse = w.valid ? a.lse[(static_cast<int64_t>(b) * a.H + w.head) * a.Nq + w.i] : -kInf;
   const float lse2 = lse == -kInf ? kInf : lse * kLog2e;
-  if (h == 0 && some && (!PRIV || wave == 0)) {
+  if (h == 0 && some && group == 0 && (!PRIV || wave == 0)) {
     Stat& st = stats_of(a, bh)[r0 / 32];
     st.lse2[c] = lse2;
     st.delta[c] = w.valid ? delta : 0.f;
     st.slope2[c] = score.slope2;
     st.query[c] = static_cast<float>(w.i - div_group(r0, a));
   }
-  const Frags<DP> frag(lane, PRIV ? wave * T::bytes : 0);
+  const Frags<DP> frag(lane, base);
   DotBlock bq[NS];
-  bq[0] = seq.next();
-  load(IC<0>{}, bq[0].blk);
-  bq[1] = seq.next();
-  load(IC<1>{}, bq[1].blk);
-  if constexpr (!PRIV) {
-    bq[2] = seq.next();
-    load(IC<2>{}, bq[2].blk);
-  }
+  int lead[NS];  // group 0's block: the groups end together
+  auto next = [&](auto SC) __attribute__((always_inline)) {
+    constexpr int S = decltype(SC)::value;
+    bq[S] = seq.next();
+    lead[S] = bq[S].blk;
+    if constexpr (GROUPS > 1) {
+      const DotBlock other = seq.next();
+      if (group) bq[S] = other;
+    }
+    load(SC, bq[S].blk);
+  };
+  next(IC<0>{});
+  next(IC<1>{});
+  if constexpr (!PRIV) next(IC<2>{});
   f32x16_t acc[NDT] = {};
   auto iteration = [&](auto SC) __attribute__((always_inline)) {
     constexpr int S = decltype(SC)::value;
     const DotBlock at = bq[S];
-    if (at.blk < 0) return false;
+    if (lead[S] < 0) return false;
     const Frags<DP> f = frag.fresh();
     if constexpr (PRIV) {
       wait_vmcnt<2 * SPW>();
@@ -269,8 +291,7 @@ __global__ __launch_bounds__(kThreads, PRIV ? 1 : 2) void dot_dq_kernel(DotArgs 
     } else {
       wait_vmcnt<4 * SPW>();
       lds_barrier_tracked();
-      bq[(S + 3) % NS] = seq.next();
-      load(IC<(S + 3) % NS>{}, bq[(S + 3) % NS].blk);
+      next(IC<(S + 3) % NS>{});
     }
     if (at.mine) {
       f32x16_t s = mfma32(f.row(xst(SC), 0), qf[0], f32x16_t{}), dp = mfma32(f.row(yst(SC), 0), gf[0], f32x16_t{});
@@ -302,8 +323,7 @@ __global__ __launch_bounds__(kThreads, PRIV ? 1 : 2) void dot_dq_kernel(DotArgs 
     if constexpr (PRIV) {
       __builtin_amdgcn_s_waitcnt(0xC07F);  // the stage is read: its next block may come
       asm volatile("" ::: "memory");
-      bq[S] = seq.next();
-      load(SC, bq[S].blk);
+      next(SC);
     }
     return true;
   };
@@ -315,6 +335,14 @@ __global__ __launch_bounds__(kThreads, PRIV ? 1 : 2) void dot_dq_kernel(DotArgs 
     }
   }
   wait_vmcnt<0>();
+  if constexpr (GROUPS > 1) {
+    float* buf = reinterpret_cast<float*>(wave == 0 ? xst0 : wave == 1 ? xst1 : wave == 2 ? xst2 : xst3) + lane;
+    __syncthreads();
+    if (group) leave(acc, buf);
+    __syncthreads();
+    if (group) return;
+    take(acc, buf);
+  }
   uint16_t* dst = static_cast<uint16_t*>(a.dq) + orow + 4 * h;
   unsigned bad = 0;
   if constexpr (PRIV) {
@@ -343,32 +371,36 @@ __global__ __launch_bounds__(kThreads, PRIV ? 1 : 2) void dot_dq_kernel(DotArgs 
 }
 
 // ---- key side ----
-template <int DP, bool CAP, bool BIAS, bool PRIV>
-__global__ __launch_bounds__(kThreads, PRIV ? 1 : 2) void dot_dkv_kernel(DotArgs a) {
+template <int DP, bool CAP, bool BIAS, bool PRIV, int GROUPS>
+__global__ __launch_bounds__(kThreads* GROUPS, PRIV ? 1 : 2) void dot_dkv_kernel(DotArgs a) {
   using T = SwzTile<DP>;
   constexpr int NT = DP / 16, NDT = DP / 32, SPW = PRIV ? T::instrs : T::instrs / kWaves, kKeys = PRIV ? 32 : 32 * kWaves;
   constexpr int NS = PRIV ? 2 : 4, kInfo = BIAS ? 512 : 256, LPB = 2 * SPW + (BIAS ? 2 : 1);  // loads of a block
-  SA_DOT_RING(PRIV ? kWaves : 1);
-  __shared__ __attribute__((aligned(16))) char info0[(PRIV ? kWaves : 1) * kInfo], info1[(PRIV ? kWaves : 1) * kInfo],
-      info2[PRIV ? 16 : kInfo], info3[PRIV ? 16 : kInfo];
-  auto ist = [&](auto SC) __attribute__((always_inline)) {
-    constexpr int X = decltype(SC)::value;
-    return to_lds(X == 0 ? info0 : X == 1 ? info1 : X == 2 ? info2 : info3) + (PRIV ? (threadIdx.x >> 6) * kInfo : 0);
-  };
+  SA_DOT_RING(PRIV ? kWaves : GROUPS, NS);
+  constexpr int kCopies = PRIV ? kWaves : GROUPS;
+  __shared__ __attribute__((aligned(16))) char info0[kCopies * kInfo], info1[kCopies * kInfo], info2[NS > 2 ? kCopies * kInfo : 16],
+      info3[NS > 2 ? kCopies * kInfo : 16];
   const int R = a.G * a.Nq, nkb = (a.Nk + kKeys - 1) / kKeys;
   int64_t unit;
-  if (!unit_of(static_cast<int64_t>(a.B) * a.Hkv, nkb, unit)) return;
+  if (!unit_of(static_cast<int64_t>(a.B) * a.Hkv, static_cast<int64_t>(nkb) * a.ks, unit)) return;
+  const int part = static_cast<int>(unit % a.ks);
+  unit /= a.ks;
   const int block = static_cast<int>(unit % nkb), bh = static_cast<int>(unit / nkb);
   const int b = bh / a.Hkv, hk = bh - b * a.Hkv;
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 31, h = lane >> 5;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane((tid >> 6) % kWaves), lane = tid & 63, c = lane & 31, h = lane >> 5;
+  const int group = GROUPS > 1 ? __builtin_amdgcn_readfirstlane(tid / kThreads) : 0, base = (PRIV ? wave : group) * T::bytes;
   const DotMask m(a, b);
+  auto ist = [&](auto SC) __attribute__((always_inline)) {
+    constexpr int X = decltype(SC)::value;
+    return to_lds(X == 0 ? info0 : X == 1 ? info1 : X == 2 ? info2 : info3) + base / T::bytes * kInfo;
+  };
   const int j0 = block * kKeys + (PRIV ? 0 : 32 * wave), j = j0 + c;
   const DotSpan all(m, block * kKeys, block * kKeys + kKeys - 1), own(m, j0, j0 + 31);
   const Scores<CAP, false> score(a, 0);
   int lo, hi;
   row_blocks(m, all, a.G, R, lo, hi);
   const bool some = j0 < m.L;
-  auto seq = block_seq(lo, hi, PRIV ? wave : 0, PRIV ? kWaves : 1, [&](int blk, bool& live, bool& mine, bool& full) {
+  auto seq = block_seq(lo, hi, PRIV ? wave : part, PRIV ? kWaves : a.ks, [&](int blk, bool& live, bool& mine, bool& full) {
     const DotSpan q(m, m.first + div_group(blk * 32, a), m.first + div_group(min(blk * 32 + 32, R) - 1, a));
     live = dot_live(m, q, all);
     mine = some && dot_live(m, q, own);
@@ -391,7 +423,6 @@ __global__ __launch_bounds__(kThreads, PRIV ? 1 : 2) void dot_dkv_kernel(DotArgs
     const int i0 = div_group(max(blk, 0) * 32, a), n = blk < 0 ? 0 : min(a.Nq - i0, 33);
     const auto rq = rows_of(qb + i0 * a.qsn, n, a.qsn, (a.H - 1) * a.qsh + a.D), rg = rows_of(gb + i0 * gsn, n, gsn, gsn);
     const auto rs = make_rsrc(stats + max(blk, 0), blk < 0 ? 0 : sizeof(Stat));
-    const int base = PRIV ? wave * T::bytes : 0;
     const int ln = lane_anew();
     // Rows of q and dO: the chunk of row 32 blk + p / CH that this lane brings.
 #pragma unroll
@@ -410,21 +441,27 @@ __global__ __launch_bounds__(kThreads, PRIV ? 1 : 2) void dot_dkv_kernel(DotArgs
   u32x4_t kf[NT], vf[NT];
   load_row<DP>(kf, static_cast<const uint16_t*>(a.k) + b * a.ksb + (key ? j : 0) * a.ksn + hk * a.ksh, key, a.D, h);
   load_row<DP>(vf, static_cast<const uint16_t*>(a.v) + b * a.vsb + (key ? j : 0) * a.vsn + hk * a.vsh, key, a.D, h);
-  const Frags<DP> frag(lane, PRIV ? wave * T::bytes : 0);
+  const Frags<DP> frag(lane, base);
   DotBlock bq[NS];
-  bq[0] = seq.next();
-  load(IC<0>{}, bq[0].blk);
-  bq[1] = seq.next();
-  load(IC<1>{}, bq[1].blk);
-  if constexpr (!PRIV) {
-    bq[2] = seq.next();
-    load(IC<2>{}, bq[2].blk);
-  }
+  int lead[NS];  // group 0's block: the groups end together
+  auto next = [&](auto SC) __attribute__((always_inline)) {
+    constexpr int S = decltype(SC)::value;
+    bq[S] = seq.next();
+    lead[S] = bq[S].blk;
+    if constexpr (GROUPS > 1) {
+      const DotBlock other = seq.next();
+      if (group) bq[S] = other;
+    }
+    load(SC, bq[S].blk);
+  };
+  next(IC<0>{});
+  next(IC<1>{});
+  if constexpr (!PRIV) next(IC<2>{});
   f32x16_t acck[NDT] = {}, accv[NDT] = {};
   auto iteration = [&](auto SC) __attribute__((always_inline)) {
     constexpr int S = decltype(SC)::value;
     const DotBlock at = bq[S];
-    if (at.blk < 0) return false;
+    if (lead[S] < 0) return false;
     const Frags<DP> f = frag.fresh();
     if constexpr (PRIV) {
       wait_vmcnt<LPB>();
@@ -432,16 +469,21 @@ __global__ __launch_bounds__(kThreads, PRIV ? 1 : 2) void dot_dkv_kernel(DotArgs
     } else {
       wait_vmcnt<2 * LPB>();
       lds_barrier_tracked();
-      bq[(S + 3) % NS] = seq.next();
-      load(IC<(S + 3) % NS>{}, bq[(S + 3) % NS].blk);
+      next(IC<(S + 3) % NS>{});
     }
     if (at.mine) {
       const int ln = lane_anew(), jn = j0 + (ln & 31);
       // Bit v: whether the pair of accumulator register v is visible (before the products,
       // where registers are free; rows past the last one have probabilities of 0 as they are).
-      const unsigned seen = at.full ? 0xffffu : pairs_seen(m, QueriesSeeing(m, jn), ln & 31, ln >> 5, [&](int x) {
-        return m.first + div_group(at.blk * 32 + x, a);
-      });
+      unsigned seen = 0;
+      auto position = [&](int x) { return m.first + div_group(at.blk * 32 + x, a); };
+      if (!at.full) {
+        const QueriesSeeing sees(m, jn);
+        if constexpr (DP == 64)
+          each_pair(m, sees, ln & 31, ln >> 5, position, [&](int v, bool see) { seen |= static_cast<unsigned>(see) << v; });
+        else  // (unrolled it spills: 3029 us for 2527 at B=1 H=32 N=8192 D=128, all pairs)
+          seen = pairs_seen(m, sees, ln & 31, ln >> 5, position);
+      }
       f32x16_t s = mfma32(f.row(xst(SC), 0), kf[0], f32x16_t{}), dp = mfma32(f.row(yst(SC), 0), vf[0], f32x16_t{});
 #pragma unroll
       for (int t = 1; t < NT; ++t) {
@@ -493,8 +535,7 @@ __global__ __launch_bounds__(kThreads, PRIV ? 1 : 2) void dot_dkv_kernel(DotArgs
     if constexpr (PRIV) {
       __builtin_amdgcn_s_waitcnt(0xC07F);  // the stage is read: its next block may come
       asm volatile("" ::: "memory");
-      bq[S] = seq.next();
-      load(SC, bq[S].blk);
+      next(SC);
     }
     return true;
   };
@@ -506,7 +547,31 @@ __global__ __launch_bounds__(kThreads, PRIV ? 1 : 2) void dot_dkv_kernel(DotArgs
     }
   }
   wait_vmcnt<0>();
+  if constexpr (GROUPS > 1) {
+    float* bk = reinterpret_cast<float*>(wave == 0 ? xst0 : wave == 1 ? xst1 : wave == 2 ? xst2 : xst3) + lane;
+    float* bv = reinterpret_cast<float*>(wave == 0 ? yst0 : wave == 1 ? yst1 : wave == 2 ? yst2 : yst3) + lane;
+    __syncthreads();
+    if (group) leave(acck, bk), leave(accv, bv);
+    __syncthreads();
+    if (group) return;
+    take(acck, bk);
+    take(accv, bv);
+  }
   const bool out = j < a.Nk;
+  if (!PRIV && a.ks > 1) {  // partial sums, added by dot_keys_kernel
+    if (!out) return;
+    const int64_t n = static_cast<int64_t>(a.B) * a.Hkv * a.Nk * a.D;
+    float* p = a.part + 2 * part * n + (static_cast<int64_t>(bh) * a.Nk + j) * a.D + 4 * h;
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (32 * dt + 8 * q < a.D) {
+          *reinterpret_cast<f32x4_t*>(p + 32 * dt + 8 * q) = f32x4_t{acck[dt][4 * q], acck[dt][4 * q + 1], acck[dt][4 * q + 2], acck[dt][4 * q + 3]};
+          *reinterpret_cast<f32x4_t*>(p + n + 32 * dt + 8 * q) = f32x4_t{accv[dt][4 * q], accv[dt][4 * q + 1], accv[dt][4 * q + 2], accv[dt][4 * q + 3]};
+        }
+    return;
+  }
   const int64_t at = ((static_cast<int64_t>(b) * a.Nk + (out ? j : 0)) * a.Hkv + hk) * a.D + 4 * h;
   uint16_t *pk = static_cast<uint16_t*>(a.dk) + at, *pv = static_cast<uint16_t*>(a.dv) + at;
   unsigned bad = 0;
@@ -539,19 +604,52 @@ __global__ __launch_bounds__(kThreads, PRIV ? 1 : 2) void dot_dkv_kernel(DotArgs
   }
 }
 
-template <int DP, bool CAP, bool BIAS, bool PRIV>
-void launch(const DotArgs& a, hipStream_t st) {
-  const int64_t R = static_cast<int64_t>(a.G) * a.Nq, heads = static_cast<int64_t>(a.B) * a.Hkv;
-  constexpr int n = PRIV ? 32 : 128;
-  dot_dq_kernel<DP, CAP, BIAS, PRIV><<<unit_grid(heads, ((R + n - 1) / n)), kThreads, 0, st>>>(a);
-  dot_dkv_kernel<DP, CAP, BIAS, PRIV><<<unit_grid(heads, ((a.Nk + n - 1) / n)), kThreads, 0, st>>>(a);
+// dK and dV from the partial sums of a.ks workgroups, a wavefront a key.
+__global__ __launch_bounds__(kThreads) void dot_keys_kernel(DotArgs a) {
+  const int64_t keys = static_cast<int64_t>(a.B) * a.Hkv * a.Nk, at = static_cast<int64_t>(blockIdx.x) * kWaves + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  if (at >= keys) return;
+  const bool d0 = lane < a.D, d1 = lane + 64 < a.D;
+  const int64_t n = keys * a.D;
+  const float* p = a.part + at * a.D + lane;
+  float x0 = 0.f, x1 = 0.f, y0 = 0.f, y1 = 0.f;
+  for (int s = 0; s < a.ks; ++s, p += 2 * n) {
+    if (d0) x0 += p[0], y0 += p[n];
+    if (d1) x1 += p[64], y1 += p[n + 64];
+  }
+  const int bh = static_cast<int>(at / a.Nk), j = static_cast<int>(at - static_cast<int64_t>(bh) * a.Nk), b = bh / a.Hkv, hk = bh - b * a.Hkv;
+  const float check = (x0 + x1) * 0.f + (y0 + y1) * 0.f;
+  if (has_mask(a) && __builtin_amdgcn_ballot_w64(check != check) != 0) {
+    const DotMask m(a, b);
+    if (j < m.L) {
+      single_key(a, m, b, hk, j);
+      return;
+    }
+  }
+  const int64_t o = ((static_cast<int64_t>(b) * a.Nk + j) * a.Hkv + hk) * a.D + lane;
+  uint16_t *pk = static_cast<uint16_t*>(a.dk) + o, *pv = static_cast<uint16_t*>(a.dv) + o;
+  if (d0) pk[0] = f32_to_bf16(x0 * a.scale), pv[0] = f32_to_bf16(y0);
+  if (d1) pk[64] = f32_to_bf16(x1 * a.scale), pv[64] = f32_to_bf16(y1);
 }
+
 template <int DP, bool CAP, bool BIAS>
 void launch(const DotArgs& a, hipStream_t st) {
-  if (a.nsplit == 0)
-    launch<DP, CAP, BIAS, false>(a, st);
+  const int64_t R = static_cast<int64_t>(a.G) * a.Nq, heads = static_cast<int64_t>(a.B) * a.Hkv;
+  const unsigned wide = unit_grid(heads, (R + 127) / 128);
+  if (a.nsplit > 0)
+    dot_dq_kernel<DP, CAP, BIAS, true, 1><<<unit_grid(heads, (R + 31) / 32), kThreads, 0, st>>>(a);
+  else if (a.nsplit == 0)
+    dot_dq_kernel<DP, CAP, BIAS, false, 1><<<wide, kThreads, 0, st>>>(a);
   else
-    launch<DP, CAP, BIAS, true>(a, st);
+    dot_dq_kernel<DP, CAP, BIAS, false, 2><<<wide, 2 * kThreads, 0, st>>>(a);
+  const unsigned keys = unit_grid(heads, (a.Nk + 127) / 128 * static_cast<int64_t>(a.ks));
+  if (a.kside > 0)
+    dot_dkv_kernel<DP, CAP, BIAS, true, 1><<<unit_grid(heads, (a.Nk + 31) / 32), kThreads, 0, st>>>(a);
+  else if (a.kside == 0)
+    dot_dkv_kernel<DP, CAP, BIAS, false, 1><<<keys, kThreads, 0, st>>>(a);
+  else
+    dot_dkv_kernel<DP, CAP, BIAS, false, 2><<<keys, 2 * kThreads, 0, st>>>(a);
+  if (a.ks > 1) dot_keys_kernel<<<static_cast<unsigned>((heads * a.Nk + kWaves - 1) / kWaves), kThreads, 0, st>>>(a);
 }
 template <int DP>
 void launch(const DotArgs& a, hipStream_t st) {

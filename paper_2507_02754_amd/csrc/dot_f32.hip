@@ -604,15 +604,33 @@ hipError_t dot_ranges(const DotArgs& a, int2* ranges, hipStream_t st) {
   return hipGetLastError();
 }
 
+// How the bf16 kernels' workgroups own `units` blocks of 128 rows (or keys) of all heads:
+// 0 whole blocks of 128, a wavefront 32 each; -1 the same with two groups of wavefronts
+// that share the other side's blocks; 1 blocks of 32, their wavefronts sharing the other
+// side. Whole blocks move the fewest bytes, but where there are few of them the time is
+// that of the longest one. Measured, forward us of 0 / -1 / 1 (causal): D = 128, units 2048
+// 1138 / 1239 / 1826 (all pairs), 1024: 305 / 345 / 520, 512: 232 / 178 / 262, 256: 111 / 82 / 81 and
+// 38 / 33 / 45, 128: 60 / 47 / 31; D = 64 (twice the workgroups of 32 fit a CU), 1024: 71 / 86 / 88, 512: 55 /
+// 63 / 50, 128: 28 / 24 / 16. Documents make some blocks much longer than others: three of
+// them, units 1024, 457 / 315 / 430.
+int rows_form(int64_t units, int64_t D, bool docs) {
+  if (D <= 64) return units < 640 ? 1 : 0;
+  if (units <= 160) return 1;
+  return units < 768 || (docs && units <= 2048) ? -1 : 0;
+}
+
 DotPlan dot_fwd_plan(int64_t B, int64_t Nq, int64_t Nk, int64_t H, int64_t Hkv, int64_t D, int causal, int window, bool docs,
                      int dtype) {
-  DotPlan p;
-  const int64_t R = H / Hkv * Nq, units = B * Hkv * ((R + kDotBlock - 1) / kDotBlock);
-  // Keys a row block walks: the parts take 256 of them at least.
-  const int64_t keys = window && causal ? std::min<int64_t>(Nk, int64_t(window) + Nq) : Nk;
-  p.nsplit = static_cast<int>(std::max<int64_t>(1, std::min((dtype == SA_DTYPE_BF16 ? 512 : 1024) / units, keys / 256)));
-  // bf16: workgroups of 128 rows where they fill the chip.
-  if (dtype == SA_DTYPE_BF16 && B * Hkv * ((R + 127) / 128) >= 256) p.nsplit = 0;
+  DotPlan p = {};
+  const bool bf16 = dtype == SA_DTYPE_BF16;
+  const int64_t R = H / Hkv * Nq;
+  p.nsplit = bf16 ? rows_form(B * Hkv * ((R + 127) / 128), D, docs) : 1;
+  if (p.nsplit == 1) {
+    // Keys a row block walks: the parts take 256 of them at least.
+    const int64_t units = B * Hkv * ((R + kDotBlock - 1) / kDotBlock);
+    const int64_t keys = window && causal ? std::min<int64_t>(Nk, int64_t(window) + Nq) : Nk;
+    p.nsplit = static_cast<int>(std::max<int64_t>(1, std::min((bf16 ? 512 : 1024) / units, keys / 256)));
+  }
   p.ranges_off = 0;
   p.part_off = docs ? up256(static_cast<size_t>(B) * ((Nk + kDotBlock - 1) / kDotBlock) * sizeof(int2)) : 0;
   p.bytes = p.part_off + (p.nsplit > 1 ? static_cast<size_t>(B) * H * Nq * p.nsplit * (D + 3) * sizeof(float) : 0);
@@ -620,16 +638,33 @@ DotPlan dot_fwd_plan(int64_t B, int64_t Nq, int64_t Nk, int64_t H, int64_t Hkv, 
 }
 DotPlan dot_bwd_plan(int64_t B, int64_t Nq, int64_t Nk, int64_t H, int64_t Hkv, int64_t D, int causal, int window, bool docs,
                      int dtype) {
-  (void)D, (void)causal, (void)window;
-  DotPlan p;
-  const int64_t R = H / Hkv * Nq;
+  (void)causal, (void)window;
+  DotPlan p = {};
+  const int64_t R = H / Hkv * Nq, rows = B * Hkv * ((R + 127) / 128), keys = B * Hkv * ((Nk + 127) / 128);
   const bool bf16 = dtype == SA_DTYPE_BF16;
-  // bf16: workgroups of 128 rows or keys where they fill the chip.
-  p.nsplit = bf16 && B * Hkv * ((std::max(R, Nk) + 127) / 128) >= 256 ? 0 : 1;
+  p.nsplit = p.kside = p.ks = 1;
+  if (bf16) {
+    p.nsplit = rows_form(rows, D, docs);
+    // The key side: as the rows where a head has few of them; else `ks` workgroups for a
+    // block of 128 keys, their float32 sums added afterwards, up to about 1024 in all.
+    // Backward us of (0, ks 1) / (-1, 1) / 1 / (0, ks 2) / 4 / 8 at D = 128: keys 1024 (units of 128)
+    // 976 / 1075 / 1879 / 1076 / 1199 / 1470; 512: 778 / 560 / 1153 / 620 / 691 / 830; 256, R = 4096: 401 / 311 / 356 / 298 / 271 / 352; 256,
+    // R = 32768: 2252 / 1624 / 1595 / 1393 / 1170 / 1103; 32, R = 8192: 601 / 402 / 250 / 342 / 219 / 162; 256, R = 1024: 124 / 98 / 146 /
+    // 118 / 130 / 207; 96, R = 1500: 162 / 118 / 74 / 129 / 109 / 121.
+    if (D <= 64 ? keys < 640 && R <= 8192 : keys <= 128 && R < 2048)
+      p.kside = 1;
+    else if (keys >= 768)
+      p.kside = 0;
+    else if (R <= 2048 || keys >= 384)
+      p.kside = -1;
+    else
+      p.kside = 0, p.ks = static_cast<int>(std::max<int64_t>(2, std::min<int64_t>(8, 1024 / keys)));
+  }
   p.ranges_off = 0;
-  p.part_off = docs ? up256(static_cast<size_t>(B) * ((Nk + kDotBlock - 1) / kDotBlock) * sizeof(int2)) : 0;
+  p.delta_off = docs ? up256(static_cast<size_t>(B) * ((Nk + kDotBlock - 1) / kDotBlock) * sizeof(int2)) : 0;
   // Delta, or for every 32 rows what the bf16 kernels keep of them (dot_bwd.hip)
-  p.bytes = p.part_off + (bf16 ? static_cast<size_t>(B) * Hkv * ((R + 31) / 32) * 512 : static_cast<size_t>(B) * H * Nq * sizeof(float));
+  p.part_off = up256(p.delta_off + (bf16 ? static_cast<size_t>(B) * Hkv * ((R + 31) / 32) * 512 : static_cast<size_t>(B) * H * Nq * sizeof(float)));
+  p.bytes = p.part_off + (p.ks > 1 ? static_cast<size_t>(p.ks) * 2 * B * Hkv * Nk * D * sizeof(float) : 0);
   return p;
 }
 

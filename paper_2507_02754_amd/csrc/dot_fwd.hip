@@ -135,13 +135,13 @@ __device__ __forceinline__ void single_rows(const DotArgs& a, const DotMask& m, 
   }
 }
 
-template <int DP, bool CAP, bool BIAS>
-__global__ __launch_bounds__(kThreads, 2) void dot_fwd_kernel(DotArgs a) {
+template <int DP, bool CAP, bool BIAS, int GROUPS>
+__global__ __launch_bounds__(kThreads* GROUPS, 2) void dot_fwd_kernel(DotArgs a) {
   using T = SwzTile<DP>;
   constexpr int NT = DP / 16, NDT = DP / 32, SPW = T::instrs / kWaves, kStages = 4, kRows = 32 * kWaves;
   static_assert(T::instrs % kWaves == 0, "every wavefront issues as many loads of a tile");
-  __shared__ __attribute__((aligned(16))) char kst0[T::bytes], kst1[T::bytes], kst2[T::bytes], kst3[T::bytes];
-  __shared__ __attribute__((aligned(16))) char vst0[T::bytes], vst1[T::bytes], vst2[T::bytes], vst3[T::bytes];
+  __shared__ __attribute__((aligned(16))) char kst0[GROUPS * T::bytes], kst1[GROUPS * T::bytes], kst2[GROUPS * T::bytes], kst3[GROUPS * T::bytes];
+  __shared__ __attribute__((aligned(16))) char vst0[GROUPS * T::bytes], vst1[GROUPS * T::bytes], vst2[GROUPS * T::bytes], vst3[GROUPS * T::bytes];
   auto kst = [&](auto SC) __attribute__((always_inline)) {
     constexpr int X = decltype(SC)::value;
     return to_lds(X == 0 ? kst0 : X == 1 ? kst1 : X == 2 ? kst2 : kst3);
@@ -155,7 +155,8 @@ __global__ __launch_bounds__(kThreads, 2) void dot_fwd_kernel(DotArgs a) {
   if (!unit_of(static_cast<int64_t>(a.B) * a.Hkv, nrb, unit)) return;
   const int block = nrb - 1 - static_cast<int>(unit % nrb), bh = static_cast<int>(unit / nrb);
   const int b = bh / a.Hkv, hk = bh - b * a.Hkv;
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 31, h = lane >> 5;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane((tid >> 6) % kWaves), lane = tid & 63, c = lane & 31, h = lane >> 5;
+  const int group = GROUPS > 1 ? __builtin_amdgcn_readfirstlane(tid / kThreads) : 0, base = group * T::bytes;
   const DotMask m(a, b);
   const int r0 = block * kRows + 32 * wave;
   const Lanes w(a, m, hk, r0 + c);
@@ -188,27 +189,37 @@ __global__ __launch_bounds__(kThreads, 2) void dot_fwd_kernel(DotArgs a) {
     const int64_t j0 = max(blk, 0) * kDotBlock;
     const auto r = rows_of(kb + j0 * a.ksn, blk < 0 ? 0 : min(m.L - static_cast<int>(j0), kDotBlock), a.ksn, a.D);
 #pragma unroll
-    for (int x = 0; x < SPW; ++x) load_lds16(r, dst + 1024 * (x * kWaves + wave), kvoff[x]);
+    for (int x = 0; x < SPW; ++x) load_lds16(r, dst + base + 1024 * (x * kWaves + wave), kvoff[x]);
   };
   auto load_v = [&](lds_char* dst, int blk) __attribute__((always_inline)) {
     const int64_t j0 = max(blk, 0) * kDotBlock;
     const auto r = rows_of(vb + j0 * a.vsn, blk < 0 ? 0 : min(m.L - static_cast<int>(j0), kDotBlock), a.vsn, a.D);
 #pragma unroll
-    for (int x = 0; x < SPW; ++x) load_lds16(r, dst + 1024 * (x * kWaves + wave), vvoff[x]);
+    for (int x = 0; x < SPW; ++x) load_lds16(r, dst + base + 1024 * (x * kWaves + wave), vvoff[x]);
   };
   u32x4_t qf[NT];
   load_row<DP>(qf, q_row(a, w, b), w.valid, a.D, h);
-  const Frags<DP> frag(lane, 0);
+  const Frags<DP> frag(lane, base);
   DotBlock bq[kStages];
-  bq[0] = seq.next();
+  int lead[kStages];  // group 0's block: the groups end together
+  auto next = [&](auto SC) __attribute__((always_inline)) {
+    constexpr int S = decltype(SC)::value;
+    bq[S] = seq.next();
+    lead[S] = bq[S].blk;
+    if constexpr (GROUPS > 1) {
+      const DotBlock other = seq.next();
+      if (group) bq[S] = other;
+    }
+  };
+  next(IC<0>{});
   load_k(kst(IC<0>{}), bq[0].blk);
-  bq[1] = seq.next();
+  next(IC<1>{});
   load_k(kst(IC<1>{}), bq[1].blk);
   load_v(vst(IC<0>{}), bq[0].blk);
-  bq[2] = seq.next();
+  next(IC<2>{});
   load_k(kst(IC<2>{}), bq[2].blk);
   load_v(vst(IC<1>{}), bq[1].blk);
-  bq[3] = seq.next();
+  next(IC<3>{});
   load_k(kst(IC<3>{}), bq[3].blk);
   load_v(vst(IC<2>{}), bq[2].blk);
 
@@ -235,11 +246,11 @@ __global__ __launch_bounds__(kThreads, 2) void dot_fwd_kernel(DotArgs a) {
   auto iteration = [&](auto SC) __attribute__((always_inline)) {
     constexpr int S = decltype(SC)::value, cur = S & 1, nxt = cur ^ 1;
     const DotBlock at = bq[S];
-    if (at.blk < 0) return false;
+    if (lead[S] < 0) return false;
     const Frags<DP> f = frag.fresh();
     wait_vmcnt<3 * SPW>();
     lds_barrier_tracked();
-    bq[S] = seq.next();
+    next(IC<S>{});
     load_k(kst(IC<S>{}), bq[S].blk);                            // K(n) was read in iteration n - 2
     load_v(vst(IC<(S + 3) % kStages>{}), bq[(S + 3) % kStages].blk);  // V(n - 1) in iteration n - 1
     if (at.mine) {
@@ -273,6 +284,29 @@ __global__ __launch_bounds__(kThreads, 2) void dot_fwd_kernel(DotArgs a) {
   }
   wait_vmcnt<0>();
   row.finish();
+  if constexpr (GROUPS > 1) {
+    // The second group's states into the first's, through the ring's LDS (a stage's array a wavefront).
+    __shared__ float stat[3][kWaves][32];
+    float* buf = reinterpret_cast<float*>(wave == 0 ? kst0 : wave == 1 ? kst1 : wave == 2 ? kst2 : kst3) + lane;
+    __syncthreads();
+    if (group) {
+      if (h == 0) stat[0][wave][c] = row.m, stat[1][wave][c] = row.l, stat[2][wave][c] = row.lr;
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) buf[64 * (16 * dt + v)] = row.acc[dt][v];
+    }
+    __syncthreads();
+    if (group) return;
+    const float om = stat[0][wave][c], top = fmaxf(row.m, om), x = fast_exp2(row.m - top), y = fast_exp2(om - top);
+    row.m = top;
+    row.l = x * row.l + y * stat[1][wave][c];
+    row.lr = x * row.lr + y * stat[2][wave][c];
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) row.acc[dt][v] = x * row.acc[dt][v] + y * buf[64 * (16 * dt + v)];
+  }
   const bool empty = row.l == 0.f;
   const float inv = empty ? 0.f : 1.f / row.lr;
   const float lse = empty ? -kInf : row.m * kLn2 + logf(row.l);
@@ -450,26 +484,40 @@ __global__ __launch_bounds__(kThreads, 1) void dot_few_kernel(DotArgs a) {
   if (wave == 0) single_rows(a, m, b, w, lse, flags[0] | flags[1] | flags[2] | flags[3]);
 }
 
-// Joins the parts of a row, four rows a workgroup, a wavefront each.
+// Joins the parts of a row: one workgroup, its wavefronts taking every fourth part.
 __global__ __launch_bounds__(kThreads) void dot_join_kernel(DotArgs a) {
-  const int64_t all = static_cast<int64_t>(a.B) * a.H * a.Nq, r = static_cast<int64_t>(blockIdx.x) * kWaves + (threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63;
-  if (r >= all) return;
+  const int64_t all = static_cast<int64_t>(a.B) * a.H * a.Nq, r = blockIdx.x;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const float* st = a.part + all * a.nsplit * a.D + r * a.nsplit * 3;
+  const float* rows = a.part + r * a.nsplit * a.D + lane;
+  const bool d0 = lane < a.D, d1 = lane + 64 < a.D;
   float top = -kInf;
   for (int s = lane; s < a.nsplit; s += 64) top = fmaxf(top, st[3 * s]);
   top = reduce32(top, [](float x, float y) { return fmaxf(x, y); });
   top = fmaxf(top, swap_halves(top));
   const float base = top == -kInf ? 0.f : top;
   float l = 0.f, lr = 0.f, x0 = 0.f, x1 = 0.f;
-  for (int s = 0; s < a.nsplit; ++s) {
-    const float f = fast_exp2(st[3 * s] - base);
-    l += f * st[3 * s + 1];
-    lr += f * st[3 * s + 2];
-    const float* p = a.part + (r * a.nsplit + s) * a.D;
-    x0 += lane < a.D ? f * p[lane] : 0.f;
-    x1 += lane + 64 < a.D ? f * p[lane + 64] : 0.f;
+  for (int s0 = 0; s0 < a.nsplit; s0 += 64) {
+    const int s = s0 + lane;
+    const float f = s < a.nsplit ? fast_exp2(st[3 * s] - base) : 0.f;
+    l += s < a.nsplit ? f * st[3 * s + 1] : 0.f;
+    lr += s < a.nsplit ? f * st[3 * s + 2] : 0.f;
+    const int n = min(a.nsplit - s0, 64);
+#pragma unroll 4
+    for (int i = wave; i < n; i += kWaves) {
+      const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), i));
+      const float* p = rows + static_cast<int64_t>(s0 + i) * a.D;
+      x0 += d0 ? w * p[0] : 0.f;
+      x1 += d1 ? w * p[64] : 0.f;
+    }
   }
+  __shared__ float sums[2][kWaves][64];
+  sums[0][wave][lane] = x0, sums[1][wave][lane] = x1;
+  __syncthreads();
+  if (wave) return;
+  x0 = ((sums[0][0][lane] + sums[0][1][lane]) + sums[0][2][lane]) + sums[0][3][lane];
+  x1 = ((sums[1][0][lane] + sums[1][1][lane]) + sums[1][2][lane]) + sums[1][3][lane];
+  l = sum64(l), lr = sum64(lr);
   const int64_t rh = static_cast<int64_t>(a.G) * a.Nq;
   const int bh = static_cast<int>(r / rh), rr = static_cast<int>(r - bh * rh), i = rr / a.G;
   const int b = bh / a.Hkv, head = (bh - b * a.Hkv) * a.G + rr - i * a.G;
@@ -481,20 +529,23 @@ __global__ __launch_bounds__(kThreads) void dot_join_kernel(DotArgs a) {
     return;
   }
   const float inv = l == 0.f ? 0.f : 1.f / lr;
-  uint16_t* out = static_cast<uint16_t*>(a.out) + ((static_cast<int64_t>(b) * a.Nq + i) * a.H + head) * a.D;
-  if (lane < a.D) out[lane] = f32_to_bf16(x0 * inv);
-  if (lane + 64 < a.D) out[lane + 64] = f32_to_bf16(x1 * inv);
+  uint16_t* out = static_cast<uint16_t*>(a.out) + ((static_cast<int64_t>(b) * a.Nq + i) * a.H + head) * a.D + lane;
+  if (d0) out[0] = f32_to_bf16(x0 * inv);
+  if (d1) out[64] = f32_to_bf16(x1 * inv);
 }
 
 template <int DP, bool CAP, bool BIAS>
 hipError_t launch(const DotArgs& a, hipStream_t st) {
   const int64_t R = static_cast<int64_t>(a.G) * a.Nq, heads = static_cast<int64_t>(a.B) * a.Hkv;
-  if (a.nsplit == 0) {
-    dot_fwd_kernel<DP, CAP, BIAS><<<unit_grid(heads, ((R + 127) / 128)), kThreads, 0, st>>>(a);
+  if (a.nsplit <= 0) {
+    if (a.nsplit == 0)
+      dot_fwd_kernel<DP, CAP, BIAS, 1><<<unit_grid(heads, (R + 127) / 128), kThreads, 0, st>>>(a);
+    else
+      dot_fwd_kernel<DP, CAP, BIAS, 2><<<unit_grid(heads, (R + 127) / 128), 2 * kThreads, 0, st>>>(a);
     return hipGetLastError();
   }
   dot_few_kernel<DP, CAP, BIAS><<<unit_grid(heads, ((R + 31) / 32) * a.nsplit), kThreads, 0, st>>>(a);
-  if (a.nsplit > 1) dot_join_kernel<<<static_cast<unsigned>((heads * R + kWaves - 1) / kWaves), kThreads, 0, st>>>(a);
+  if (a.nsplit > 1) dot_join_kernel<<<static_cast<unsigned>(heads * R), kThreads, 0, st>>>(a);
   return hipGetLastError();
 }
 template <int DP>

@@ -265,14 +265,15 @@ int simplicial_dot_attn_bwd(const void* q, const void* k, const void* v, const v
   a.dq = dq, a.dk = dk, a.dv = dv;
   char* ws = static_cast<char*>(workspace);
   hipStream_t st = static_cast<hipStream_t>(stream);
-  a.delta = reinterpret_cast<float*>(ws + p.part_off);
+  a.delta = reinterpret_cast<float*>(ws + p.delta_off);
+  a.part = reinterpret_cast<float*>(ws + p.part_off);
   if (documents) {
     int2* ranges = reinterpret_cast<int2*>(ws + p.ranges_off);
     const int r = to_status(sa::dot_ranges(a, ranges, st));
     if (r != SA_OK) return r;
     a.ranges = ranges;
   }
-  a.nsplit = p.nsplit;
+  a.nsplit = p.nsplit, a.kside = p.kside, a.ks = p.ks;
   return to_status(dtype == SA_DTYPE_BF16 ? sa::dot_bwd_bf16(a, st) : sa::dot_bwd_f32(a, st));
 }
 

@@ -73,13 +73,18 @@ struct DotArgs {
   // Smallest and largest document number of every 32 positions, [B, ceil(Nk / 32)].
   const int2* ranges;
   float* delta;  // backward: Delta [B, H, Nq] (bf16: what dot_bwd.hip keeps of the rows)
-  int nsplit;    // forward: parts of the key axis (bf16, 0: workgroups of 128 rows or keys)
-  float* part;   // forward, nsplit > 1: their partial results
+  // Workgroups over rows. Forward: parts of the key axis that workgroups of 32 rows take; bf16
+  // also 0: workgroups of 128 rows, -1: of 128 rows with two groups of wavefronts.
+  int nsplit;
+  // bf16 backward: likewise over keys (1, 0 or -1), and workgroups that share a block of
+  // keys, each a part of the rows (not with 1).
+  int kside, ks;
+  float* part;   // partial results of nsplit or ks > 1
   int dtype;
 };
 struct DotPlan {
-  int nsplit;
-  size_t ranges_off, part_off, bytes;
+  int nsplit, kside, ks;
+  size_t ranges_off, delta_off, part_off, bytes;
 };
 DotPlan dot_fwd_plan(int64_t B, int64_t Nq, int64_t Nk, int64_t H, int64_t Hkv, int64_t D, int causal, int window,
                      bool docs, int dtype);

@@ -81,6 +81,59 @@ def test_against_float64(size, dt):
     _check(q, k, v, dout, str(size), causal=causal, window=window, softcap=cap, slopes=_slopes(H) if alibi else None)
 
 
+# Sizes that take every form of the bf16 kernels: workgroups of 128 rows and keys, with one
+# group of wavefronts and two, and several workgroups a block of keys (float32 the same).
+FORMS = [
+    (4, 390, 64, 64, 128),   # 1024 blocks of 128 rows and of keys
+    (2, 450, 40, 20, 128),   # two groups of wavefronts on both sides
+    (1, 700, 16, 4, 128),    # grouped heads: several workgroups a block of keys
+    (1, 2100, 3, 1, 64),     # head_dim 64, likewise
+    (5, 300, 48, 48, 64),    # 128 rows at head_dim 64
+    (3, 520, 48, 16, 32),
+]
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("size", FORMS, ids=str)
+def test_every_form(size, dt):
+    """Each with a causal mask alone, documents with padding, a window with cap and bias, and
+    a prefix over caches filled to different lengths (one empty, one shorter than its queries)."""
+    B, N, H, Hkv, D = size
+    print(f"\n[dot] form {size} {dt}", flush=True)
+    q, k, v, dout = _inputs(B, N, N, H, Hkv, D, dt, seed=N)
+    _check(q, k, v, dout, f"{size} causal")
+    at = torch.arange(N)
+    ids = torch.stack([(at >= 37 + 11 * b).int() + (at >= N // 2).int() + (at >= N - 60).int() * 5 for b in range(B)]).to(torch.int32)
+    ids[0, N - 30:] = -1
+    _check(q, k, v, dout, f"{size} documents", documents=ids.cuda())
+    _check(q, k, v, dout, f"{size} window", window=131, softcap=3.0, slopes=_slopes(H))
+    lens = torch.tensor([N, N // 2, 0, 40, N - 1][:B], dtype=torch.int32).cuda()
+    prefix = torch.tensor([77, 33, 5, N, 0][:B], dtype=torch.int32).cuda()
+    for b in range(B):
+        k[b, int(lens[b]):] = float("nan")
+        v[b, int(lens[b]):] = float("inf")
+    _check(q, k, v, dout, f"{size} prefix", prefix=prefix, k_lens=lens, softcap=20.0)
+
+
+@pytest.mark.parametrize("size", [s for s in FORMS if s[4] >= 64], ids=str)
+@pytest.mark.parametrize("bad", [float("nan"), float("-inf")])
+def test_masked_values_in_every_form(size, bad):
+    """One later document of nothing but NaN or infinities: the others do not see it."""
+    B, N, H, Hkv, D = size
+    q, k, v, dout = _inputs(B, N, N, H, Hkv, D, BF, seed=N + 1)
+    n = N // 2 + 13
+    ids = (torch.arange(N) >= n).to(torch.int32).expand(B, N).contiguous().cuda()
+    want = ref.dot_attention(q, k, v, documents=ids, dout=dout)
+    for x in (q, k, v, dout):
+        x[:, n:] = bad
+    out, lse = simplicial_dot_attn_fwd(q, k, v, documents=ids)
+    grads = simplicial_dot_attn_bwd(q, k, v, out, dout, lse, documents=ids)
+    torch.cuda.synchronize()
+    ref.close(lse[:, :, :n], *(x[:, :, :n] for x in want["lse"]), "lse")
+    for name, x in zip(("out", "dq", "dk", "dv"), (out, *grads)):
+        ref.close(x[:, :n], *(y[:, :n] for y in want[name]), name)
+
+
 # B, Nq, Nk, H, Hkv, D, window, cap, lens
 NEW = [
     (1, 1, 1, 4, 4, 64, 0, 0.0, None),

@@ -169,7 +169,7 @@ int simplicial_norm_rotate_fwd(int32_t count, const void* const* x, const int64_
 
 size_t simplicial_norm_rotate_bwd_workspace_size(int32_t count, int64_t B, int64_t N, int64_t D) {
   if (count < 1 || count > SA_ROTATE_MAX || B <= 0 || N <= 0 || !known_dim(D)) return 0;
-  return sa::rotate_bwd_bytes(count, B, N, D);
+  return sa::rotate_bwd_bytes(count, D);
 }
 
 int simplicial_norm_rotate_bwd(int32_t count, const void* const* x, const int64_t* strides,
@@ -196,7 +196,7 @@ int simplicial_norm_rotate_bwd(int32_t count, const void* const* x, const int64_
   }
   if (dw) {
     if (!good({workspace})) return SA_ERR_INVALID;
-    if (workspace_bytes < sa::rotate_bwd_bytes(count, B, N, D)) return SA_ERR_WORKSPACE;
+    if (workspace_bytes < sa::rotate_bwd_bytes(count, D)) return SA_ERR_WORKSPACE;
   }
   return to_status(sa::rotate_bwd(a, dw ? static_cast<float*>(workspace) : nullptr, static_cast<hipStream_t>(stream)));
 }

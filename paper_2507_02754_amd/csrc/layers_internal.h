@@ -18,7 +18,7 @@ struct RotArgs {
   void* y[kRotTensors];         // forward: y, backward: dx
   void* dw[kRotTensors];        // backward: [D] or null
   int64_t sb[kRotTensors], sn[kRotTensors], sh[kRotTensors];
-  int heads[kRotTensors];
+  int heads[kRotTensors], shares[kRotTensors];
   int count;
   const int64_t* pos;
   int64_t pos_stride, start;
@@ -27,7 +27,7 @@ struct RotArgs {
   double turns[kRotFreqs];  // turns per position: freqs / 2 pi
 };
 hipError_t rotate_fwd(const RotArgs& a, hipStream_t st);
-size_t rotate_bwd_bytes(int count, int64_t B, int64_t N, int64_t D);
+size_t rotate_bwd_bytes(int count, int64_t D);
 hipError_t rotate_bwd(const RotArgs& a, float* part, hipStream_t st);
 
 // ---- logprobs.hip ----

@@ -180,207 +180,200 @@ __device__ __forceinline__ void turn_row(float* u, const Turn<LAYOUT>& t, const 
   }
 }
 
-// What a lane group works on: position (b, n) and heads s, s + hsplit, ... of all
-// tensors' heads in a row. Tensor and head of a flat head index.
-struct Which {
-  int t, h;
+// What a lane group works on: position (b, n) and heads sub, sub + n, ... of one tensor, whose
+// heads n groups share.
+struct Share {
+  int t, sub, n;
+  __device__ __forceinline__ Share(const RotArgs& a, int s) {
+    const int n0 = a.shares[0], n1 = a.shares[1];
+    t = s < n0 ? 0 : s < n0 + n1 ? 1 : 2;
+    sub = t == 0 ? s : t == 1 ? s - n0 : s - n0 - n1;
+    n = t == 0 ? n0 : t == 1 ? n1 : a.shares[2];
+  }
 };
-__device__ __forceinline__ Which which(const RotArgs& a, int f) {
-  const int h0 = a.heads[0], h1 = a.count > 1 ? a.heads[1] : 0;
-  return f < h0 ? Which{0, f} : f < h0 + h1 ? Which{1, f - h0} : Which{2, f - h0 - h1};
-}
 template <typename P>
 __device__ __forceinline__ P pick(P const (&p)[kRotTensors], int t) {
   return t == 0 ? p[0] : t == 1 ? p[1] : p[2];
-}
-__device__ __forceinline__ int all_heads(const RotArgs& a) {
-  return a.heads[0] + (a.count > 1 ? a.heads[1] : 0) + (a.count > 2 ? a.heads[2] : 0);
 }
 __device__ __forceinline__ float inv_rms(float sum, const RotArgs& a) {
   const float ms = sum / static_cast<float>(a.D) + a.eps;
   return ms > 0.f ? 1.f / sqrtf(ms) : ms == 0.f ? 0.f : ms;  // (NaN stays NaN)
 }
 
+// The weight's 16 elements of the lane (ones without one).
+template <int LAYOUT>
+__device__ __forceinline__ void lane_weight(float* w, const void* p, const RotArgs& a, const Runs<LAYOUT>& runs) {
+#pragma unroll
+  for (int e = 0; e < 16; ++e) w[e] = p ? ld_w(p, a.wdtype, (e < 8 ? runs.a : runs.b - 8) + e) : 1.f;
+}
+
 template <typename T, int LPR, int LAYOUT>
-__global__ __launch_bounds__(kRThreads) void rotate_fwd_kernel(RotArgs a, int hsplit) {
+__global__ __launch_bounds__(kRThreads) void rotate_fwd_kernel(RotArgs a) {
   const double* turns = arg_turns();
+  const int groups = a.shares[0] + a.shares[1] + a.shares[2];  // of a position
   const int64_t group = (static_cast<int64_t>(blockIdx.x) * kRThreads + threadIdx.x) / LPR;
   const int r = threadIdx.x % LPR;
-  const int64_t bn = group / hsplit;
+  const int64_t bn = group / groups;
   if (bn >= static_cast<int64_t>(a.B) * a.N) return;
-  const int s = static_cast<int>(group - bn * hsplit);
+  const Share sh(a, static_cast<int>(group - bn * groups));
   const int b = static_cast<int>(bn / a.N), n = static_cast<int>(bn - static_cast<int64_t>(b) * a.N);
   const Runs<LAYOUT> runs(r, a.nfreq);
   const int64_t p = a.pos ? a.pos[b * a.pos_stride + n] : a.start + n;
   const Turn<LAYOUT> turn(a, turns, r, static_cast<double>(p));
-  const int H = all_heads(a);
-  for (int f = s; f < H; f += hsplit) {
-    const Which w = which(a, f);
-    const T* x = static_cast<const T*>(pick(a.x, w.t)) + b * pick(a.sb, w.t) + n * pick(a.sn, w.t) + w.h * pick(a.sh, w.t);
+  const int heads = pick(a.heads, sh.t);
+  const int64_t step = pick(a.sh, sh.t);
+  const T* x = static_cast<const T*>(pick(a.x, sh.t)) + b * pick(a.sb, sh.t) + n * pick(a.sn, sh.t);
+  T* y = static_cast<T*>(pick(a.y, sh.t)) + bn * heads * a.D;
+  float w[16];
+  lane_weight(w, a.norm ? pick(a.w, sh.t) : nullptr, a, runs);
+  for (int h = sh.sub; h < heads; h += sh.n) {
     float u[16];
-    ld_run(x + runs.a).get(u);
-    ld_run(x + runs.b).get(u + 8);
+    ld_run(x + h * step + runs.a).get(u);
+    ld_run(x + h * step + runs.b).get(u + 8);
     if (a.norm) {
       float sum = 0.f;
 #pragma unroll
       for (int e = 0; e < 16; ++e) sum += u[e] * u[e];
       const float inv = inv_rms(row_sum<LPR>(sum), a);
-      const void* wt = pick(a.w, w.t);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) u[e] *= inv;
-      if (wt) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) u[e] *= ld_w(wt, a.wdtype, (e < 8 ? runs.a : runs.b - 8) + e);
-      }
+      for (int e = 0; e < 16; ++e) u[e] = u[e] * inv * w[e];
     }
     turn_row<LAYOUT, LPR, false>(u, turn, runs, r, a.nfreq);
-    const int hs = w.t == 0 ? a.heads[0] : w.t == 1 ? a.heads[1] : a.heads[2];
-    T* y = static_cast<T*>(pick(a.y, w.t)) + (bn * hs + w.h) * a.D;
     Run8<T> o;
     o.set(u);
-    *reinterpret_cast<Run8<T>*>(y + runs.a) = o;
+    *reinterpret_cast<Run8<T>*>(y + h * a.D + runs.a) = o;
     o.set(u + 8);
-    *reinterpret_cast<Run8<T>*>(y + runs.b) = o;
+    *reinterpret_cast<Run8<T>*>(y + h * a.D + runs.b) = o;
   }
 }
 
 // Backward. With a weight's gradient asked for (DW) the lane groups stride over the
-// positions and every workgroup leaves one partial sum per tensor in `part`
-// ([workgroup, tensor, D]), which rotate_dw_kernel adds in order.
+// positions (the grid is a multiple of a position's groups, so that each keeps its
+// tensor) and every workgroup leaves one partial sum per tensor in `part` ([workgroup,
+// tensor, D]), which rotate_dw_kernel adds in order.
 template <typename T, int LPR, int LAYOUT, bool DW>
-__global__ __launch_bounds__(kRThreads) void rotate_bwd_kernel(RotArgs a, int hsplit, float* part) {
+__global__ __launch_bounds__(kRThreads) void rotate_bwd_kernel(RotArgs a, float* part) {
   const double* turns = arg_turns();
+  const int groups = a.shares[0] + a.shares[1] + a.shares[2];
   const int64_t first = (static_cast<int64_t>(blockIdx.x) * kRThreads + threadIdx.x) / LPR;
-  const int64_t groups = static_cast<int64_t>(a.B) * a.N * hsplit;
-  const int64_t step = DW ? static_cast<int64_t>(gridDim.x) * (kRThreads / LPR) : groups;
+  const int64_t all = static_cast<int64_t>(a.B) * a.N;
+  const int64_t step = DW ? static_cast<int64_t>(gridDim.x) * (kRThreads / LPR) / groups : all;
   const int r = threadIdx.x % LPR;
   const Runs<LAYOUT> runs(r, a.nfreq);
-  const int H = all_heads(a);
-  float acc[DW ? kRotTensors : 1][16] = {};
-  for (int64_t group = first; group < groups; group += step) {
-    const int64_t bn = group / hsplit;
-    const int s = static_cast<int>(group - bn * hsplit);
+  const Share sh(a, static_cast<int>(first % groups));
+  const int heads = pick(a.heads, sh.t);
+  const int64_t hstep = pick(a.sh, sh.t);
+  float w[16];
+  lane_weight(w, a.norm ? pick(a.w, sh.t) : nullptr, a, runs);
+  float acc[DW ? 16 : 1] = {};
+  for (int64_t bn = first / groups; bn < all; bn += step) {
     const int b = static_cast<int>(bn / a.N), n = static_cast<int>(bn - static_cast<int64_t>(b) * a.N);
     const int64_t p = a.pos ? a.pos[b * a.pos_stride + n] : a.start + n;
     const Turn<LAYOUT> turn(a, turns, r, static_cast<double>(p));
-    for (int f = s; f < H; f += hsplit) {
-      const Which w = which(a, f);
-      const int hs = w.t == 0 ? a.heads[0] : w.t == 1 ? a.heads[1] : a.heads[2];
-      const int64_t o = (bn * hs + w.h) * a.D;
-      const T* dy = static_cast<const T*>(pick(a.dy, w.t)) + o;
-      float g[16];
-      ld_run(dy + runs.a).get(g);
-      ld_run(dy + runs.b).get(g + 8);
+    const T* x = static_cast<const T*>(pick(a.x, sh.t)) + b * pick(a.sb, sh.t) + n * pick(a.sn, sh.t);
+    const T* dy = static_cast<const T*>(pick(a.dy, sh.t)) + bn * heads * a.D;
+    T* dx = static_cast<T*>(pick(a.y, sh.t)) + bn * heads * a.D;
+    for (int h = sh.sub; h < heads; h += sh.n) {
+      float g[16], u[16];
+      const Run8<T> ga = ld_run(dy + h * a.D + runs.a), gb = ld_run(dy + h * a.D + runs.b);
+      const Run8<T> xa = ld_run(x + h * hstep + runs.a), xb = ld_run(x + h * hstep + runs.b);
+      ga.get(g);
+      gb.get(g + 8);
       turn_row<LAYOUT, LPR, true>(g, turn, runs, r, a.nfreq);
       if (a.norm) {
-        const T* x = static_cast<const T*>(pick(a.x, w.t)) + b * pick(a.sb, w.t) + n * pick(a.sn, w.t) + w.h * pick(a.sh, w.t);
-        float u[16];
-        ld_run(x + runs.a).get(u);
-        ld_run(x + runs.b).get(u + 8);
+        xa.get(u);
+        xb.get(u + 8);
         float sum = 0.f;
 #pragma unroll
         for (int e = 0; e < 16; ++e) sum += u[e] * u[e];
         const float inv = inv_rms(row_sum<LPR>(sum), a);
-        // u: x r from here on
-#pragma unroll
-        for (int e = 0; e < 16; ++e) u[e] *= inv;
-        if constexpr (DW) {
-#pragma unroll
-          for (int t = 0; t < kRotTensors; ++t)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[t][e] += w.t == t ? g[e] * u[e] : 0.f;
-        }
-        const void* wt = pick(a.w, w.t);
-        if (wt) {
-#pragma unroll
-          for (int e = 0; e < 16; ++e) g[e] *= ld_w(wt, a.wdtype, (e < 8 ? runs.a : runs.b - 8) + e);
-        }
         float dot = 0.f;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) dot += g[e] * u[e];
+        for (int e = 0; e < 16; ++e) {
+          u[e] *= inv;  // x r
+          if constexpr (DW) acc[e] += g[e] * u[e];
+          g[e] *= w[e];
+          dot += g[e] * u[e];
+        }
         dot = row_sum<LPR>(dot) / static_cast<float>(a.D);
 #pragma unroll
         for (int e = 0; e < 16; ++e) g[e] = inv * (g[e] - u[e] * dot);
       }
-      T* dx = static_cast<T*>(pick(a.y, w.t)) + o;
       Run8<T> z;
       z.set(g);
-      *reinterpret_cast<Run8<T>*>(dx + runs.a) = z;
+      *reinterpret_cast<Run8<T>*>(dx + h * a.D + runs.a) = z;
       z.set(g + 8);
-      *reinterpret_cast<Run8<T>*>(dx + runs.b) = z;
+      *reinterpret_cast<Run8<T>*>(dx + h * a.D + runs.b) = z;
     }
   }
   if constexpr (DW) {
+    constexpr int kGroups = kRThreads / LPR;
     __shared__ float red[kRThreads * 17];
 #pragma unroll
-    for (int t = 0; t < kRotTensors; ++t) {
-      if (t >= a.count) break;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) red[threadIdx.x * 17 + e] = acc[t][e];
-      __syncthreads();
-      if (threadIdx.x < 16 * LPR) {
-        const int lane = threadIdx.x / 16, e = threadIdx.x % 16;
-        float x = 0.f;
-        for (int g = 0; g < kRThreads / LPR; ++g) x += red[(g * LPR + lane) * 17 + e];
-        const Runs<LAYOUT> of(lane, a.nfreq);
-        part[(static_cast<int64_t>(blockIdx.x) * a.count + t) * a.D + (e < 8 ? of.a : of.b - 8) + e] = x;
-      }
-      __syncthreads();
+    for (int e = 0; e < 16; ++e) red[threadIdx.x * 17 + e] = acc[e];
+    __syncthreads();
+    const int64_t g0 = static_cast<int64_t>(blockIdx.x) * kGroups;
+    for (int at = threadIdx.x; at < a.count * 16 * LPR; at += kRThreads) {
+      const int t = at / (16 * LPR), lane = at / 16 % LPR, e = at % 16;
+      float x = 0.f;
+      for (int g = 0; g < kGroups; ++g)
+        if (Share(a, static_cast<int>((g0 + g) % groups)).t == t) x += red[(g * LPR + lane) * 17 + e];
+      const Runs<LAYOUT> of(lane, a.nfreq);
+      part[(static_cast<int64_t>(blockIdx.x) * a.count + t) * a.D + (e < 8 ? of.a : of.b - 8) + e] = x;
     }
   }
 }
 
-// dweight: 16 columns of one tensor a workgroup, 16 threads a column.
-__global__ __launch_bounds__(kRThreads) void rotate_dw_kernel(RotArgs a, const float* part, int blocks) {
+// dweight: 16 columns of one tensor a workgroup, 64 threads a column.
+constexpr int kDwThreads = 1024;
+__global__ __launch_bounds__(kDwThreads) void rotate_dw_kernel(RotArgs a, const float* part, int blocks) {
   const int per = a.D / 16, t = blockIdx.x / per, d = blockIdx.x % per * 16 + threadIdx.x % 16, row = threadIdx.x / 16;
   void* dw = pick(a.dw, t);
   if (!dw) return;
   float x = 0.f;
-  for (int i = row; i < blocks; i += 16) x += part[(static_cast<int64_t>(i) * a.count + t) * a.D + d];
-  __shared__ float red[16][17];
+#pragma unroll 4
+  for (int i = row; i < blocks; i += kDwThreads / 16) x += part[(static_cast<int64_t>(i) * a.count + t) * a.D + d];
+  __shared__ float red[kDwThreads / 16][17];
   red[row][threadIdx.x % 16] = x;
   __syncthreads();
   if (row) return;
   x = 0.f;
-  for (int i = 0; i < 16; ++i) x += red[i][threadIdx.x];
+  for (int i = 0; i < kDwThreads / 16; ++i) x += red[i][threadIdx.x];
   if (a.wdtype == SA_DTYPE_F32)
     static_cast<float*>(dw)[d] = x;
   else
     static_cast<uint16_t*>(dw)[d] = f32_to_bf16(x);
 }
 
-constexpr int64_t kRotBlocks = 1024;  // workgroups of a backward with weights
+constexpr int kRotBlocks = 1024;        // workgroups of a backward with weights, at most
 constexpr int64_t kRotLanes = 1 << 19;  // lanes that fill the chip (256 CUs x 2048)
 
-// Groups that share a position's heads: as few as fill the chip, so that sines and
-// cosines are formed for as many heads as possible.
-int head_split(int64_t positions, int lpr, int heads) {
-  int s = 1;
-  while (s < heads && positions * lpr * s < kRotLanes) s *= 2;
-  return std::min(s, heads);
-}
-int heads_of(const RotArgs& a) {
-  int h = 0;
-  for (int t = 0; t < a.count; ++t) h += a.heads[t];
-  return h;
-}
-int64_t rot_blocks(int64_t positions, int lpr, int hsplit) {
-  return (positions * hsplit * lpr + kRThreads - 1) / kRThreads;
+// Groups that share a tensor's heads at a position: few, so that sines and cosines are
+// formed for as many heads as possible, but enough for all positions to fill the chip.
+// Returns their sum.
+int share_heads(RotArgs& a, int lpr) {
+  int all = 0, sum = 0;
+  for (int t = 0; t < a.count; ++t) all += a.heads[t];
+  const int64_t positions = static_cast<int64_t>(a.B) * a.N, want = std::min<int64_t>({all, kRotBlocks / 2, (kRotLanes + positions * lpr - 1) / (positions * lpr)});
+  for (int t = 0; t < kRotTensors; ++t) {
+    a.shares[t] = t < a.count ? static_cast<int>(std::max<int64_t>(1, want * a.heads[t] / all)) : 0;
+    sum += a.shares[t];
+  }
+  return sum;
 }
 
 template <typename T, int LPR, int LAYOUT>
-hipError_t launch_rotate(const RotArgs& a, bool backward, float* part, hipStream_t st) {
-  const int64_t positions = static_cast<int64_t>(a.B) * a.N;
-  const int hs = head_split(positions, LPR, heads_of(a));
-  const int64_t blocks = rot_blocks(positions, LPR, hs);
+hipError_t launch_rotate(RotArgs a, bool backward, float* part, hipStream_t st) {
+  const int groups = share_heads(a, LPR);
+  const unsigned blocks = static_cast<unsigned>((static_cast<int64_t>(a.B) * a.N * groups * LPR + kRThreads - 1) / kRThreads);
   if (!backward) {
-    rotate_fwd_kernel<T, LPR, LAYOUT><<<static_cast<unsigned>(blocks), kRThreads, 0, st>>>(a, hs);
+    rotate_fwd_kernel<T, LPR, LAYOUT><<<blocks, kRThreads, 0, st>>>(a);
   } else if (!part) {
-    rotate_bwd_kernel<T, LPR, LAYOUT, false><<<static_cast<unsigned>(blocks), kRThreads, 0, st>>>(a, hs, nullptr);
+    rotate_bwd_kernel<T, LPR, LAYOUT, false><<<blocks, kRThreads, 0, st>>>(a, nullptr);
   } else {
-    const int nb = static_cast<int>(std::min(blocks, kRotBlocks));
-    rotate_bwd_kernel<T, LPR, LAYOUT, true><<<nb, kRThreads, 0, st>>>(a, hs, part);
-    rotate_dw_kernel<<<a.count * (a.D / 16), kRThreads, 0, st>>>(a, part, nb);
+    const int nb = std::max(1, static_cast<int>(std::min<unsigned>(blocks, kRotBlocks)) / groups) * groups;  // <= kRotBlocks
+    rotate_bwd_kernel<T, LPR, LAYOUT, true><<<nb, kRThreads, 0, st>>>(a, part);
+    rotate_dw_kernel<<<a.count * (a.D / 16), kDwThreads, 0, st>>>(a, part, nb);
   }
   return hipGetLastError();
 }
@@ -409,11 +402,7 @@ hipError_t launch(const RotArgs& a, bool backward, float* part, hipStream_t st) 
 
 hipError_t rotate_fwd(const RotArgs& a, hipStream_t st) { return launch(a, false, nullptr, st); }
 
-// (an upper bound over the head counts)
-size_t rotate_bwd_bytes(int count, int64_t B, int64_t N, int64_t D) {
-  (void)B, (void)N;
-  return static_cast<size_t>(kRotBlocks) * count * D * sizeof(float);
-}
+size_t rotate_bwd_bytes(int count, int64_t D) { return static_cast<size_t>(kRotBlocks) * count * D * sizeof(float); }
 hipError_t rotate_bwd(const RotArgs& a, float* part, hipStream_t st) { return launch(a, true, part, st); }
 
 }  // namespace sa

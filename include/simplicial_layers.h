@@ -96,6 +96,8 @@ int simplicial_norm_rotate_bwd(int32_t count, const void* const* x, const int64_
  *   q           [B, Nq, H, D], strides q_sb, q_sn, q_sh (batch, position, head)
  *   k, v        [B, Nk, Hkv, D], strides likewise
  *   out         [B, Nq, H, D] contiguous, dtype;  lse [B, H, Nq] float32
+ *   out_lo      as out, or NULL: what its rounding took, rounded likewise (out + out_lo
+ *               has twice the digits), for the backward. SA_DTYPE_BF16 only.
  *   slopes      [H] float32, documents [B, Nk] int32, prefix [B] int32, k_lens
  *               [B] int32, each contiguous or NULL
  *   workspace   simplicial_dot_attn_fwd_workspace_size() bytes (0: may be NULL):
@@ -106,8 +108,8 @@ int simplicial_norm_rotate_bwd(int32_t count, const void* const* x, const int64_
 size_t simplicial_dot_attn_fwd_workspace_size(int64_t B, int64_t Nq, int64_t Nk, int64_t H,
                                               int64_t Hkv, int64_t D, int32_t causal, int32_t window,
                                               int32_t has_documents, int32_t dtype);
-int simplicial_dot_attn_fwd(const void* q, const void* k, const void* v, void* out, float* lse,
-                            void* workspace, size_t workspace_bytes, int64_t B, int64_t Nq, int64_t Nk,
+int simplicial_dot_attn_fwd(const void* q, const void* k, const void* v, void* out, void* out_lo,
+                            float* lse, void* workspace, size_t workspace_bytes, int64_t B, int64_t Nq, int64_t Nk,
                             int64_t H, int64_t Hkv, int64_t D, int64_t q_sb, int64_t q_sn, int64_t q_sh,
                             int64_t k_sb, int64_t k_sn, int64_t k_sh, int64_t v_sb, int64_t v_sn,
                             int64_t v_sh, float scale, float softcap, int32_t causal, int32_t window,
@@ -121,7 +123,9 @@ int simplicial_dot_attn_fwd(const void* q, const void* k, const void* v, void* o
  *     dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO
  * dK and dV of a head shared by several query heads are sums over them in
  * float32, rounded once. The slopes get no gradient.
- *   out, lse, dout   of the forward, contiguous;  dq [B, Nq, H, D], dk and dv
+ *   out, lse, dout   of the forward, contiguous
+ *   out_lo           of the forward, or NULL: Delta of the rounded output, whose error (bf16
+ *                    2^-8 of |dO| |O|) all of a row's gradients share;  dq [B, Nq, H, D], dk and dv
  *                    [B, Nk, Hkv, D] contiguous, fully overwritten (rows that no
  *                    query sees with zeros)
  *   workspace        simplicial_dot_attn_bwd_workspace_size() bytes
@@ -130,7 +134,7 @@ size_t simplicial_dot_attn_bwd_workspace_size(int64_t B, int64_t Nq, int64_t Nk,
                                               int64_t Hkv, int64_t D, int32_t causal, int32_t window,
                                               int32_t has_documents, int32_t dtype);
 int simplicial_dot_attn_bwd(const void* q, const void* k, const void* v, const void* out,
-                            const void* dout, const float* lse, void* dq, void* dk, void* dv,
+                            const void* out_lo, const void* dout, const float* lse, void* dq, void* dk, void* dv,
                             void* workspace, size_t workspace_bytes, int64_t B, int64_t Nq, int64_t Nk,
                             int64_t H, int64_t Hkv, int64_t D, int64_t q_sb, int64_t q_sn, int64_t q_sh,
                             int64_t k_sb, int64_t k_sn, int64_t k_sh, int64_t v_sb, int64_t v_sn,

@@ -242,17 +242,13 @@ __global__ __launch_bounds__(kThreads* GROUPS, PRIV ? 1 : 2) void dot_dq_kernel(
   load_row<DP>(qf, q_row(a, w, b), w.valid, a.D, h);
   load_row<DP>(gf, static_cast<const uint16_t*>(a.dout) + orow, w.valid, a.D, h);
   float delta = 0.f;
-  {
+  for (int part = 0; part < (a.out_lo_in ? 2 : 1); ++part) {
     u32x4_t of[NT];
-    load_row<DP>(of, static_cast<const uint16_t*>(a.out_in) + orow, w.valid, a.D, h);
+    load_row<DP>(of, static_cast<const uint16_t*>(part ? a.out_lo_in : a.out_in) + orow, w.valid, a.D, h);
+    f32x16_t x = mfma32(of[0], gf[0], f32x16_t{});
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        delta += bf16_lo(gf[t][e]) * bf16_lo(of[t][e]);
-        delta += bf16_hi(gf[t][e]) * bf16_hi(of[t][e]);
-      }
-    delta += swap_halves(delta);
+    for (int t = 1; t < NT; ++t) x = mfma32(of[t], gf[t], x);
+    delta += diagonal(x, c, h);
   }
   const float lse = w.valid ? a.lse[(static_cast<int64_t>(b) * a.H + w.head) * a.Nq + w.i] : -kInf;
   const float lse2 = lse == -kInf ? kInf : lse * kLog2e;

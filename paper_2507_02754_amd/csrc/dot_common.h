@@ -232,6 +232,16 @@ __device__ __forceinline__ int div_group(int r, const DotArgs& a) {
   return a.G == 1 ? r : static_cast<int>(__umulhi(static_cast<unsigned>(r), a.magic) >> a.shift);
 }
 
+// Element (c, c) of an accumulator tile, in both of lane c's halves. Delta = <dO, O> is taken
+// from such a product, not from a sum of the lane's own: where a row sees one key alone, O is
+// V's row and Delta then dP to the bit, and its dS of 0 comes out as 0.
+__device__ __forceinline__ float diagonal(const f32x16_t& x, int c, int h) {
+  float y = 0.f;
+#pragma unroll
+  for (int v = 0; v < 16; ++v) y = acc_row(v, h) == c ? x[v] : y;
+  return y + swap_halves(y);
+}
+
 // Sum over the wavefront; every lane gets it.
 __device__ __forceinline__ float sum64(float x) {
   x = reduce32(x, [](float p, float q) { return p + q; });

@@ -389,11 +389,7 @@ __global__ __launch_bounds__(kThreads, 1) void dot_dq_f32_kernel(DotArgs a) {
     g.load(rows_of(static_cast<const T*>(a.dout) + at, a.Nq - row.i0, orow, orow), off, h);
     RowOp<T, D> o;
     o.load(rows_of(static_cast<const T*>(a.out_in) + at, a.Nq - row.i0, orow, orow), off, h);
-#pragma unroll
-    for (int t = 0; t < Geo<D>::NF; ++t)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) delta += g.f[t].x[e] * o.f[t].x[e];
-    delta += swap_halves(delta);
+    delta = diagonal(row_product(o, g), c, h);
   }
   const int64_t srow = row.valid ? (static_cast<int64_t>(b) * a.H + row.head) * a.Nq + row.i : 0;
   const float lse = row.valid ? a.lse[srow] : -kInf;

@@ -99,6 +99,14 @@ struct Row {
   }
 };
 
+// Columns `at` (if d0) and at + 64 (if d1) of O.
+__device__ __forceinline__ void write_out(const DotArgs& a, int64_t at, bool d0, float x0, bool d1, float x1) {
+  uint16_t *out = static_cast<uint16_t*>(a.out) + at, *lo = static_cast<uint16_t*>(a.out_lo) + at;
+  if (d0) out[0] = f32_to_bf16(x0);
+  if (d1) out[64] = f32_to_bf16(x1);
+  if (a.out_lo && d0) lo[0] = f32_to_bf16(rounded_off(x0));
+  if (a.out_lo && d1) lo[64] = f32_to_bf16(rounded_off(x1));
+}
 // O of one row by itself, over its visible keys (LSE is not touched by masked pairs), a
 // wavefront's 64 lanes along the columns: for rows whose products met an infinity or NaN.
 __device__ __forceinline__ void single_row(const DotArgs& a, const DotMask& m, int b, int i, int head, float lse) {
@@ -121,9 +129,7 @@ __device__ __forceinline__ void single_row(const DotArgs& a, const DotMask& m, i
     o1 += d1 ? w * bf16_to_f32(v[vj + 64]) : 0.f;
     if (__builtin_amdgcn_ballot_w64((d0 && o0 == o0) || (d1 && o1 == o1)) == 0) break;  // all NaN
   }
-  uint16_t* out = static_cast<uint16_t*>(a.out) + ((static_cast<int64_t>(b) * a.Nq + i) * a.H + head) * a.D + lane;
-  if (d0) out[0] = f32_to_bf16(o0);
-  if (d1) out[64] = f32_to_bf16(o1);
+  write_out(a, ((static_cast<int64_t>(b) * a.Nq + i) * a.H + head) * a.D + lane, d0, o0, d1, o1);
 }
 // The rows of `bad` (a bit for each of the wavefront's 32), one after another.
 __device__ __forceinline__ void single_rows(const DotArgs& a, const DotMask& m, int b, const Lanes& w, float lse, unsigned bad) {
@@ -313,8 +319,11 @@ __global__ __launch_bounds__(kThreads* GROUPS, 2) void dot_fwd_kernel(DotArgs a)
   const float check = not_finite(row.acc);
   const unsigned bad = has_mask(a) ? rows_where(w.valid && fabsf(row.l) < kInf && check != check) : 0;
   if (w.valid) {
-    if (!((bad >> c) & 1))
-      store_row<DP>(static_cast<uint16_t*>(a.out) + ((static_cast<int64_t>(b) * a.Nq + w.i) * a.H + w.head) * a.D + 4 * h, row.acc, inv, a.D);
+    if (!((bad >> c) & 1)) {
+      const int64_t o = ((static_cast<int64_t>(b) * a.Nq + w.i) * a.H + w.head) * a.D + 4 * h;
+      store_row<DP>(static_cast<uint16_t*>(a.out) + o, row.acc, inv, a.D);
+      if (a.out_lo) store_row_lo<DP>(static_cast<uint16_t*>(a.out_lo) + o, row.acc, inv, a.D);
+    }
     if (h == 0) a.lse[(static_cast<int64_t>(b) * a.H + w.head) * a.Nq + w.i] = lse;
   }
   single_rows(a, m, b, w, lse, bad);
@@ -443,7 +452,8 @@ __global__ __launch_bounds__(kThreads, 1) void dot_few_kernel(DotArgs a) {
   const float inv = a.nsplit > 1 ? 1.f : empty ? 0.f : 1.f / lr;
   const int64_t rr = static_cast<int64_t>(bh) * R + block * 32 + c;
   float* pr = a.part + (rr * a.nsplit + part) * a.D + 4 * h;
-  uint16_t* out = static_cast<uint16_t*>(a.out) + ((static_cast<int64_t>(b) * a.Nq + w.i) * a.H + w.head) * a.D + 4 * h;
+  const int64_t o = ((static_cast<int64_t>(b) * a.Nq + w.i) * a.H + w.head) * a.D + 4 * h;
+  uint16_t *out = static_cast<uint16_t*>(a.out) + o, *olo = static_cast<uint16_t*>(a.out_lo) + o;
   float check = 0.f;
   const float lse = empty ? -kInf : top * kLn2 + logf(l);
   // Each wavefront takes quad `wave` of every tile.
@@ -465,6 +475,9 @@ __global__ __launch_bounds__(kThreads, 1) void dot_few_kernel(DotArgs a) {
             u32x4_t{__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3])};
       else
         *reinterpret_cast<u32x2_t*>(out + 32 * dt + 8 * wave) = u32x2_t{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
+      if (a.nsplit == 1 && a.out_lo)
+        *reinterpret_cast<u32x2_t*>(olo + 32 * dt + 8 * wave) = u32x2_t{pack_bf16x2(rounded_off(y[0]), rounded_off(y[1])),
+                                                                        pack_bf16x2(rounded_off(y[2]), rounded_off(y[3]))};
     }
   }
   if (wave == 0 && h == 0 && w.valid) {
@@ -503,7 +516,6 @@ __global__ __launch_bounds__(kThreads) void dot_join_kernel(DotArgs a) {
     l += s < a.nsplit ? f * st[3 * s + 1] : 0.f;
     lr += s < a.nsplit ? f * st[3 * s + 2] : 0.f;
     const int n = min(a.nsplit - s0, 64);
-#pragma unroll 4
     for (int i = wave; i < n; i += kWaves) {
       const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), i));
       const float* p = rows + static_cast<int64_t>(s0 + i) * a.D;
@@ -529,9 +541,7 @@ __global__ __launch_bounds__(kThreads) void dot_join_kernel(DotArgs a) {
     return;
   }
   const float inv = l == 0.f ? 0.f : 1.f / lr;
-  uint16_t* out = static_cast<uint16_t*>(a.out) + ((static_cast<int64_t>(b) * a.Nq + i) * a.H + head) * a.D + lane;
-  if (d0) out[0] = f32_to_bf16(x0 * inv);
-  if (d1) out[64] = f32_to_bf16(x1 * inv);
+  write_out(a, ((static_cast<int64_t>(b) * a.Nq + i) * a.H + head) * a.D + lane, d0, x0 * inv, d1, x1 * inv);
 }
 
 template <int DP, bool CAP, bool BIAS>

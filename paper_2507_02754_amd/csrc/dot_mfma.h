@@ -87,6 +87,22 @@ __device__ __forceinline__ void store_row(uint16_t* p, const f32x16_t (&acc)[DP 
         *reinterpret_cast<u32x2_t*>(p + 32 * dt + 8 * q) =
             u32x2_t{pack_bf16x2(acc[dt][4 * q] * mul, acc[dt][4 * q + 1] * mul), pack_bf16x2(acc[dt][4 * q + 2] * mul, acc[dt][4 * q + 3] * mul)};
 }
+// What rounding to bf16 takes from x (not a number's: nothing).
+__device__ __forceinline__ float rounded_off(float x) {
+  const float d = x - bf16_to_f32(f32_to_bf16(x));
+  return d == d ? d : 0.f;
+}
+template <int DP>
+__device__ __forceinline__ void store_row_lo(uint16_t* p, const f32x16_t (&acc)[DP / 32], float mul, int D) {
+#pragma unroll
+  for (int dt = 0; dt < DP / 32; ++dt)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (32 * dt + 8 * q < D)
+        *reinterpret_cast<u32x2_t*>(p + 32 * dt + 8 * q) =
+            u32x2_t{pack_bf16x2(rounded_off(acc[dt][4 * q] * mul), rounded_off(acc[dt][4 * q + 1] * mul)),
+                    pack_bf16x2(rounded_off(acc[dt][4 * q + 2] * mul), rounded_off(acc[dt][4 * q + 3] * mul))};
+}
 // NaN if any of a lane's accumulators is an infinity or NaN, else 0.
 template <int NDT>
 __device__ __forceinline__ float not_finite(const f32x16_t (&acc)[NDT]) {

@@ -208,8 +208,8 @@ size_t simplicial_dot_attn_fwd_workspace_size(int64_t B, int64_t Nq, int64_t Nk,
   return sa::dot_fwd_plan(B, Nq, Nk, H, Hkv, D, causal, window, has_documents != 0, dtype).bytes;
 }
 
-int simplicial_dot_attn_fwd(const void* q, const void* k, const void* v, void* out, float* lse,
-                            void* workspace, size_t workspace_bytes, int64_t B, int64_t Nq, int64_t Nk,
+int simplicial_dot_attn_fwd(const void* q, const void* k, const void* v, void* out, void* out_lo,
+                            float* lse, void* workspace, size_t workspace_bytes, int64_t B, int64_t Nq, int64_t Nk,
                             int64_t H, int64_t Hkv, int64_t D, int64_t q_sb, int64_t q_sn, int64_t q_sh,
                             int64_t k_sb, int64_t k_sn, int64_t k_sh, int64_t v_sb, int64_t v_sn,
                             int64_t v_sh, float scale, float softcap, int32_t causal, int32_t window,
@@ -220,11 +220,12 @@ int simplicial_dot_attn_fwd(const void* q, const void* k, const void* v, void* o
   if (!good({q, k, v, out, lse})) return SA_ERR_INVALID;
   const int rc = check_dot_call(c);
   if (rc != SA_OK) return rc;
+  if (!aligned(out_lo, 16) || (out_lo && dtype != SA_DTYPE_BF16)) return SA_ERR_INVALID;
   const sa::DotPlan p = sa::dot_fwd_plan(B, Nq, Nk, H, Hkv, D, causal, window, documents != nullptr, dtype);
   if (p.bytes && !good({workspace})) return SA_ERR_INVALID;
   if (workspace_bytes < p.bytes) return SA_ERR_WORKSPACE;
   sa::DotArgs a = dot_args(c, q, k, v);
-  a.out = out, a.lse = lse;
+  a.out = out, a.out_lo = out_lo, a.lse = lse;
   char* ws = static_cast<char*>(workspace);
   hipStream_t st = static_cast<hipStream_t>(stream);
   a.nsplit = p.nsplit;
@@ -246,7 +247,7 @@ size_t simplicial_dot_attn_bwd_workspace_size(int64_t B, int64_t Nq, int64_t Nk,
 }
 
 int simplicial_dot_attn_bwd(const void* q, const void* k, const void* v, const void* out,
-                            const void* dout, const float* lse, void* dq, void* dk, void* dv,
+                            const void* out_lo, const void* dout, const float* lse, void* dq, void* dk, void* dv,
                             void* workspace, size_t workspace_bytes, int64_t B, int64_t Nq, int64_t Nk,
                             int64_t H, int64_t Hkv, int64_t D, int64_t q_sb, int64_t q_sn, int64_t q_sh,
                             int64_t k_sb, int64_t k_sn, int64_t k_sh, int64_t v_sb, int64_t v_sn,
@@ -258,10 +259,11 @@ int simplicial_dot_attn_bwd(const void* q, const void* k, const void* v, const v
   if (!good({q, k, v, out, dout, lse, dq, dk, dv, workspace})) return SA_ERR_INVALID;
   const int rc = check_dot_call(c);
   if (rc != SA_OK) return rc;
+  if (!aligned(out_lo, 16) || (out_lo && dtype != SA_DTYPE_BF16)) return SA_ERR_INVALID;
   const sa::DotPlan p = sa::dot_bwd_plan(B, Nq, Nk, H, Hkv, D, causal, window, documents != nullptr, dtype);
   if (workspace_bytes < p.bytes) return SA_ERR_WORKSPACE;
   sa::DotArgs a = dot_args(c, q, k, v);
-  a.out_in = out, a.dout = dout, a.lse = const_cast<float*>(lse);
+  a.out_in = out, a.out_lo_in = out_lo, a.dout = dout, a.lse = const_cast<float*>(lse);
   a.dq = dq, a.dk = dk, a.dv = dv;
   char* ws = static_cast<char*>(workspace);
   hipStream_t st = static_cast<hipStream_t>(stream);

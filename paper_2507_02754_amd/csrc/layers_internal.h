@@ -56,8 +56,8 @@ hipError_t logprobs_bwd(const LogprobGrad& a, hipStream_t st);
 // every position, r = G i + g: one position's heads share their keys.
 struct DotArgs {
   const void *q, *k, *v, *dout;
-  const void* out_in;  // backward: O
-  void* out;
+  const void *out_in, *out_lo_in;  // backward: O, and what its rounding took or null
+  void *out, *out_lo;
   float* lse;  // forward: written, backward: read
   void *dq, *dk, *dv;
   int64_t qsb, qsn, qsh, ksb, ksn, ksh, vsb, vsn, vsh;

@@ -9,8 +9,7 @@ import collections
 
 import torch
 
-from .layers_binding import (simplicial_dot_attn_bwd, simplicial_dot_attn_fwd, simplicial_logprobs_bwd,
-                             simplicial_logprobs_fwd, simplicial_norm_rotate_bwd, simplicial_norm_rotate_fwd)
+from .layers_binding import _DotCall, _RotateCall, simplicial_logprobs_bwd, simplicial_logprobs_fwd
 
 __all__ = ["norm_rotate", "dot_attention", "token_logprobs", "TokenLogprobs", "NormRotateFunction", "DotAttentionFunction",
            "TokenLogprobsFunction"]
@@ -18,9 +17,10 @@ __all__ = ["norm_rotate", "dot_attention", "token_logprobs", "TokenLogprobs", "N
 
 def _rows(t):
     """`t`, or a contiguous copy where its rows are not 16-byte aligned."""
+    if t.dim() != 4 or (t.is_contiguous() and t.data_ptr() % 16 == 0):
+        return t
     unit = 16 // t.element_size()
-    if t.dim() == 4 and (t.stride(3) != 1 or t.data_ptr() % 16 or
-                         any(s % unit for s, n in zip(t.stride()[:3], t.shape) if n > 1)):
+    if t.stride(3) != 1 or t.data_ptr() % 16 or any(s % unit for s, n in zip(t.stride()[:3], t.shape) if n > 1):
         return t.contiguous() if not t.is_contiguous() else t.clone()
     return t
 
@@ -35,26 +35,30 @@ class NormRotateFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, options, count, *tensors):
         xs, weights = [_rows(x) for x in tensors[:count]], tensors[count:] or None
-        ys = simplicial_norm_rotate_fwd(xs, weights, **options)
+        call = _RotateCall(xs, weights, *options)
         ctx.save_for_backward(*xs, *(weights or ()))
-        ctx.options, ctx.count = options, count
-        return tuple(ys)
+        # (the tensors stay with save_for_backward, which watches for changes in place)
+        call.kept = (None, weights and [None] * count, options[3])
+        ctx.call, ctx.count = call, count
+        return tuple(call.forward())
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, *dys):
-        tensors = ctx.saved_tensors
-        xs, weights = tensors[:ctx.count], tensors[ctx.count:] or None
-        dys = [torch.zeros(x.shape, dtype=x.dtype, device=x.device) if dy is None else _dense(dy, x.dtype)
-               for x, dy in zip(xs, dys)]
-        dxs, dws = simplicial_norm_rotate_bwd(xs, dys, weights, weight_grads=any(ctx.needs_input_grad[2 + ctx.count:]),
-                                              **ctx.options)
+        tensors, count, call = ctx.saved_tensors, ctx.count, ctx.call
+        weights = tensors[count:]
+        dys = [torch.zeros(s, dtype=call.dtype, device=call.device) if dy is None else _dense(dy, call.dtype)
+               for s, dy in zip(call.shapes, dys)]
+        call.kept = (tensors[:count], weights or None, call.kept[2])
+        dxs, dws = call.backward(dys, weight_grads=any(ctx.needs_input_grad[2 + count:]))
+        call.kept = (None, weights and [None] * count, call.kept[2])
         return (None, None, *dxs, *(dws if weights else ()))
 
 
 def _dense(g, dtype):
     """An upstream gradient as the kernels take it: contiguous and aligned, of the output's type."""
-    g = g.to(dtype).contiguous()
+    if g.dtype != dtype or not g.is_contiguous():
+        g = g.to(dtype).contiguous()
     return g if g.data_ptr() % 16 == 0 else g.clone()
 
 
@@ -65,13 +69,13 @@ def norm_rotate(xs, weights=None, eps=1e-6, freqs=None, layout="half", positions
     xs[t] is [B, N, heads_t, D]; arguments as simplicial_norm_rotate_fwd, whose results
     are returned as a tuple. eps = 0 without weights is the L2 norm scaled by sqrt(D). A
     weight is given for every tensor or for none."""
-    options = dict(eps=eps, freqs=freqs, layout=layout, positions=positions, start=start)
+    options = (eps, freqs, layout, positions, start)
     xs = list(xs)
     if weights is not None and any(w is None for w in weights):
         raise ValueError("a weight for every tensor, or weights=None")
     if _needs_grad(*xs, *(weights or ())):
         return NormRotateFunction.apply(options, len(xs), *xs, *(weights or ()))
-    return tuple(simplicial_norm_rotate_fwd([_rows(x) for x in xs], weights, **options))
+    return tuple(_RotateCall([_rows(x) for x in xs], weights, *options).forward())
 
 
 class DotAttentionFunction(torch.autograd.Function):
@@ -80,19 +84,24 @@ class DotAttentionFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, options):
         q, k, v = _rows(q), _rows(k), _rows(v)
-        out, lse = simplicial_dot_attn_fwd(q, k, v, **options)
-        ctx.save_for_backward(q, k, v, out, lse)
-        ctx.options = options
+        call = _DotCall(q, k, v, *options)
+        lo = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q.dtype == torch.bfloat16 else None
+        out, lse = call.forward(out_lo=lo)
+        ctx.save_for_backward(q, k, v, out, lse, *(() if lo is None else (lo,)))
+        call.q = call.k = call.v = None  # (they stay with save_for_backward, which watches for changes in place)
+        ctx.call = call
         ctx.mark_non_differentiable(lse)
         return out, lse
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dout, _dlse):
-        q, k, v, out, lse = ctx.saved_tensors
-        if dout is None:
-            dout = torch.zeros_like(out)
-        return (*simplicial_dot_attn_bwd(q, k, v, out, _dense(dout, out.dtype), lse, **ctx.options), None)
+        call = ctx.call
+        call.q, call.k, call.v, out, lse, *lo = ctx.saved_tensors
+        dout = torch.zeros_like(out) if dout is None else _dense(dout, out.dtype)
+        grads = call.backward(out, dout, lse, *lo)
+        call.q = call.k = call.v = None
+        return (*grads, None)
 
 
 def dot_attention(q, k, v, scale=None, causal=True, window=0, softcap=0.0, slopes=None, documents=None, prefix=None,
@@ -102,13 +111,12 @@ def dot_attention(q, k, v, scale=None, causal=True, window=0, softcap=0.0, slope
     Arguments as simplicial_dot_attn_fwd: q [B, Nq, H, D], k and v [B, Nk, Hkv, D], the
     queries the last Nq of the keys' positions; score cap, distance bias, and causal,
     window, prefix and document masks. The options are not differentiated."""
-    options = dict(scale=scale, causal=causal, window=window, softcap=softcap, slopes=slopes, documents=documents,
-                   prefix=prefix, k_lens=k_lens)
+    options = (scale, causal, window, softcap, slopes, documents, prefix, k_lens)
     if slopes is not None and slopes.requires_grad:
         raise ValueError("the slopes of the distance bias get no gradient")
     if _needs_grad(q, k, v):
         return DotAttentionFunction.apply(q, k, v, options)[0]
-    return simplicial_dot_attn_fwd(_rows(q), _rows(k), _rows(v), **options)[0]
+    return _DotCall(_rows(q), _rows(k), _rows(v), *options).forward()[0]
 
 
 TokenLogprobs = collections.namedtuple("TokenLogprobs", "logprob entropy lse top_logprobs top_tokens")

@@ -44,8 +44,8 @@ def _library():
                                                                   vp, i32, i32, i32, vp]
     lib.simplicial_norm_rotate_bwd_workspace_size.argtypes = [i32, i64, i64, i64]
     dot = [i64] * 15 + [f32, f32, i32, i32] + [vp] * 4 + [i32, vp]
-    lib.simplicial_dot_attn_fwd.argtypes = [vp] * 6 + [size] + dot
-    lib.simplicial_dot_attn_bwd.argtypes = [vp] * 10 + [size] + dot
+    lib.simplicial_dot_attn_fwd.argtypes = [vp] * 7 + [size] + dot
+    lib.simplicial_dot_attn_bwd.argtypes = [vp] * 11 + [size] + dot
     lib.simplicial_logprobs_fwd.argtypes = [vp] * 8 + [size, i64, i64, i64, i32, i32, vp]
     lib.simplicial_logprobs_bwd.argtypes = [vp] * 8 + [i64, i64, i64, i32, vp]
     for name in ("norm_rotate_fwd", "norm_rotate_bwd", "dot_attn_fwd", "dot_attn_bwd", "logprobs_fwd", "logprobs_bwd"):
@@ -123,52 +123,100 @@ def _freq_array(freqs):
     return (ctypes.c_double * max(len(freqs), 1))(*freqs)
 
 
-def _rotate_args(xs, weights, eps, freqs, layout, positions, start):
-    """Checked arguments shared by forward and backward: (count, strides, weights, heads, middle, tail, wdtype)."""
-    n = len(xs)
-    if not 1 <= n <= ROTATE_MAX:
-        raise ValueError(f"1 to {ROTATE_MAX} tensors, got {n}")
-    x0 = xs[0]
-    for t, x in enumerate(xs):
-        _check_view(x, f"x[{t}]", x0)
-        if x.shape[:2] != x0.shape[:2] or x.shape[3] != x0.shape[3]:
-            raise ValueError(f"x[{t}] has shape {tuple(x.shape)}, expected [B, N, heads, D] of {tuple(x0.shape)}")
-    B, N, _, D = x0.shape
-    if layout not in ROTATE_LAYOUTS:
-        raise ValueError(f"layout {layout!r}; expected one of {', '.join(ROTATE_LAYOUTS)}")
-    wdtype = torch.float32
-    if weights is not None:
-        if len(weights) != n:
-            raise ValueError(f"{len(weights)} weights for {n} tensors")
-        given = [w for w in weights if w is not None]
-        if given and eps is None:
-            raise ValueError("weights need a norm (eps is None)")
-        for w in given:
-            if w.dtype not in _DTYPES:
-                raise ValueError(f"unsupported weight dtype {w.dtype}; expected float32 or bfloat16")
-            _check_like(w, (D,), given[0].dtype, x0.device, "a weight")
-        wdtype = given[0].dtype if given else wdtype
-    pos_stride = 0
-    if positions is not None:
-        if positions.dtype != torch.int64 or positions.device != x0.device or positions.shape not in ((N,), (B, N)):
-            raise ValueError(f"positions must be int64 of shape [{N}] or [{B}, {N}] on {x0.device}, got "
-                             f"{positions.dtype} {tuple(positions.shape)} on {positions.device}")
-        if N > 1 and positions.stride(-1) != 1:
-            raise ValueError("positions must be contiguous in their last dimension")
-        if positions.dim() == 2 and B > 1:
-            pos_stride = positions.stride(0)
-    freqs = tuple(freqs) if freqs is not None else ()
-    norm = eps is not None
-    heads = (ctypes.c_int32 * n)(*(x.shape[2] for x in xs))
-    strides = (ctypes.c_int64 * (3 * n))(*(s for x in xs for s in _strides(x)))
-    w = None if weights is None else _pointers(weights)
-    tail = (B, N, D, norm, float(eps) if norm else 0.0, ROTATE_LAYOUTS[layout], _freq_array(freqs), len(freqs),
-            _DTYPES[x0.dtype], _DTYPES[wdtype])
-    return n, strides, w, heads, (_ptr(positions), pos_stride, int(start)), tail, wdtype
+class _RotateCall:
+    """Checked arguments of a norm and rotation, in the form the library takes: the same
+    for the forward and its backward."""
+
+    __slots__ = ("n", "shapes", "dtype", "device", "strides", "xs", "weights", "heads", "pos", "tail", "kept")
+
+    def __init__(self, xs, weights, eps, freqs, layout, positions, start):
+        n = len(xs)
+        if not 1 <= n <= ROTATE_MAX:
+            raise ValueError(f"1 to {ROTATE_MAX} tensors, got {n}")
+        x0 = xs[0]
+        for t, x in enumerate(xs):
+            _check_view(x, "x", x0)
+        B, N, _, D = x0.shape
+        shapes = [x.shape for x in xs]
+        for t, s in enumerate(shapes):
+            if s[0] != B or s[1] != N or s[3] != D:
+                raise ValueError(f"x[{t}] has shape {tuple(s)}, expected [B, N, heads, D] of {tuple(x0.shape)}")
+        code = ROTATE_LAYOUTS.get(layout)
+        if code is None:
+            raise ValueError(f"layout {layout!r}; expected one of {', '.join(ROTATE_LAYOUTS)}")
+        device = x0.device
+        wdtype = torch.float32
+        if weights is not None:
+            if len(weights) != n:
+                raise ValueError(f"{len(weights)} weights for {n} tensors")
+            given = [w for w in weights if w is not None]
+            if given:
+                wdtype = given[0].dtype
+                if eps is None:
+                    raise ValueError("weights need a norm (eps is None)")
+                if wdtype not in _DTYPES:
+                    raise ValueError(f"unsupported weight dtype {wdtype}; expected float32 or bfloat16")
+            for w in given:
+                _check_like(w, (D,), wdtype, device, "a weight")
+        pos, pos_stride = None, 0
+        if positions is not None:
+            if positions.dtype != torch.int64 or positions.device != device or positions.shape not in ((N,), (B, N)):
+                raise ValueError(f"positions must be int64 of shape [{N}] or [{B}, {N}] on {device}, got "
+                                 f"{positions.dtype} {tuple(positions.shape)} on {positions.device}")
+            if N > 1 and positions.stride(-1) != 1:
+                raise ValueError("positions must be contiguous in their last dimension")
+            if positions.dim() == 2 and B > 1:
+                pos_stride = positions.stride(0)
+            pos = positions.data_ptr()
+        freqs = tuple(freqs) if freqs is not None else ()
+        self.n, self.shapes, self.dtype, self.device = n, shapes, x0.dtype, device
+        self.heads = (ctypes.c_int32 * n)(*[s[2] for s in shapes])
+        self.strides = (ctypes.c_int64 * (3 * n))(*[s for x in xs for s in _strides(x)])
+        self.xs = _pointers(xs)
+        self.weights = None if weights is None else _pointers(weights)
+        self.pos = (pos, pos_stride, int(start))
+        self.tail = (B, N, D, eps is not None, float(eps or 0.0), code, _freq_array(freqs), len(freqs), _DTYPES[x0.dtype],
+                     _DTYPES[wdtype])
+        self.kept = (xs, weights, positions)  # what the pointers point to
+
+    def forward(self, out=None):
+        if out is None:
+            out = [torch.empty(s, dtype=self.dtype, device=self.device) for s in self.shapes]
+        else:
+            for s, y in zip(self.shapes, out, strict=True):
+                _check_like(y, s, self.dtype, self.device, "an output")
+        _call("simplicial_norm_rotate_fwd", self.device, self.n, self.xs, self.strides, self.weights, _pointers(out),
+              self.heads, *self.pos, *self.tail)
+        return list(out)
+
+    def backward(self, dys, weight_grads=True, grads=None):
+        n, device = self.n, self.device
+        if len(dys) != n:
+            raise ValueError(f"{len(dys)} gradients for {n} tensors")
+        for s, dy in zip(self.shapes, dys):
+            _check_like(dy, s, self.dtype, device, "an output's gradient")
+        if grads is None:
+            grads = [torch.empty(s, dtype=self.dtype, device=device) for s in self.shapes]
+        else:
+            for s, dx in zip(self.shapes, grads, strict=True):
+                _check_like(dx, s, self.dtype, device, "an input's gradient")
+        dws, dw, workspace, nbytes = [None] * n, None, None, 0
+        if weight_grads and self.weights is not None:
+            dws = [None if t is None else torch.empty_like(t) for t in self.kept[1]]
+            dw = _pointers(dws)
+            B, N, D = self.tail[:3]
+            nbytes = (_lib or _library()).simplicial_norm_rotate_bwd_workspace_size(n, B, N, D)
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        _call("simplicial_norm_rotate_bwd", device, n, self.xs, self.strides, self.weights, _pointers(dys), _pointers(grads),
+              dw, self.heads, *self.pos, _ptr(workspace), nbytes, *self.tail)
+        return list(grads), dws
 
 
 def _pointers(tensors):
-    return (ctypes.c_void_p * len(tensors))(*(_ptr(t) for t in tensors))
+    return _POINTERS[len(tensors)](*[None if t is None else t.data_ptr() for t in tensors])
+
+
+_POINTERS = {n: ctypes.c_void_p * n for n in range(1, ROTATE_MAX + 1)}
 
 
 def simplicial_norm_rotate_fwd(xs, weights=None, eps=1e-6, freqs=None, layout="half", positions=None, start=0, out=None):
@@ -180,43 +228,14 @@ def simplicial_norm_rotate_fwd(xs, weights=None, eps=1e-6, freqs=None, layout="h
     position of the pairs that `layout` names: "half" (i, n + i), "pairs" (2 i, 2 i + 1)
     or "axis" (3 i, 3 i + 1: the first two of each 3-component chunk of the determinant
     logits); None: no rotation. Positions: int64 [N] or [B, N], or start, start + 1, ..."""
-    n, strides, w, heads, pos, tail, _ = _rotate_args(xs, weights, eps, freqs, layout, positions, start)
-    device = xs[0].device
-    if out is None:
-        out = [torch.empty(x.shape, dtype=x.dtype, device=device) for x in xs]
-    else:
-        for x, y in zip(xs, out, strict=True):
-            _check_like(y, x.shape, x.dtype, device, "an output")
-    _call("simplicial_norm_rotate_fwd", device, n, _pointers(xs), strides, w, _pointers(out), heads, *pos, *tail)
-    return list(out)
+    return _RotateCall(xs, weights, eps, freqs, layout, positions, start).forward(out)
 
 
 def simplicial_norm_rotate_bwd(xs, dys, weights=None, eps=1e-6, freqs=None, layout="half", positions=None, start=0,
                                weight_grads=True, grads=None):
     """(dxs, dweights) of simplicial_norm_rotate_fwd: lists, the latter with None where
     there is no weight, or all None with weight_grads False."""
-    n, strides, w, heads, pos, tail, wdtype = _rotate_args(xs, weights, eps, freqs, layout, positions, start)
-    device = xs[0].device
-    if len(dys) != n:
-        raise ValueError(f"{len(dys)} gradients for {n} tensors")
-    for x, dy in zip(xs, dys):
-        _check_like(dy, x.shape, x.dtype, device, "an output's gradient")
-    if grads is None:
-        grads = [torch.empty(x.shape, dtype=x.dtype, device=device) for x in xs]
-    else:
-        for x, dx in zip(xs, grads, strict=True):
-            _check_like(dx, x.shape, x.dtype, device, "an input's gradient")
-    dws = [None] * n
-    if weight_grads and weights is not None:
-        dws = [None if t is None else torch.empty_like(t) for t in weights]
-    workspace, nbytes = None, 0
-    if any(t is not None for t in dws):
-        B, N, D = tail[:3]
-        nbytes = (_lib or _library()).simplicial_norm_rotate_bwd_workspace_size(n, B, N, D)
-        workspace = _workspace(nbytes, device)
-    _call("simplicial_norm_rotate_bwd", device, n, _pointers(xs), strides, w, _pointers(dys), _pointers(grads),
-          _pointers(dws), heads, *pos, _ptr(workspace), nbytes, *tail)
-    return list(grads), dws
+    return _RotateCall(xs, weights, eps, freqs, layout, positions, start).backward(dys, weight_grads, grads)
 
 
 # ---- dot-product attention ----
@@ -234,37 +253,82 @@ def simplicial_dot_attn_bwd_workspace_size(B, Nq, Nk, H, Hkv, D, causal, window,
                                                                  bool(has_documents), int(dt)))
 
 
-def _dot_args(q, k, v, scale, causal, window, softcap, slopes, documents, prefix, k_lens):
-    _check_view(q, "q")
-    _check_view(k, "k", q)
-    _check_view(v, "v", q)
-    B, Nq, H, D = q.shape
-    Nk, Hkv = k.shape[1], k.shape[2]
-    if k.shape != v.shape or k.shape[0] != B or k.shape[3] != D:
-        raise ValueError(f"k and v must be [{B}, Nk, Hkv, {D}], got {tuple(k.shape)} and {tuple(v.shape)}")
-    if H % Hkv:
-        raise ValueError(f"{H} query heads are no multiple of {Hkv} heads of k and v")
-    if Nq > Nk:
-        raise ValueError(f"{Nq} queries of {Nk} keys: the queries are the last of the keys' positions")
-    device = q.device
-    if slopes is not None:
-        _check_like(slopes, (H,), torch.float32, device, "slopes")
-    if documents is not None:
-        _check_like(documents, (B, Nk), torch.int32, device, "documents")
-    if prefix is not None:
-        _check_like(prefix, (B,), torch.int32, device, "prefix")
-    if k_lens is not None:
-        _check_like(k_lens, (B,), torch.int32, device, "k_lens")
-    dt = _DTYPES[q.dtype]
-    sizes = (B, Nq, Nk, H, Hkv, D)
-    plan = (*sizes, bool(causal), int(window), documents is not None, dt)
-    args = (*sizes, *_strides(q), *_strides(k), *_strides(v), D ** -0.5 if scale is None else float(scale), float(softcap),
-            bool(causal), int(window), _ptr(slopes), _ptr(documents), _ptr(prefix), _ptr(k_lens), dt)
-    return sizes, plan, args
+class _DotCall:
+    """Checked arguments of a dot-product attention, in the form the library takes: the same
+    for the forward and its backward."""
+
+    __slots__ = ("q", "k", "v", "plan", "args", "kept")
+
+    def __init__(self, q, k, v, scale, causal, window, softcap, slopes, documents, prefix, k_lens):
+        _check_view(q, "q", q)
+        _check_view(k, "k", q)
+        _check_view(v, "v", q)
+        B, Nq, H, D = q.shape
+        kshape = k.shape
+        Nk, Hkv = kshape[1], kshape[2]
+        if kshape != v.shape or kshape[0] != B or kshape[3] != D:
+            raise ValueError(f"k and v must be [{B}, Nk, Hkv, {D}], got {tuple(kshape)} and {tuple(v.shape)}")
+        if H % Hkv:
+            raise ValueError(f"{H} query heads are no multiple of {Hkv} heads of k and v")
+        if Nq > Nk:
+            raise ValueError(f"{Nq} queries of {Nk} keys: the queries are the last of the keys' positions")
+        device = q.device
+        if slopes is not None:
+            _check_like(slopes, (H,), torch.float32, device, "slopes")
+        if documents is not None:
+            _check_like(documents, (B, Nk), torch.int32, device, "documents")
+        if prefix is not None:
+            _check_like(prefix, (B,), torch.int32, device, "prefix")
+        if k_lens is not None:
+            _check_like(k_lens, (B,), torch.int32, device, "k_lens")
+        causal, window, dt = bool(causal), int(window), _DTYPES[q.dtype]
+        self.q, self.k, self.v = q, k, v
+        self.plan = (B, Nq, Nk, H, Hkv, D, causal, window, documents is not None, dt)
+        self.args = (B, Nq, Nk, H, Hkv, D, *_strides(q), *_strides(k), *_strides(v), D ** -0.5 if scale is None else float(scale),
+                     float(softcap), causal, window, _ptr(slopes), _ptr(documents), _ptr(prefix), _ptr(k_lens), dt)
+        self.kept = (slopes, documents, prefix, k_lens)  # what the pointers point to
+
+    def forward(self, out=None, lse=None, out_lo=None):
+        q = self.q
+        device, (B, Nq, _, H) = q.device, self.plan[:4]
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=device)
+        else:
+            _check_like(out, q.shape, q.dtype, device, "out")
+        if lse is None:
+            lse = torch.empty((B, H, Nq), dtype=torch.float32, device=device)
+        else:
+            _check_like(lse, (B, H, Nq), torch.float32, device, "lse")
+        if out_lo is not None:
+            _check_like(out_lo, q.shape, torch.bfloat16, device, "out_lo")
+        nbytes = (_lib or _library()).simplicial_dot_attn_fwd_workspace_size(*self.plan)
+        workspace = _workspace(nbytes, device)
+        _call("simplicial_dot_attn_fwd", device, q.data_ptr(), self.k.data_ptr(), self.v.data_ptr(), out.data_ptr(),
+              _ptr(out_lo), lse.data_ptr(), _ptr(workspace), nbytes, *self.args)
+        return out, lse
+
+    def backward(self, out, dout, lse, out_lo=None, grads=None):
+        q = self.q
+        device, (B, Nq, _, H) = q.device, self.plan[:4]
+        _check_like(out, q.shape, q.dtype, device, "out")
+        _check_like(dout, q.shape, q.dtype, device, "dout")
+        _check_like(lse, (B, H, Nq), torch.float32, device, "lse")
+        if out_lo is not None:
+            _check_like(out_lo, q.shape, torch.bfloat16, device, "out_lo")
+        if grads is None:
+            grads = tuple([torch.empty(t.shape, dtype=t.dtype, device=device) for t in (q, self.k, self.v)])
+        else:
+            for t, g, name in zip((q, self.k, self.v), grads, ("dq", "dk", "dv"), strict=True):
+                _check_like(g, t.shape, t.dtype, device, name)
+        nbytes = (_lib or _library()).simplicial_dot_attn_bwd_workspace_size(*self.plan)
+        workspace = _workspace(nbytes, device)
+        _call("simplicial_dot_attn_bwd", device, q.data_ptr(), self.k.data_ptr(), self.v.data_ptr(), out.data_ptr(),
+              _ptr(out_lo), dout.data_ptr(), lse.data_ptr(), *[g.data_ptr() for g in grads], _ptr(workspace), nbytes, *self.args)
+        return grads
 
 
 def simplicial_dot_attn_fwd(q, k, v, scale=None, causal=True, window=0, softcap=0.0, slopes=None, documents=None, prefix=None,
-                            k_lens=None, out=None, lse=None):
+                            k_lens=None, out=None, lse=None, out_lo=None):
     """(O, LSE) of dot-product attention: q [B, Nq, H, D], k and v [B, Nk, Hkv, D] (H a
     multiple of Hkv), the queries the last Nq of the sequence's positions; LSE is
     [B, H, Nq] float32. Views with 16-byte aligned rows will do.
@@ -274,43 +338,19 @@ def simplicial_dot_attn_fwd(q, k, v, scale=None, causal=True, window=0, softcap=
     (causal) with |p - j| < window (window > 0), and those before prefix[b] ([B] int32); with
     `documents` ([B, Nk] int32, negative: padding) of its own document alone. k_lens [B]
     int32: filled lengths of a cache, its last Nq positions the queries. A query that sees
-    no key gives O = 0 and LSE = -inf."""
-    (B, Nq, _, H, _, _), plan, args = _dot_args(q, k, v, scale, causal, window, softcap, slopes, documents, prefix, k_lens)
-    device = q.device
-    if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=device)
-    else:
-        _check_like(out, q.shape, q.dtype, device, "out")
-    if lse is None:
-        lse = torch.empty((B, H, Nq), dtype=torch.float32, device=device)
-    else:
-        _check_like(lse, (B, H, Nq), torch.float32, device, "lse")
-    nbytes = (_lib or _library()).simplicial_dot_attn_fwd_workspace_size(*plan)
-    workspace = _workspace(nbytes, device)
-    _call("simplicial_dot_attn_fwd", device, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(),
-          _ptr(workspace), nbytes, *args)
-    return out, lse
+    no key gives O = 0 and LSE = -inf. `out_lo` (bfloat16 as O): takes what rounding O to
+    bfloat16 took from it, for the backward."""
+    call = _DotCall(q, k, v, scale, causal, window, softcap, slopes, documents, prefix, k_lens)
+    return call.forward(out, lse, out_lo)
 
 
 def simplicial_dot_attn_bwd(q, k, v, out, dout, lse, scale=None, causal=True, window=0, softcap=0.0, slopes=None,
-                            documents=None, prefix=None, k_lens=None, grads=None):
-    """(dQ, dK, dV) of simplicial_dot_attn_fwd with the same options; `out` and `lse` are
-    its results. The slopes get no gradient."""
-    (B, Nq, _, H, _, _), plan, args = _dot_args(q, k, v, scale, causal, window, softcap, slopes, documents, prefix, k_lens)
-    device = q.device
-    _check_like(out, q.shape, q.dtype, device, "out")
-    _check_like(dout, q.shape, q.dtype, device, "dout")
-    _check_like(lse, (B, H, Nq), torch.float32, device, "lse")
-    if grads is None:
-        grads = tuple(torch.empty(t.shape, dtype=t.dtype, device=device) for t in (q, k, v))
-    else:
-        for t, g, name in zip((q, k, v), grads, ("dq", "dk", "dv"), strict=True):
-            _check_like(g, t.shape, t.dtype, device, name)
-    nbytes = (_lib or _library()).simplicial_dot_attn_bwd_workspace_size(*plan)
-    workspace = _workspace(nbytes, device)
-    _call("simplicial_dot_attn_bwd", device, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), dout.data_ptr(),
-          lse.data_ptr(), *(g.data_ptr() for g in grads), _ptr(workspace), nbytes, *args)
-    return grads
+                            documents=None, prefix=None, k_lens=None, grads=None, out_lo=None):
+    """(dQ, dK, dV) of simplicial_dot_attn_fwd with the same options; `out`, `lse` and
+    (where it was asked for: without it the gradients have the rounding of O in them)
+    `out_lo` are its results. The slopes get no gradient."""
+    call = _DotCall(q, k, v, scale, causal, window, softcap, slopes, documents, prefix, k_lens)
+    return call.backward(out, dout, lse, out_lo, grads)
 
 
 # ---- log probabilities ----

@@ -34,10 +34,11 @@ def _slopes(H):
 
 
 def _check(q, k, v, dout, label, **opts):
-    out, lse = simplicial_dot_attn_fwd(q, k, v, **opts)
+    lo = torch.empty_like(q, memory_format=torch.contiguous_format) if q.dtype == BF and dout is not None else None
+    out, lse = simplicial_dot_attn_fwd(q, k, v, out_lo=lo, **opts)
     got = {"out": out, "lse": lse}
     if dout is not None:
-        got.update(zip(("dq", "dk", "dv"), simplicial_dot_attn_bwd(q, k, v, out, dout, lse, **opts)))
+        got.update(zip(("dq", "dk", "dv"), simplicial_dot_attn_bwd(q, k, v, out, dout, lse, out_lo=lo, **opts)))
     torch.cuda.synchronize()
     want = ref.dot_attention(q, k, v, dout=dout, **opts)
     for name, w in want.items():
@@ -260,6 +261,21 @@ def test_one_head_for_all_by_stride():
 
 
 @pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("D", [16, 64, 128])
+def test_one_key_alone_has_no_gradient_of_scores(dt, D):
+    """Rows that see one key (a first token, a window of one): O is its value, dq and dk are 0."""
+    for N, H, Hkv, B in ((1, 4, 2, 3), (70, 4, 4, 1), (390, 64, 64, 4)):
+        q, k, v, dout = _inputs(B, N, N, H, Hkv, D, dt, seed=N)
+        leaves = [t.clone().requires_grad_(True) for t in (q, k, v)]
+        out = dot_attention(*leaves, window=1)
+        dq, dk, dv = torch.autograd.grad(out, leaves, dout)
+        assert torch.equal(out, v.repeat_interleave(H // Hkv, 2))
+        assert (dq == 0).all() and (dk == 0).all()
+        want = dout.double().view(B, N, Hkv, H // Hkv, D).sum(3)
+        ref.close(dv, want, 2 * ref.HALF[dt] * dout.double().abs().view(B, N, Hkv, H // Hkv, D).sum(3) + 1e-30, "dv")
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
 def test_large_scores(dt):
     """Scores of hundreds (one key takes all weight), a zero scale and a negative one."""
     q, k, v, dout = _inputs(1, 140, 140, 2, 2, 64, dt, seed=6, scale=8.0)
@@ -290,9 +306,32 @@ def test_autograd_equals_the_direct_calls():
     leaves = [t.clone().requires_grad_(True) for t in (q, k, v)]
     out = dot_attention(*leaves, softcap=9.0, window=30)
     grads = torch.autograd.grad(out, leaves, dout.float().to(BF).transpose(1, 2).contiguous().transpose(1, 2))
-    o, lse = simplicial_dot_attn_fwd(q, k, v, softcap=9.0, window=30)
-    want = simplicial_dot_attn_bwd(q, k, v, o, dout, lse, softcap=9.0, window=30)
+    lo = torch.empty_like(q)
+    o, lse = simplicial_dot_attn_fwd(q, k, v, softcap=9.0, window=30, out_lo=lo)
+    want = simplicial_dot_attn_bwd(q, k, v, o, dout, lse, softcap=9.0, window=30, out_lo=lo)
     assert torch.equal(out, o) and all(torch.equal(a, b) for a, b in zip(grads, want))
+
+
+@pytest.mark.parametrize("size", [(1, 50, 4, 2, 128), (1, 300, 8, 8, 64), (2, 450, 40, 20, 128), (4, 390, 64, 64, 128)], ids=str)
+def test_what_rounding_took(size):
+    """O + out_lo is O to twice the digits, in every form of the forward and over a split key
+    axis, and the gradients without it are within the rounding of O."""
+    B, N, H, Hkv, D = size
+    q, k, v, dout = _inputs(B, N, N, H, Hkv, D, BF, seed=13)
+    lo = torch.empty_like(q)
+    out, lse = simplicial_dot_attn_fwd(q, k, v, out_lo=lo)
+    exact, bound = ref.dot_attention(q, k, v)["out"]
+    both = out.double() + lo.double()
+    assert ((both - exact).abs() <= bound - 2.0 ** -8 * exact.abs() + 2.0 ** -15 * exact.abs()).all()
+    assert (lo.double().abs() <= 2.0 ** -8 * both.abs() * 1.01 + 1e-30).all()
+    grads = simplicial_dot_attn_bwd(q, k, v, out, dout, lse)
+    for name, x in zip(("dq", "dk", "dv"), grads):
+        ref.close(x, *ref.dot_attention(q, k, v, dout=dout)[name], name)
+    one = q[:, -1:].contiguous()
+    lo1 = torch.empty_like(one)
+    out1, _ = simplicial_dot_attn_fwd(one, k, v, out_lo=lo1)
+    both1 = out1.double() + lo1.double()
+    assert ((both1 - exact[:, -1:]).abs() <= bound[:, -1:] - 2.0 ** -8 * exact[:, -1:].abs() + 2.0 ** -15 * exact[:, -1:].abs()).all()
 
 
 def test_gradients_against_differences():

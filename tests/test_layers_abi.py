@@ -77,7 +77,7 @@ def test_norm_rotate_refusals(lib, backward):
 
 def _dot(lib, backward=False, ptrs=None, ws=A, ws_bytes=1 << 40, B=2, Nq=8, Nk=16, H=4, Hkv=2, D=64, q=None, k=None, scale=0.1,
          cap=0.0, causal=1, window=0, opts=(0, 0, 0, 0), dtype=1):
-    n = 9 if backward else 5
+    n = 10 if backward else 6
     q, k = q or (Nq * H * D, H * D, D), k or (Nk * Hkv * D, Hkv * D, D)
     tail = (B, Nq, Nk, H, Hkv, D, *q, *k, *k, scale, cap, causal, window, *opts, dtype, None)
     f = lib.simplicial_dot_attn_bwd if backward else lib.simplicial_dot_attn_fwd
@@ -89,10 +89,12 @@ def _dot(lib, backward=False, ptrs=None, ws=A, ws_bytes=1 << 40, B=2, Nq=8, Nk=1
 def test_dot_attention_refusals(lib, backward):
     def rc(**kw):
         return _dot(lib, backward, **kw)
-    n = 9 if backward else 5
+    n = 10 if backward else 6
     for i in range(n):
         for bad in (0, ODD):
-            assert rc(ptrs=[A] * i + [bad] + [A] * (n - i - 1)) == 1, i
+            if i != 4 or bad:  # (out_lo may be null)
+                assert rc(ptrs=[A] * i + [bad] + [A] * (n - i - 1)) == 1, i
+    assert rc(dtype=0) == 1  # out_lo is of bf16 results
     for bad in (dict(B=0), dict(Nq=0), dict(Nk=0), dict(H=0), dict(Hkv=0), dict(D=-64), dict(Nq=17), dict(H=4, Hkv=3),
                 dict(H=2, Hkv=4), dict(window=-1), dict(scale=float("nan")), dict(cap=-1.0), dict(cap=float("inf")),
                 dict(q=(2048, 256, 12)), dict(k=(-8, 128, 64)), dict(opts=(A + 2, 0, 0, 0)), dict(opts=(0, A + 1, 0, 0)),

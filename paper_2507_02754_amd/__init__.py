@@ -6,11 +6,15 @@ seeded synthetic workloads used by the tests and the benchmark, and a
 torch.autograd wrapper (`simplicial_attention`) over the forward and backward
 entry points, and the surrounding layer (`SimplicialAttention`: the K, K', V,
 V' projections of Section 4 around the kernels) with a small stack that
-interleaves it with dot-product attention (`InterleavedStack`).
+interleaves it with dot-product attention (`InterleavedStack`). Around it, from
+the same library (include/simplicial_layers.h): the norm and position rotation
+of queries and keys (`norm_rotate`), dot-product attention with capped scores,
+distance bias and masks (`dot_attention`), and log probabilities of tokens
+(`token_logprobs`).
 """
 
 from .autograd import SimplicialAttnFunction, simplicial_attention  # noqa: F401
-from .layer import InterleavedStack, SimplicialAttention  # noqa: F401
+from .layer import DotProductAttention, InterleavedStack, SimplicialAttention  # noqa: F401
 from .layers_autograd import TokenLogprobs, dot_attention, norm_rotate, token_logprobs  # noqa: F401
 from .layers_binding import (  # noqa: F401
     rotary_freqs,

@@ -5,7 +5,7 @@
 //     dA = P (dO v - Delta);  dS = dA (1 - tanh^2);  dq = scale dS k, ...
 //
 // A workgroup owns 32 rows (forward, dq) or 32 keys (dk, dv) of one K-side head; its
-// 4 wavefronts take every fourth block of 32 keys (rows) that holds a visible pair
+// wavefronts (4 or 8) take every 4th or 8th block of 32 keys (rows) that holds a visible pair
 // and add their sums at the end in a fixed order. A block's products S^T = K Q^T put
 // one row in each lane, so the softmax statistics are the lane's own and the
 // probabilities go into the next product's operand as they are. Matrix operands come
@@ -29,8 +29,10 @@
 namespace sa {
 namespace {
 
-constexpr int kWaves = 4;
-constexpr int kThreads = 64 * kWaves;
+// Wavefronts of a backward workgroup: two for each SIMD where their registers allow it
+// (one takes the other's load latency).
+template <int D>
+constexpr int kWavesOf = D <= 64 ? 8 : 4;
 constexpr int kFar = 0x7fffffff;  // an offset past every buffer's end
 
 __device__ __forceinline__ f32x16_t mfma_f32(float a, float b, f32x16_t c) {
@@ -106,23 +108,35 @@ __device__ __forceinline__ f32x16_t row_product(const RowOp<T, D>& a, const RowO
   return x;
 }
 
-// Sum of the tile's columns over the block's 32 rows x, weighted with w (accumulator
-// order): off(x) is row x's byte offset in `r`. `masked`: pairs of bit v of `seen` zero
-// are left out where the products are not finite.
+// The block's 32 rows by columns: lane (h, c) holds column 32 dt + c of rows acc_row(v, h).
+// off(x) is row x's byte offset in the buffer.
+template <typename T, int D>
+struct ColOp {
+  float x[Geo<D>::NDT][16];
+  template <typename Off>
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, Off off, int c, int h) {
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      const int o = off(acc_row(v, h));
+#pragma unroll
+      for (int dt = 0; dt < Geo<D>::NDT; ++dt) {
+        x[dt][v] = ld1<T>(r, o == kFar ? kFar : o + (32 * dt + (D < 32 ? c & (D - 1) : c)) * static_cast<int>(sizeof(T)));
+        if (D < 32 && c >= D) x[dt][v] = 0.f;
+      }
+    }
+  }
+};
+// Adds the sum of the block's rows x weighted with w (accumulator order). `masked`: pairs of
+// bit v of `seen` zero are left out where the products are not finite.
 template <typename T, int D, typename Off>
-__device__ __forceinline__ void weighted_rows(f32x16_t (&acc)[Geo<D>::NDT], const float* w, __amdgpu_buffer_rsrc_t r, Off off,
-                                              int c, int h, bool masked, unsigned seen, float* scratch) {
+__device__ __forceinline__ void weighted_rows(f32x16_t (&acc)[Geo<D>::NDT], const float* w, const ColOp<T, D>& cols,
+                                              __amdgpu_buffer_rsrc_t r, Off off, int c, int h, bool masked, unsigned seen, float* scratch) {
   constexpr int S = static_cast<int>(sizeof(T));
 #pragma unroll
   for (int dt = 0; dt < Geo<D>::NDT; ++dt) {
     f32x16_t u = {};
 #pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      const int o = off(acc_row(v, h));
-      float x = ld1<T>(r, o == kFar ? kFar : o + (32 * dt + (D < 32 ? c & (D - 1) : c)) * S);
-      if (D < 32 && c >= D) x = 0.f;
-      u = mfma_f32(x, w[v], u);
-    }
+    for (int v = 0; v < 16; ++v) u = mfma_f32(cols.x[dt][v], w[v], u);
     if (masked) {
       float sum = 0.f;
 #pragma unroll
@@ -175,8 +189,8 @@ struct Score {
 };
 
 // Adds the wavefronts' accumulators in order: afterwards wavefront w holds the sum's
-// tiles dt = w, w + 4, .. (the others' are left as they were). `lds`: 4 NDT 1024 floats.
-template <int NDT>
+// tile w, if there is one (the others' are left as they were). `lds`: kWaves NDT 1024 floats.
+template <int kWaves, int NDT>
 __device__ __forceinline__ void add_waves(f32x16_t (&acc)[NDT], float* lds, int wave, int lane) {
 #pragma unroll
   for (int dt = 0; dt < NDT; ++dt)
@@ -214,8 +228,8 @@ struct Rows {
 };
 
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads, 1) void dot_fwd_f32_kernel(DotArgs a) {
-  constexpr int NDT = Geo<D>::NDT, S = sizeof(T);
+__global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void dot_fwd_f32_kernel(DotArgs a) {
+  constexpr int NDT = Geo<D>::NDT, S = sizeof(T), kWaves = 4;
   __shared__ float lds[kWaves * NDT * 1024 > kWaves * kScratch ? kWaves * NDT * 1024 : kWaves * kScratch];
   __shared__ float stat[2][kWaves][32];
   const int nrb = (a.G * a.Nq + kDotBlock - 1) / kDotBlock;
@@ -253,6 +267,11 @@ __global__ __launch_bounds__(kThreads, 1) void dot_fwd_f32_kernel(DotArgs a) {
         const int j0 = blk * kDotBlock;
         RowOp<T, D> k;
         k.load(rows_of(kb + j0 * a.ksn, m.L - j0, a.ksn, D), static_cast<int>(c * a.ksn * S), h);
+        const auto rv = rows_of(vb + j0 * a.vsn, m.L - j0, a.vsn, D);
+        auto voff = [&](int y) { return static_cast<int>(y * a.vsn * S); };
+        ColOp<T, D> vt;  // (on its way while the scores are formed)
+        vt.load(rv, voff, c, h);
+        __builtin_amdgcn_sched_barrier(0);
         const f32x16_t s = row_product(k, q);
         float x[16], top = -kInf;
         unsigned seen = 0;
@@ -282,8 +301,7 @@ __global__ __launch_bounds__(kThreads, 1) void dot_fwd_f32_kernel(DotArgs a) {
         for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
           for (int v = 0; v < 16; ++v) acc[dt][v] *= down;
-        weighted_rows<T, D>(acc, x, rows_of(vb + j0 * a.vsn, m.L - j0, a.vsn, D),
-                            [&](int y) { return static_cast<int>(y * a.vsn * S); }, c, h, !full, seen, lds + wave * kScratch);
+        weighted_rows<T, D>(acc, x, vt, rv, voff, c, h, !full, seen, lds + wave * kScratch);
       });
   l += swap_halves(l);
   if (h == 0) stat[0][wave][c] = mx, stat[1][wave][c] = l;
@@ -300,7 +318,7 @@ __global__ __launch_bounds__(kThreads, 1) void dot_fwd_f32_kernel(DotArgs a) {
   for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
     for (int v = 0; v < 16; ++v) acc[dt][v] *= down;
-  add_waves(acc, lds, wave, lane);
+  add_waves<kWaves>(acc, lds, wave, lane);
   if (!row.valid) return;
   const float scale = a.nsplit > 1 ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
   const int64_t r = static_cast<int64_t>(bh) * a.G * a.Nq + block * kDotBlock + c;
@@ -364,8 +382,8 @@ __global__ void dot_join_kernel(DotArgs a) {
 __device__ __forceinline__ float prob(float x, float lse) { return lse == -kInf ? 0.f : fast_exp2((x - lse) * kLog2e); }
 
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads, 1) void dot_dq_f32_kernel(DotArgs a) {
-  constexpr int NDT = Geo<D>::NDT, S = sizeof(T);
+__global__ __launch_bounds__(64 * kWavesOf<D>, D <= 64 ? 2 : 1) void dot_dq_f32_kernel(DotArgs a) {
+  constexpr int NDT = Geo<D>::NDT, S = sizeof(T), kWaves = kWavesOf<D>;
   __shared__ float lds[kWaves * NDT * 1024 > kWaves * kScratch ? kWaves * NDT * 1024 : kWaves * kScratch];
   const int nrb = (a.G * a.Nq + kDotBlock - 1) / kDotBlock;
   int64_t unit;
@@ -409,11 +427,28 @@ __global__ __launch_bounds__(kThreads, 1) void dot_dq_f32_kernel(DotArgs a) {
       [&](int blk, bool full) {
         const int j0 = blk * kDotBlock;
         const auto rk = rows_of(kb + j0 * a.ksn, m.L - j0, a.ksn, D);
-        RowOp<T, D> k;
-        k.load(rk, static_cast<int>(c * a.ksn * S), h);
+        auto koff = [&](int y) { return static_cast<int>(y * a.ksn * S); };
+        // At head_dim 128, with one wavefront a SIMD and registers to spare, operands are loaded a
+        // product ahead (527 -> 372 us at B=1 H=8 N=3000; at 64 it spills, 73 -> 78 us at H=4 N=2000).
+        constexpr bool kAhead = D > 64;
+        const auto rv = rows_of(vb + j0 * a.vsn, m.L - j0, a.vsn, D);
+        const int voff = static_cast<int>(c * a.vsn * S);
+        RowOp<T, D> k, v;
+        ColOp<T, D> kt;
+        k.load(rk, koff(c), h);
+        if constexpr (kAhead) {
+          v.load(rv, voff, h);
+          __builtin_amdgcn_sched_barrier(0);
+        }
         const f32x16_t s = row_product(k, q);
-        k.load(rows_of(vb + j0 * a.vsn, m.L - j0, a.vsn, D), static_cast<int>(c * a.vsn * S), h);
-        const f32x16_t dp = row_product(k, g);
+        if constexpr (kAhead) {
+          kt.load(rk, koff, c, h);
+          __builtin_amdgcn_sched_barrier(0);
+        } else {
+          v.load(rv, voff, h);
+        }
+        const f32x16_t dp = row_product(v, g);
+        if constexpr (!kAhead) kt.load(rk, koff, c, h);
         float x[16];
         unsigned seen = 0;
 #pragma unroll
@@ -428,11 +463,10 @@ __global__ __launch_bounds__(kThreads, 1) void dot_dq_f32_kernel(DotArgs a) {
             seen |= static_cast<unsigned>(see) << v;
             x[v] = see ? x[v] : 0.f;
           });
-        weighted_rows<T, D>(acc, x, rk, [&](int y) { return static_cast<int>(y * a.ksn * S); }, c, h, !full, seen,
-                            lds + wave * kScratch);
+        weighted_rows<T, D>(acc, x, kt, rk, koff, c, h, !full, seen, lds + wave * kScratch);
       });
   __syncthreads();
-  add_waves(acc, lds, wave, lane);
+  add_waves<kWaves>(acc, lds, wave, lane);
   if (!row.valid) return;
   T* dst = static_cast<T*>(a.dq) + ((static_cast<int64_t>(b) * a.Nq + row.i) * a.H + row.head) * D;
 #pragma unroll
@@ -455,8 +489,8 @@ struct RowInfo {
 };
 
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads, 1) void dot_dkv_f32_kernel(DotArgs a) {
-  constexpr int NDT = Geo<D>::NDT, S = sizeof(T);
+__global__ __launch_bounds__(64 * kWavesOf<D>, D <= 64 ? 2 : 1) void dot_dkv_f32_kernel(DotArgs a) {
+  constexpr int NDT = Geo<D>::NDT, S = sizeof(T), kWaves = kWavesOf<D>;
   __shared__ float lds[kWaves * NDT * 1024 > kWaves * kScratch ? kWaves * NDT * 1024 : kWaves * kScratch];
   __shared__ RowInfo infos[kWaves];
   const int nkb = (a.Nk + kDotBlock - 1) / kDotBlock;
@@ -506,11 +540,17 @@ __global__ __launch_bounds__(kThreads, 1) void dot_dkv_f32_kernel(DotArgs a) {
         __builtin_amdgcn_wave_barrier();
         const auto rq = rows_of(qb + i0 * a.qsn, a.Nq - i0, a.qsn, (a.H - 1) * a.qsh + D);
         const auto rg = rows_of(static_cast<const T*>(a.dout) + (static_cast<int64_t>(b) * a.Nq + i0) * orow, a.Nq - i0, orow, orow);
-        RowOp<T, D> q;
+        auto qat = [&](int y) { return info.qoff[y]; };
+        auto gat = [&](int y) { return info.goff[y]; };
+        RowOp<T, D> q, g;
         q.load(rq, qoff, h);
+        g.load(rg, goff, h);
+        __builtin_amdgcn_sched_barrier(0);
         const f32x16_t s = row_product(q, k);
-        q.load(rg, goff, h);
-        const f32x16_t dp = row_product(q, v);
+        ColOp<T, D> t;
+        t.load(rg, gat, c, h);
+        __builtin_amdgcn_sched_barrier(0);
+        const f32x16_t dp = row_product(g, v);
         float x[16], w[16];
         unsigned seen = 0;
 #pragma unroll
@@ -527,13 +567,14 @@ __global__ __launch_bounds__(kThreads, 1) void dot_dkv_f32_kernel(DotArgs a) {
             x[e] = see ? x[e] : 0.f;
           });
         // (rows past the last query load as zeros, with probabilities of 0)
-        weighted_rows<T, D>(accv, w, rg, [&](int y) { return info.goff[y]; }, c, h, !full, seen, lds + wave * kScratch);
-        weighted_rows<T, D>(acck, x, rq, [&](int y) { return info.qoff[y]; }, c, h, !full, seen, lds + wave * kScratch);
+        weighted_rows<T, D>(accv, w, t, rg, gat, c, h, !full, seen, lds + wave * kScratch);
+        t.load(rq, qat, c, h);
+        weighted_rows<T, D>(acck, x, t, rq, qat, c, h, !full, seen, lds + wave * kScratch);
         __builtin_amdgcn_wave_barrier();
       });
   __syncthreads();
-  add_waves(accv, lds, wave, lane);
-  add_waves(acck, lds, wave, lane);
+  add_waves<kWaves>(accv, lds, wave, lane);
+  add_waves<kWaves>(acck, lds, wave, lane);
   if (j >= a.Nk) return;
   const int64_t at = ((static_cast<int64_t>(b) * a.Nk + j) * a.Hkv + hk) * D;
 #pragma unroll
@@ -565,7 +606,7 @@ __global__ void dot_ranges_kernel(const int* docs, int2* ranges, int B, int Nk) 
 template <typename T, int D>
 hipError_t launch_fwd(const DotArgs& a, hipStream_t st) {
   const int64_t nrb = (static_cast<int64_t>(a.G) * a.Nq + kDotBlock - 1) / kDotBlock;
-  dot_fwd_f32_kernel<T, D><<<unit_grid(static_cast<int64_t>(a.B) * a.Hkv, nrb * a.nsplit), kThreads, 0, st>>>(a);
+  dot_fwd_f32_kernel<T, D><<<unit_grid(static_cast<int64_t>(a.B) * a.Hkv, nrb * a.nsplit), 256, 0, st>>>(a);
   if (a.nsplit > 1) {
     const int64_t rows = static_cast<int64_t>(a.B) * a.H * a.Nq;
     dot_join_kernel<T><<<static_cast<unsigned>((rows + 256 / D - 1) / (256 / D)), 256, 0, st>>>(a);
@@ -576,8 +617,8 @@ template <typename T, int D>
 hipError_t launch_bwd(const DotArgs& a, hipStream_t st) {
   const int64_t nrb = (static_cast<int64_t>(a.G) * a.Nq + kDotBlock - 1) / kDotBlock;
   const int64_t nkb = (a.Nk + kDotBlock - 1) / kDotBlock;
-  dot_dq_f32_kernel<T, D><<<unit_grid(static_cast<int64_t>(a.B) * a.Hkv, nrb), kThreads, 0, st>>>(a);
-  dot_dkv_f32_kernel<T, D><<<unit_grid(static_cast<int64_t>(a.B) * a.Hkv, nkb), kThreads, 0, st>>>(a);
+  dot_dq_f32_kernel<T, D><<<unit_grid(static_cast<int64_t>(a.B) * a.Hkv, nrb), 64 * kWavesOf<D>, 0, st>>>(a);
+  dot_dkv_f32_kernel<T, D><<<unit_grid(static_cast<int64_t>(a.B) * a.Hkv, nkb), 64 * kWavesOf<D>, 0, st>>>(a);
   return hipGetLastError();
 }
 template <typename T>

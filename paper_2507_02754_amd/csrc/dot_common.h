@@ -177,14 +177,15 @@ struct DotBlock {
   int blk;
   bool mine, full;
 };
-template <typename Test>
+// Blocks lo + off, lo + off + step, .. < hi, or (BACK) hi - 1 - off, hi - 1 - off - step, .. >= lo.
+template <bool BACK, typename Test>
 struct BlockSeq {
   Test test;
-  int lo, count, step, n0;
+  int first, count, step, n0;
   unsigned long long todo, mine, full;
-  __device__ __forceinline__ BlockSeq(int lo_, int hi, int off, int step_, Test t) : test(t), lo(lo_ + off), step(step_), n0(-64), todo(0), mine(0), full(0) {
-    count = lo < hi ? (hi - lo + step - 1) / step : 0;
-  }
+  __device__ __forceinline__ BlockSeq(int lo, int hi, int off, int by, Test t)
+      : test(t), first(BACK ? hi - 1 - off : lo + off), count(lo + off < hi ? (hi - lo - off + by - 1) / by : 0), step(BACK ? -by : by),
+        n0(-64), todo(0), mine(0), full(0) {}
   __device__ __forceinline__ DotBlock next() {
     while (todo == 0) {
       n0 += 64;
@@ -194,19 +195,19 @@ struct BlockSeq {
       }
       const int lane = threadIdx.x & 63;
       bool l = false, w = false, f = false;
-      if (n0 + lane < count) test(lo + (n0 + lane) * step, l, w, f);
+      if (n0 + lane < count) test(first + (n0 + lane) * step, l, w, f);
       todo = __builtin_amdgcn_ballot_w64(l);
       mine = __builtin_amdgcn_ballot_w64(w);
       full = __builtin_amdgcn_ballot_w64(f);
     }
     const int i = __builtin_ctzll(todo);
     todo &= todo - 1;
-    return DotBlock{lo + (n0 + i) * step, static_cast<bool>((mine >> i) & 1), static_cast<bool>((full >> i) & 1)};
+    return DotBlock{first + (n0 + i) * step, static_cast<bool>((mine >> i) & 1), static_cast<bool>((full >> i) & 1)};
   }
 };
-template <typename Test>
-__device__ __forceinline__ BlockSeq<Test> block_seq(int lo, int hi, int off, int step, Test t) {
-  return BlockSeq<Test>(lo, hi, off, step, t);
+template <bool BACK = false, typename Test>
+__device__ __forceinline__ BlockSeq<BACK, Test> block_seq(int lo, int hi, int off, int step, Test t) {
+  return BlockSeq<BACK, Test>(lo, hi, off, step, t);
 }
 
 // Workgroup order. Workgroups go to the 8 XCDs in turn. `heads` (sequence, K-side head) pairs of

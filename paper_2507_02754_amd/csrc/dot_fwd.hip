@@ -22,6 +22,10 @@
 // for the product with V (it is then a weighted mean of V's rows whatever the
 // rounding); LSE takes the sum of the unrounded ones.
 //
+// With a distance bias the blocks are walked from the nearest keys back: the scores fall
+// on the way, where forwards every block would raise the maximum (B=1 H=16 Hkv=4 N=8192
+// D=128 causal: 451 us forwards, 313 back).
+//
 // A block whose pairs are all visible has no mask work; blocks without a visible pair
 // are not visited (walked 64 at a time, a lane each). A masked pair's probability of
 // 0 times an infinity or NaN of V is NaN: rows that come out so are formed again by
@@ -49,27 +53,32 @@ struct Row {
     m = -1e30f, l = 0.f, lr = 0.f;
   }
   // Probabilities of a block, packed; `masked`: hide(s) sets the scores of pairs that are not
-  // visible to -inf.
+  // visible to -inf; `behind`: all keys are at or before the wavefront's queries.
   template <typename Hide>
-  __device__ __forceinline__ void step(f32x16_t& s, const Scores<CAP, BIAS>& score, float dj, bool masked, Hide hide,
+  __device__ __forceinline__ void step(f32x16_t& s, const Scores<CAP, BIAS>& score, float dj, bool behind, bool masked, Hide hide,
                                        u32x4_t (&pf)[2]) {
     const bf16x2_t ones = {static_cast<__bf16>(1.0f), static_cast<__bf16>(1.0f)};
-    float mul = score.scale2;
-    if (CAP || BIAS || masked) {
+    float mul = score.scale2, less = 0.f;  // scores are mul s - less
+    if (BIAS && behind) {
+      mul = 1.f, less = score.slope2 * dj;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[v] = score.behind(s[v], v);
+    } else if (CAP || BIAS || masked) {
       mul = 1.f;
 #pragma unroll
-      for (int v = 0; v < 16; ++v) s[v] = score(s[v], dj - static_cast<float>(8 * (v >> 2) + (v & 3)));
-      if (masked) hide(s);
+      for (int v = 0; v < 16; ++v) s[v] = score(s[v], v, dj);
     }
+    if (masked) hide(s);
     float lb, lrb;
     auto form = [&]() __attribute__((always_inline)) {
       lb = 0.f, lrb = 0.f;
+      const float n = BIAS ? -(m + less) : -m;
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float x = fast_exp2(__builtin_fmaf(s[8 * u + 2 * e], mul, -m));
-          const float y = fast_exp2(__builtin_fmaf(s[8 * u + 2 * e + 1], mul, -m));
+          const float x = fast_exp2(__builtin_fmaf(s[8 * u + 2 * e], mul, n));
+          const float y = fast_exp2(__builtin_fmaf(s[8 * u + 2 * e + 1], mul, n));
           lb += x;
           lb += y;
           const unsigned xy = pack_bf16x2(x, y);
@@ -82,6 +91,7 @@ struct Row {
       float mx = s[0] * mul;
 #pragma unroll
       for (int v = 1; v < 16; ++v) mx = fmaxf(mx, s[v] * mul);
+      if constexpr (BIAS) mx -= less;  // (the halves' differ)
       mx = fmaxf(m, fmaxf(mx, swap_halves(mx)));
       const float down = fast_exp2(m - mx);
       l *= down, lr *= down;
@@ -173,7 +183,7 @@ __global__ __launch_bounds__(kThreads* GROUPS, 2) void dot_fwd_kernel(DotArgs a)
   int lo, hi;
   key_blocks(m, all, lo, hi);
   const bool some = r0 < R;
-  auto seq = block_seq(lo, hi, 0, 1, [&](int blk, bool& live, bool& mine, bool& full) {
+  auto seq = block_seq<BIAS>(lo, hi, 0, 1, [&](int blk, bool& live, bool& mine, bool& full) {
     const DotSpan k(m, blk * kDotBlock, blk * kDotBlock + kDotBlock - 1);
     live = dot_live(m, all, k);
     mine = some && dot_live(m, own, k);
@@ -269,7 +279,7 @@ __global__ __launch_bounds__(kThreads* GROUPS, 2) void dot_fwd_kernel(DotArgs a)
       products(sc[nxt]);
       u32x4_t pf[2];
       const int j0 = at.blk * kDotBlock;
-      row.step(sc[cur], score, static_cast<float>(pos - j0), !at.full,
+      row.step(sc[cur], score, static_cast<float>(pos - j0), BIAS && j0 + 31 <= own.p0, !at.full,
                [&](f32x16_t& s) __attribute__((always_inline)) {
                  each_pair(m, seen, c, h, [&](int x) { return j0 + x; }, [&](int v, bool see) { s[v] = see ? s[v] : -kInf; });
                },
@@ -354,7 +364,7 @@ __global__ __launch_bounds__(kThreads, 1) void dot_few_kernel(DotArgs a) {
   const int pos = w.p - 4 * h;
   int lo, hi;
   key_blocks(m, own, lo, hi);
-  auto seq = block_seq(lo, hi, part * kWaves + wave, kWaves * a.nsplit, [&](int blk, bool& live, bool& mine, bool& full) {
+  auto seq = block_seq<BIAS>(lo, hi, part * kWaves + wave, kWaves * a.nsplit, [&](int blk, bool& live, bool& mine, bool& full) {
     const DotSpan k(m, blk * kDotBlock, blk * kDotBlock + kDotBlock - 1);
     live = dot_live(m, own, k);
     mine = live;
@@ -410,7 +420,7 @@ __global__ __launch_bounds__(kThreads, 1) void dot_few_kernel(DotArgs a) {
     load(SC, bq[S].blk);
     u32x4_t pf[2];
     const int j0 = at.blk * kDotBlock;
-    row.step(s, score, static_cast<float>(pos - j0), !at.full,
+    row.step(s, score, static_cast<float>(pos - j0), BIAS && j0 + 31 <= own.p0, !at.full,
              [&](f32x16_t& s) __attribute__((always_inline)) {
                each_pair(m, seen, c, h, [&](int x) { return j0 + x; }, [&](int v, bool see) { s[v] = see ? s[v] : -kInf; });
              },

@@ -34,18 +34,32 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const uint16_t* p, int
 template <bool CAP, bool BIAS>
 struct Scores {
   float scale2, to_cap, cap2, slope2;
+  float ramp[BIAS ? 16 : 1];  // the bias over a block's keys: slope2 times key 8 (v / 4) + v % 4
   __device__ __forceinline__ Scores(const DotArgs& a, int head)
       : scale2(a.scale * kLog2e), to_cap(CAP ? 2.f * kLog2e * a.scale / a.cap : 0.f), cap2(a.cap * kLog2e),
-        slope2(BIAS ? a.slopes[head] * kLog2e : 0.f) {}
-  // dj: position less key j
-  __device__ __forceinline__ float operator()(float s, float dj) const {
+        slope2(BIAS ? a.slopes[head] * kLog2e : 0.f) {
+    if constexpr (BIAS) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) ramp[v] = slope2 * static_cast<float>(8 * (v >> 2) + (v & 3));
+    }
+  }
+  // dj: position less the block's first key (of the lane's half).
+  __device__ __forceinline__ float operator()(float s, int v, float dj) const {
     float x;
     if constexpr (CAP)
       x = cap2 - 2.f * cap2 * __builtin_amdgcn_rcpf(fast_exp2(s * to_cap) + 1.f);  // cap tanh
     else
       x = s * scale2;
-    if constexpr (BIAS) x = __builtin_fmaf(-slope2, fabsf(dj), x);
+    if constexpr (BIAS) x = __builtin_fmaf(-slope2, fabsf(dj - static_cast<float>(8 * (v >> 2) + (v & 3))), x);
     return x;
+  }
+  // The same plus slope2 dj, for a block whose keys are all at or before the query: no
+  // distance to form for each.
+  __device__ __forceinline__ float behind(float s, int v) const {
+    if constexpr (CAP)
+      return cap2 - 2.f * cap2 * __builtin_amdgcn_rcpf(fast_exp2(s * to_cap) + 1.f) + (BIAS ? ramp[v] : 0.f);
+    else
+      return __builtin_fmaf(s, scale2, BIAS ? ramp[v] : 0.f);
   }
 };
 

@@ -683,7 +683,9 @@ DotPlan dot_bwd_plan(int64_t B, int64_t Nq, int64_t Nk, int64_t H, int64_t Hkv, 
   if (bf16) {
     p.nsplit = rows_form(rows, D, docs);
     // The key side: as the rows where a head has few of them; else `ks` workgroups for a
-    // block of 128 keys, their float32 sums added afterwards, up to about 1024 in all.
+    // block of 128 keys, their float32 sums added afterwards, up to about 1024 in all (2048
+    // with documents, which make some key blocks' rows many: three of them, keys 256, R 32768,
+    // ks 4 / 6 / 8: 1008 / 959 / 936 us).
     // Backward us of (0, ks 1) / (-1, 1) / 1 / (0, ks 2) / 4 / 8 at D = 128: keys 1024 (units of 128)
     // 976 / 1075 / 1879 / 1076 / 1199 / 1470; 512: 778 / 560 / 1153 / 620 / 691 / 830; 256, R = 4096: 401 / 311 / 356 / 298 / 271 / 352; 256,
     // R = 32768: 2252 / 1624 / 1595 / 1393 / 1170 / 1103; 32, R = 8192: 601 / 402 / 250 / 342 / 219 / 162; 256, R = 1024: 124 / 98 / 146 /
@@ -695,7 +697,7 @@ DotPlan dot_bwd_plan(int64_t B, int64_t Nq, int64_t Nk, int64_t H, int64_t Hkv, 
     else if (R <= 2048 || keys >= 384)
       p.kside = -1;
     else
-      p.kside = 0, p.ks = static_cast<int>(std::max<int64_t>(2, std::min<int64_t>(8, 1024 / keys)));
+      p.kside = 0, p.ks = static_cast<int>(std::max<int64_t>(2, std::min<int64_t>(8, (docs ? 2048 : 1024) / keys)));
   }
   p.ranges_off = 0;
   p.delta_off = docs ? up256(static_cast<size_t>(B) * ((Nk + kDotBlock - 1) / kDotBlock) * sizeof(int2)) : 0;

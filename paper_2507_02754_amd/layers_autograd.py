@@ -29,6 +29,21 @@ def _needs_grad(*tensors):
     return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
 
 
+# A Function keeps the tensors of its call with save_for_backward alone, which notices
+# changes in place and lets hooks put them elsewhere meanwhile; the checked arguments serve the
+# backward where the tensors come back to the same places.
+def _save(ctx, call, options, tensors):
+    ctx.save_for_backward(*[t for t in tensors if t is not None])
+    ctx.present = [t is not None for t in tensors]
+    ctx.call, ctx.options, ctx.places = call, options, call.places()
+    call.kept = None
+
+
+def _saved(ctx):
+    tensors = iter(ctx.saved_tensors)
+    return [next(tensors) if there else None for there in ctx.present]
+
+
 class NormRotateFunction(torch.autograd.Function):
     """ys = norm and rotation of the first `count` of `tensors`, with the rest as their weights."""
 
@@ -36,22 +51,24 @@ class NormRotateFunction(torch.autograd.Function):
     def forward(ctx, options, count, *tensors):
         xs, weights = [_rows(x) for x in tensors[:count]], tensors[count:] or None
         call = _RotateCall(xs, weights, *options)
-        ctx.save_for_backward(*xs, *(weights or ()))
-        # (the tensors stay with save_for_backward, which watches for changes in place)
-        call.kept = (None, weights and [None] * count, options[3])
-        ctx.call, ctx.count = call, count
-        return tuple(call.forward())
+        ys = call.forward()
+        _save(ctx, call, options, [*xs, *(weights or ()), options[3]])
+        ctx.count = count
+        return tuple(ys)
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, *dys):
-        tensors, count, call = ctx.saved_tensors, ctx.count, ctx.call
-        weights = tensors[count:]
+        call, count, options = ctx.call, ctx.count, ctx.options
+        *tensors, positions = _saved(ctx)
+        xs, weights = tensors[:count], tensors[count:] or None
+        call.kept = (xs, weights, positions)
+        if call.places() != ctx.places:
+            call = _RotateCall(xs, weights, *options[:3], positions, *options[4:])
         dys = [torch.zeros(s, dtype=call.dtype, device=call.device) if dy is None else _dense(dy, call.dtype)
                for s, dy in zip(call.shapes, dys)]
-        call.kept = (tensors[:count], weights or None, call.kept[2])
         dxs, dws = call.backward(dys, weight_grads=any(ctx.needs_input_grad[2 + count:]))
-        call.kept = (None, weights and [None] * count, call.kept[2])
+        ctx.call.kept = None
         return (None, None, *dxs, *(dws if weights else ()))
 
 
@@ -69,7 +86,7 @@ def norm_rotate(xs, weights=None, eps=1e-6, freqs=None, layout="half", positions
     xs[t] is [B, N, heads_t, D]; arguments as simplicial_norm_rotate_fwd, whose results
     are returned as a tuple. eps = 0 without weights is the L2 norm scaled by sqrt(D). A
     weight is given for every tensor or for none."""
-    options = (eps, freqs, layout, positions, start)
+    options = (eps, None if freqs is None else tuple(freqs), layout, positions, start)
     xs = list(xs)
     if weights is not None and any(w is None for w in weights):
         raise ValueError("a weight for every tensor, or weights=None")
@@ -87,9 +104,8 @@ class DotAttentionFunction(torch.autograd.Function):
         call = _DotCall(q, k, v, *options)
         lo = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q.dtype == torch.bfloat16 else None
         out, lse = call.forward(out_lo=lo)
-        ctx.save_for_backward(q, k, v, out, lse, *(() if lo is None else (lo,)))
-        call.q = call.k = call.v = None  # (they stay with save_for_backward, which watches for changes in place)
-        ctx.call = call
+        _save(ctx, call, options, [q, k, v, out, lse, lo, *options[4:]])
+        call.q = call.k = call.v = None
         ctx.mark_non_differentiable(lse)
         return out, lse
 
@@ -97,10 +113,13 @@ class DotAttentionFunction(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, dout, _dlse):
         call = ctx.call
-        call.q, call.k, call.v, out, lse, *lo = ctx.saved_tensors
+        q, k, v, out, lse, lo, *masks = _saved(ctx)
+        call.q, call.k, call.v, call.kept = q, k, v, masks
+        if call.places() != ctx.places:
+            call = _DotCall(q, k, v, *ctx.options[:4], *masks)
         dout = torch.zeros_like(out) if dout is None else _dense(dout, out.dtype)
-        grads = call.backward(out, dout, lse, *lo)
-        call.q = call.k = call.v = None
+        grads = call.backward(out, dout, lse, lo)
+        ctx.call.q = ctx.call.k = ctx.call.v = ctx.call.kept = None
         return (*grads, None)
 
 

@@ -179,6 +179,11 @@ class _RotateCall:
                      _DTYPES[wdtype])
         self.kept = (xs, weights, positions)  # what the pointers point to
 
+    def places(self):
+        """Where the tensors lie: the arguments hold for other tensors with the same ones."""
+        xs, weights, positions = self.kept
+        return ([(x.data_ptr(), x.stride()) for x in xs], weights and [_ptr(w) for w in weights], _ptr(positions))
+
     def forward(self, out=None):
         if out is None:
             out = [torch.empty(s, dtype=self.dtype, device=self.device) for s in self.shapes]
@@ -287,6 +292,10 @@ class _DotCall:
         self.args = (B, Nq, Nk, H, Hkv, D, *_strides(q), *_strides(k), *_strides(v), D ** -0.5 if scale is None else float(scale),
                      float(softcap), causal, window, _ptr(slopes), _ptr(documents), _ptr(prefix), _ptr(k_lens), dt)
         self.kept = (slopes, documents, prefix, k_lens)  # what the pointers point to
+
+    def places(self):
+        """As _RotateCall's."""
+        return ([t.stride() for t in (self.q, self.k, self.v)], [_ptr(t) for t in self.kept])
 
     def forward(self, out=None, lse=None, out_lo=None):
         q = self.q

@@ -206,6 +206,78 @@ def test_new_token_over_a_cache_is_the_whole_sequence():
         assert torch.isfinite(r.logprob).all() and (r.top_logprobs[:, 0] >= r.logprob).all()
 
 
+def _one_step(qkv, head, ws, targets, ids, freqs):
+    b, n = qkv.shape[:2]
+    q, k, v = qkv.split([4, 2, 2], dim=2)
+    q, k = norm_rotate([q, k], weights=ws, freqs=freqs, positions=torch.arange(n, device="cuda"))
+    o = dot_attention(q, k, v, documents=ids, softcap=10.0)
+    r = token_logprobs(o.view(b * n, -1) @ head.t(), targets.view(-1))
+    return torch.autograd.grad([r.logprob, r.entropy], [qkv, head, *ws], [torch.ones_like(r.logprob), 0.1 * torch.ones_like(r.entropy)])
+
+
+def _step_inputs(seed=3, n=75):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    qkv = torch.randn(2, n, 8, 64, generator=g, device="cuda").to(BF).requires_grad_(True)
+    head = (torch.randn(200, 256, generator=g, device="cuda") / 16).to(BF).requires_grad_(True)
+    ws = [torch.ones(64, device="cuda", requires_grad=True) for _ in range(2)]
+    targets = torch.randint(0, 200, (2, n), device="cuda", generator=g)
+    ids = (torch.arange(n, device="cuda") // 30).to(torch.int32).expand(2, n).contiguous()
+    return qkv, head, ws, targets, ids, rotary_freqs(32)
+
+
+def test_saved_tensors_elsewhere():
+    """Hooks that keep the saved tensors on the host (and bring them back to other places,
+    with other strides): the same gradients."""
+    inputs = _step_inputs()
+    want = _one_step(*inputs)
+    with torch.autograd.graph.save_on_cpu():
+        got = _one_step(*inputs)
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+def test_changes_in_place_are_noticed():
+    qkv, _, ws, _, ids, freqs = _step_inputs()
+    q, k, v = (t.contiguous() for t in qkv.split([4, 2, 2], dim=2))
+    o = dot_attention(q, k, v, documents=ids)
+    ids += 1
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        o.sum().backward()
+
+
+def test_another_stream():
+    """Calls on a stream of their own, the inputs made on it."""
+    want = _one_step(*_step_inputs())
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = _one_step(*_step_inputs())
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+def test_two_graphs_replayed_in_turn():
+    """Two captured steps of other sizes, whose workspaces are their own."""
+    cases = [_step_inputs(5, 75), _step_inputs(6, 300)]
+    graphs, held = [], []
+    for c in cases:
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            _one_step(*c)
+        torch.cuda.current_stream().wait_stream(side)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            held.append(_one_step(*c))
+        graphs.append(g)
+    want = [_one_step(*c) for c in cases]
+    for i in (0, 1, 1, 0, 1):
+        for t in held[i]:
+            t.zero_()
+        graphs[i].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want[i], held[i])), i
+
+
 def test_captured_training_step():
     """Norm and rotation, attention, a head and the log probabilities with all gradients in
     one graph, replayed on new inputs with eager work between."""

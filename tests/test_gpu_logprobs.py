@@ -68,6 +68,9 @@ def test_views_of_a_padded_vocabulary(dt):
         base[:, V:] = float("nan")
         x = base[:, :V]
         _check(x, torch.arange(6).cuda(), 4, f"view {V} of {pad}", _grads(6, V))
+        for start in (1, 5):
+            part = base[:, start:V - 9]  # rows that begin anywhere
+            _check(part, torch.arange(6).cuda(), 4, f"view {start} .. {V - 9} of {pad}", _grads(6, V))
 
 
 @pytest.mark.parametrize("dt", [BF, F32])

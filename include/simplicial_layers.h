@@ -122,7 +122,8 @@ int simplicial_dot_attn_fwd(const void* q, const void* k, const void* v, void* o
  *     dS = dA * (1 - tanh^2(s / softcap))
  *     dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO
  * dK and dV of a head shared by several query heads are sums over them in
- * float32, rounded once. The slopes get no gradient.
+ * float32, rounded once. The slopes get no gradient. P carries the rounding of LSE to
+ * float32, 2^-24 |LSE|: gradients of scores past 2^20 or so mean little.
  *   out, lse, dout   of the forward, contiguous
  *   out_lo           of the forward, or NULL: Delta of the rounded output, whose error (bf16
  *                    2^-8 of |dO| |O|) all of a row's gradients share;  dq [B, Nq, H, D], dk and dv

@@ -37,16 +37,13 @@ __device__ __forceinline__ Stat* stats_of(const DotArgs& a, int bh) {
 }
 
 // Base-2 score and the cap's derivative.
-template <bool CAP, bool BIAS>
+template <int CAP, bool BIAS>
 __device__ __forceinline__ float score_of(const Scores<CAP, BIAS>& c, float s, float slope2, float dj, float less, float& dcap) {
   float x;
-  if constexpr (CAP) {
-    const float u = __builtin_amdgcn_rcpf(fast_exp2(s * c.to_cap) + 1.f);  // tanh = 1 - 2 u
-    x = c.cap2 - 2.f * c.cap2 * u - less;
-    dcap = 4.f * (u - u * u);
-  } else {
+  if constexpr (CAP)
+    x = c.capped(s, dcap) - less;
+  else
     x = __builtin_fmaf(s, c.scale2, -less);
-  }
   if constexpr (BIAS) x = __builtin_fmaf(-slope2, fabsf(dj), x);
   return x;
 }
@@ -189,7 +186,7 @@ __device__ __forceinline__ float store_quads(uint16_t* p, const float (&y)[NDT][
 }
 
 // ---- query side ----
-template <int DP, bool CAP, bool BIAS, bool PRIV, int GROUPS>
+template <int DP, int CAP, bool BIAS, bool PRIV, int GROUPS>
 __global__ __launch_bounds__(kThreads* GROUPS, PRIV ? 1 : 2) void dot_dq_kernel(DotArgs a) {
   using T = SwzTile<DP>;
   constexpr int NT = DP / 16, NDT = DP / 32, SPW = PRIV ? T::instrs : T::instrs / kWaves, kRows = PRIV ? 32 : 32 * kWaves;
@@ -367,7 +364,7 @@ __global__ __launch_bounds__(kThreads* GROUPS, PRIV ? 1 : 2) void dot_dq_kernel(
 }
 
 // ---- key side ----
-template <int DP, bool CAP, bool BIAS, bool PRIV, int GROUPS>
+template <int DP, int CAP, bool BIAS, bool PRIV, int GROUPS>
 __global__ __launch_bounds__(kThreads* GROUPS, PRIV ? 1 : 2) void dot_dkv_kernel(DotArgs a) {
   using T = SwzTile<DP>;
   constexpr int NT = DP / 16, NDT = DP / 32, SPW = PRIV ? T::instrs : T::instrs / kWaves, kKeys = PRIV ? 32 : 32 * kWaves;
@@ -628,8 +625,8 @@ __global__ __launch_bounds__(kThreads) void dot_keys_kernel(DotArgs a) {
   if (d1) pk[64] = f32_to_bf16(x1 * a.scale), pv[64] = f32_to_bf16(y1);
 }
 
-template <int DP, bool CAP, bool BIAS>
-void launch(const DotArgs& a, hipStream_t st) {
+template <int DP, int CAP, bool BIAS>
+hipError_t launch(const DotArgs& a, hipStream_t st) {
   const int64_t R = static_cast<int64_t>(a.G) * a.Nq, heads = static_cast<int64_t>(a.B) * a.Hkv;
   const unsigned wide = unit_grid(heads, (R + 127) / 128);
   if (a.nsplit > 0)
@@ -646,20 +643,18 @@ void launch(const DotArgs& a, hipStream_t st) {
   else
     dot_dkv_kernel<DP, CAP, BIAS, false, 2><<<keys, 2 * kThreads, 0, st>>>(a);
   if (a.ks > 1) dot_keys_kernel<<<static_cast<unsigned>((heads * a.Nk + kWaves - 1) / kWaves), kThreads, 0, st>>>(a);
+  return hipGetLastError();
 }
 template <int DP>
-void launch(const DotArgs& a, hipStream_t st) {
-  if (a.cap > 0.f)
-    a.slopes ? launch<DP, true, true>(a, st) : launch<DP, true, false>(a, st);
-  else
-    a.slopes ? launch<DP, false, true>(a, st) : launch<DP, false, false>(a, st);
+hipError_t launch(const DotArgs& a, hipStream_t st) {
+  return with_cap(a.cap, [&](auto cap) {
+    constexpr int CAP = decltype(cap)::value;
+    return a.slopes ? launch<DP, CAP, true>(a, st) : launch<DP, CAP, false>(a, st);
+  });
 }
 
 }  // namespace
 
-hipError_t dot_bwd_bf16(const DotArgs& a, hipStream_t st) {
-  a.D <= 64 ? launch<64>(a, st) : launch<128>(a, st);
-  return hipGetLastError();
-}
+hipError_t dot_bwd_bf16(const DotArgs& a, hipStream_t st) { return a.D <= 64 ? launch<64>(a, st) : launch<128>(a, st); }
 
 }  // namespace sa

@@ -1,5 +1,5 @@
 // Dot-product attention in float32 arithmetic on the gfx950 matrix cores
-// (v_mfma_f32_32x32x2_f32): float32 data, and bf16 data widened on load.
+// (v_mfma_f32_32x32x2_f32).
 //
 //     s = scale q k;  a = cap tanh(s / cap) - slope |p - j|;  O = softmax(a) v
 //     dA = P (dO v - Delta);  dS = dA (1 - tanh^2);  dq = scale dS k, ...
@@ -41,29 +41,13 @@ __device__ __forceinline__ f32x16_t mfma_f32(float a, float b, f32x16_t c) {
 struct F4 {
   float x[4];
 };
-template <typename T>
 __device__ __forceinline__ F4 ld4(__amdgpu_buffer_rsrc_t r, int off) {
-  if constexpr (sizeof(T) == 4) {
-    const u32x4_t a = ldbuf128(r, off);
-    return F4{{__uint_as_float(a[0]), __uint_as_float(a[1]), __uint_as_float(a[2]), __uint_as_float(a[3])}};
-  } else {
-    const u32x2_t a = ldbuf64(r, off);
-    return F4{{bf16_lo(a[0]), bf16_hi(a[0]), bf16_lo(a[1]), bf16_hi(a[1])}};
-  }
+  const u32x4_t a = ldbuf128(r, off);
+  return F4{{__uint_as_float(a[0]), __uint_as_float(a[1]), __uint_as_float(a[2]), __uint_as_float(a[3])}};
 }
-template <typename T>
-__device__ __forceinline__ float ld1(__amdgpu_buffer_rsrc_t r, int off) {
-  if constexpr (sizeof(T) == 4)
-    return __uint_as_float(ldbuf32(r, off));
-  else
-    return bf16_to_f32(__builtin_amdgcn_raw_buffer_load_b16(r, off, 0, 0));
-}
-template <typename T>
-__device__ __forceinline__ void st4(T* p, const float* x) {
-  if constexpr (sizeof(T) == 4)
-    *reinterpret_cast<u32x4_t*>(p) = u32x4_t{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
-  else
-    *reinterpret_cast<u32x2_t*>(p) = u32x2_t{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+__device__ __forceinline__ float ld1(__amdgpu_buffer_rsrc_t r, int off) { return __uint_as_float(ldbuf32(r, off)); }
+__device__ __forceinline__ void st4(float* p, const float* x) {
+  *reinterpret_cast<u32x4_t*>(p) = u32x4_t{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
 }
 
 template <int D>
@@ -76,25 +60,24 @@ struct Geo {
 // `n` positions from `p` on, `sn` elements apart, whose rows reach `more` elements past
 // the last position: the buffer that a block's loads go through (what lies
 // behind it loads as zeros).
-template <typename T>
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const T* p, int n, int64_t sn, int64_t more) {
-  const int64_t bytes = n > 0 ? ((n - 1) * sn + more) * static_cast<int64_t>(sizeof(T)) : 0;
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const float* p, int n, int64_t sn, int64_t more) {
+  const int64_t bytes = n > 0 ? ((n - 1) * sn + more) * static_cast<int64_t>(sizeof(float)) : 0;
   return make_rsrc(p, static_cast<unsigned>(bytes < kFar ? bytes : kFar));
 }
 // One row in every lane: its float4s of columns 8 t + 4 h.
-template <typename T, int D>
+template <int D>
 struct RowOp {
   F4 f[Geo<D>::NF];
   __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, int off, int h) {
 #pragma unroll
     for (int t = 0; t < Geo<D>::NF; ++t)
-      f[t] = ld4<T>(r, off == kFar ? kFar : off + (8 * t + 4 * h) * static_cast<int>(sizeof(T)));
+      f[t] = ld4(r, off == kFar ? kFar : off + (8 * t + 4 * h) * 4);
   }
 };
 // a's rows times b's rows, contracted over the columns, in two chains added at the end
 // (the rounding of one chain of D is the largest error of a score).
-template <typename T, int D>
-__device__ __forceinline__ f32x16_t row_product(const RowOp<T, D>& a, const RowOp<T, D>& b) {
+template <int D>
+__device__ __forceinline__ f32x16_t row_product(const RowOp<D>& a, const RowOp<D>& b) {
   f32x16_t x = {}, y = {};
 #pragma unroll
   for (int t = 0; t < Geo<D>::NF / 2; ++t)
@@ -110,7 +93,7 @@ __device__ __forceinline__ f32x16_t row_product(const RowOp<T, D>& a, const RowO
 
 // The block's 32 rows by columns: lane (h, c) holds column 32 dt + c of rows acc_row(v, h).
 // off(x) is row x's byte offset in the buffer.
-template <typename T, int D>
+template <int D>
 struct ColOp {
   float x[Geo<D>::NDT][16];
   template <typename Off>
@@ -120,7 +103,7 @@ struct ColOp {
       const int o = off(acc_row(v, h));
 #pragma unroll
       for (int dt = 0; dt < Geo<D>::NDT; ++dt) {
-        x[dt][v] = ld1<T>(r, o == kFar ? kFar : o + (32 * dt + (D < 32 ? c & (D - 1) : c)) * static_cast<int>(sizeof(T)));
+        x[dt][v] = ld1(r, o == kFar ? kFar : o + (32 * dt + (D < 32 ? c & (D - 1) : c)) * 4);
         if (D < 32 && c >= D) x[dt][v] = 0.f;
       }
     }
@@ -128,10 +111,10 @@ struct ColOp {
 };
 // Adds the sum of the block's rows x weighted with w (accumulator order). `masked`: pairs of
 // bit v of `seen` zero are left out where the products are not finite.
-template <typename T, int D, typename Off>
-__device__ __forceinline__ void weighted_rows(f32x16_t (&acc)[Geo<D>::NDT], const float* w, const ColOp<T, D>& cols,
+template <int D, typename Off>
+__device__ __forceinline__ void weighted_rows(f32x16_t (&acc)[Geo<D>::NDT], const float* w, const ColOp<D>& cols,
                                               __amdgpu_buffer_rsrc_t r, Off off, int c, int h, bool masked, unsigned seen, float* scratch) {
-  constexpr int S = static_cast<int>(sizeof(T));
+  constexpr int S = 4;
 #pragma unroll
   for (int dt = 0; dt < Geo<D>::NDT; ++dt) {
     f32x16_t u = {};
@@ -158,7 +141,7 @@ __device__ __forceinline__ void weighted_rows(f32x16_t (&acc)[Geo<D>::NDT], cons
           const int o = off(x);
 #pragma unroll
           for (int vq = 0; vq < Geo<D>::NV / 4; ++vq) {
-            const F4 y = ld4<T>(r, o == kFar ? kFar : o + (32 * dt + 8 * vq + 4 * h) * S);
+            const F4 y = ld4(r, o == kFar ? kFar : o + (32 * dt + 8 * vq + 4 * h) * S);
 #pragma unroll
             for (int e = 0; e < 4; ++e) u[4 * vq + e] += use ? wx * y.x[e] : 0.f;
           }
@@ -227,9 +210,9 @@ struct Rows {
   }
 };
 
-template <typename T, int D>
+template <int D>
 __global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void dot_fwd_f32_kernel(DotArgs a) {
-  constexpr int NDT = Geo<D>::NDT, S = sizeof(T), kWaves = 4;
+  constexpr int NDT = Geo<D>::NDT, S = 4, kWaves = 4;
   __shared__ float lds[kWaves * NDT * 1024 > kWaves * kScratch ? kWaves * NDT * 1024 : kWaves * kScratch];
   __shared__ float stat[2][kWaves][32];
   const int nrb = (a.G * a.Nq + kDotBlock - 1) / kDotBlock;
@@ -245,13 +228,13 @@ __global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void dot_fwd_f32_kernel(DotAr
   const KeysSeen sees(m, row.p);
   const float slope = a.slopes ? a.slopes[row.valid ? row.head : 0] : 0.f;
   const Score score(a);
-  RowOp<T, D> q;
+  RowOp<D> q;
   {
-    const auto r = rows_of(static_cast<const T*>(a.q) + b * a.qsb + row.i0 * a.qsn, a.Nq - row.i0, a.qsn, (a.H - 1) * a.qsh + D);
+    const auto r = rows_of(static_cast<const float*>(a.q) + b * a.qsb + row.i0 * a.qsn, a.Nq - row.i0, a.qsn, (a.H - 1) * a.qsh + D);
     q.load(r, row.valid ? static_cast<int>(((row.i - row.i0) * a.qsn + row.head * a.qsh) * S) : kFar, h);
   }
-  const T* kb = static_cast<const T*>(a.k) + b * a.ksb + hk * a.ksh;
-  const T* vb = static_cast<const T*>(a.v) + b * a.vsb + hk * a.vsh;
+  const float* kb = static_cast<const float*>(a.k) + b * a.ksb + hk * a.ksh;
+  const float* vb = static_cast<const float*>(a.v) + b * a.vsb + hk * a.vsh;
   f32x16_t acc[NDT] = {};
   float mx = -kInf, l = 0.f;
   int lo, hi;
@@ -265,11 +248,11 @@ __global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void dot_fwd_f32_kernel(DotAr
       },
       [&](int blk, bool full) {
         const int j0 = blk * kDotBlock;
-        RowOp<T, D> k;
+        RowOp<D> k;
         k.load(rows_of(kb + j0 * a.ksn, m.L - j0, a.ksn, D), static_cast<int>(c * a.ksn * S), h);
         const auto rv = rows_of(vb + j0 * a.vsn, m.L - j0, a.vsn, D);
         auto voff = [&](int y) { return static_cast<int>(y * a.vsn * S); };
-        ColOp<T, D> vt;  // (on its way while the scores are formed)
+        ColOp<D> vt;  // (on its way while the scores are formed)
         vt.load(rv, voff, c, h);
         __builtin_amdgcn_sched_barrier(0);
         const f32x16_t s = row_product(k, q);
@@ -301,7 +284,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void dot_fwd_f32_kernel(DotAr
         for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
           for (int v = 0; v < 16; ++v) acc[dt][v] *= down;
-        weighted_rows<T, D>(acc, x, vt, rv, voff, c, h, !full, seen, lds + wave * kScratch);
+        weighted_rows<D>(acc, x, vt, rv, voff, c, h, !full, seen, lds + wave * kScratch);
       });
   l += swap_halves(l);
   if (h == 0) stat[0][wave][c] = mx, stat[1][wave][c] = l;
@@ -323,7 +306,7 @@ __global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void dot_fwd_f32_kernel(DotAr
   const float scale = a.nsplit > 1 ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
   const int64_t r = static_cast<int64_t>(bh) * a.G * a.Nq + block * kDotBlock + c;
   float* pr = a.part + (r * a.nsplit + part) * D;
-  T* out = static_cast<T*>(a.out) + ((static_cast<int64_t>(b) * a.Nq + row.i) * a.H + row.head) * D;
+  float* out = static_cast<float*>(a.out) + ((static_cast<int64_t>(b) * a.Nq + row.i) * a.H + row.head) * D;
 #pragma unroll
   for (int dt = 0; dt < NDT; ++dt) {
     if (dt % kWaves != wave) continue;
@@ -349,7 +332,6 @@ __global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void dot_fwd_f32_kernel(DotAr
 }
 
 // Joins the parts of a row: one thread a column.
-template <typename T>
 __global__ void dot_join_kernel(DotArgs a) {
   const int rows = blockDim.x / a.D;
   const int64_t r = static_cast<int64_t>(blockIdx.x) * rows + threadIdx.x / a.D, all = static_cast<int64_t>(a.B) * a.H * a.Nq;
@@ -370,20 +352,17 @@ __global__ void dot_join_kernel(DotArgs a) {
   const int bh = static_cast<int>(r / rh), rr = static_cast<int>(r - bh * rh), i = rr / a.G;
   const int b = bh / a.Hkv, head = (bh - b * a.Hkv) * a.G + rr - i * a.G;
   const float y = l == 0.f ? 0.f : x / l;
-  T* out = static_cast<T*>(a.out) + ((static_cast<int64_t>(b) * a.Nq + i) * a.H + head) * a.D + d;
-  if constexpr (sizeof(T) == 4)
-    *out = y;
-  else
-    *out = f32_to_bf16(y);
+  float* out = static_cast<float*>(a.out) + ((static_cast<int64_t>(b) * a.Nq + i) * a.H + head) * a.D + d;
+  *out = y;
   if (d == 0) a.lse[(static_cast<int64_t>(b) * a.H + head) * a.Nq + i] = l == 0.f ? -kInf : top + logf(l);
 }
 
 // Probability of a score; of a row without a key: 0.
 __device__ __forceinline__ float prob(float x, float lse) { return lse == -kInf ? 0.f : fast_exp2((x - lse) * kLog2e); }
 
-template <typename T, int D>
+template <int D>
 __global__ __launch_bounds__(64 * kWavesOf<D>, D <= 64 ? 2 : 1) void dot_dq_f32_kernel(DotArgs a) {
-  constexpr int NDT = Geo<D>::NDT, S = sizeof(T), kWaves = kWavesOf<D>;
+  constexpr int NDT = Geo<D>::NDT, S = 4, kWaves = kWavesOf<D>;
   __shared__ float lds[kWaves * NDT * 1024 > kWaves * kScratch ? kWaves * NDT * 1024 : kWaves * kScratch];
   const int nrb = (a.G * a.Nq + kDotBlock - 1) / kDotBlock;
   int64_t unit;
@@ -396,24 +375,24 @@ __global__ __launch_bounds__(64 * kWavesOf<D>, D <= 64 ? 2 : 1) void dot_dq_f32_
   const KeysSeen sees(m, row.p);
   const float slope = a.slopes ? a.slopes[row.valid ? row.head : 0] : 0.f;
   const Score score(a);
-  RowOp<T, D> q, g;
+  RowOp<D> q, g;
   float delta = 0.f;
   const int64_t orow = static_cast<int64_t>(a.H) * D;
   const int off = row.valid ? static_cast<int>(((row.i - row.i0) * orow + row.head * D) * S) : kFar;
   {
-    const auto r = rows_of(static_cast<const T*>(a.q) + b * a.qsb + row.i0 * a.qsn, a.Nq - row.i0, a.qsn, (a.H - 1) * a.qsh + D);
+    const auto r = rows_of(static_cast<const float*>(a.q) + b * a.qsb + row.i0 * a.qsn, a.Nq - row.i0, a.qsn, (a.H - 1) * a.qsh + D);
     q.load(r, row.valid ? static_cast<int>(((row.i - row.i0) * a.qsn + row.head * a.qsh) * S) : kFar, h);
     const int64_t at = (static_cast<int64_t>(b) * a.Nq + row.i0) * orow;
-    g.load(rows_of(static_cast<const T*>(a.dout) + at, a.Nq - row.i0, orow, orow), off, h);
-    RowOp<T, D> o;
-    o.load(rows_of(static_cast<const T*>(a.out_in) + at, a.Nq - row.i0, orow, orow), off, h);
+    g.load(rows_of(static_cast<const float*>(a.dout) + at, a.Nq - row.i0, orow, orow), off, h);
+    RowOp<D> o;
+    o.load(rows_of(static_cast<const float*>(a.out_in) + at, a.Nq - row.i0, orow, orow), off, h);
     delta = diagonal(row_product(o, g), c, h);
   }
   const int64_t srow = row.valid ? (static_cast<int64_t>(b) * a.H + row.head) * a.Nq + row.i : 0;
   const float lse = row.valid ? a.lse[srow] : -kInf;
   if (row.valid && wave == 0 && h == 0) a.delta[srow] = delta;
-  const T* kb = static_cast<const T*>(a.k) + b * a.ksb + hk * a.ksh;
-  const T* vb = static_cast<const T*>(a.v) + b * a.vsb + hk * a.vsh;
+  const float* kb = static_cast<const float*>(a.k) + b * a.ksb + hk * a.ksh;
+  const float* vb = static_cast<const float*>(a.v) + b * a.vsb + hk * a.vsh;
   f32x16_t acc[NDT] = {};
   int lo, hi;
   key_blocks(m, row.span, lo, hi);
@@ -433,8 +412,8 @@ __global__ __launch_bounds__(64 * kWavesOf<D>, D <= 64 ? 2 : 1) void dot_dq_f32_
         constexpr bool kAhead = D > 64;
         const auto rv = rows_of(vb + j0 * a.vsn, m.L - j0, a.vsn, D);
         const int voff = static_cast<int>(c * a.vsn * S);
-        RowOp<T, D> k, v;
-        ColOp<T, D> kt;
+        RowOp<D> k, v;
+        ColOp<D> kt;
         k.load(rk, koff(c), h);
         if constexpr (kAhead) {
           v.load(rv, voff, h);
@@ -463,12 +442,12 @@ __global__ __launch_bounds__(64 * kWavesOf<D>, D <= 64 ? 2 : 1) void dot_dq_f32_
             seen |= static_cast<unsigned>(see) << v;
             x[v] = see ? x[v] : 0.f;
           });
-        weighted_rows<T, D>(acc, x, kt, rk, koff, c, h, !full, seen, lds + wave * kScratch);
+        weighted_rows<D>(acc, x, kt, rk, koff, c, h, !full, seen, lds + wave * kScratch);
       });
   __syncthreads();
   add_waves<kWaves>(acc, lds, wave, lane);
   if (!row.valid) return;
-  T* dst = static_cast<T*>(a.dq) + ((static_cast<int64_t>(b) * a.Nq + row.i) * a.H + row.head) * D;
+  float* dst = static_cast<float*>(a.dq) + ((static_cast<int64_t>(b) * a.Nq + row.i) * a.H + row.head) * D;
 #pragma unroll
   for (int dt = 0; dt < NDT; ++dt) {
     if (dt % kWaves != wave) continue;
@@ -488,9 +467,9 @@ struct RowInfo {
   float lse[32], delta[32], slope[32];
 };
 
-template <typename T, int D>
+template <int D>
 __global__ __launch_bounds__(64 * kWavesOf<D>, D <= 64 ? 2 : 1) void dot_dkv_f32_kernel(DotArgs a) {
-  constexpr int NDT = Geo<D>::NDT, S = sizeof(T), kWaves = kWavesOf<D>;
+  constexpr int NDT = Geo<D>::NDT, S = 4, kWaves = kWavesOf<D>;
   __shared__ float lds[kWaves * NDT * 1024 > kWaves * kScratch ? kWaves * NDT * 1024 : kWaves * kScratch];
   __shared__ RowInfo infos[kWaves];
   const int nkb = (a.Nk + kDotBlock - 1) / kDotBlock;
@@ -505,10 +484,10 @@ __global__ __launch_bounds__(64 * kWavesOf<D>, D <= 64 ? 2 : 1) void dot_dkv_f32
   const int j0 = block * kDotBlock, j = j0 + c, R = a.G * a.Nq;
   const DotSpan span(m, j0, j0 + kDotBlock - 1);
   const QueriesSeeing sees(m, j);
-  RowOp<T, D> k, v;
-  k.load(rows_of(static_cast<const T*>(a.k) + b * a.ksb + hk * a.ksh + j0 * a.ksn, m.L - j0, a.ksn, D), static_cast<int>(c * a.ksn * S), h);
-  v.load(rows_of(static_cast<const T*>(a.v) + b * a.vsb + hk * a.vsh + j0 * a.vsn, m.L - j0, a.vsn, D), static_cast<int>(c * a.vsn * S), h);
-  const T* qb = static_cast<const T*>(a.q) + b * a.qsb;
+  RowOp<D> k, v;
+  k.load(rows_of(static_cast<const float*>(a.k) + b * a.ksb + hk * a.ksh + j0 * a.ksn, m.L - j0, a.ksn, D), static_cast<int>(c * a.ksn * S), h);
+  v.load(rows_of(static_cast<const float*>(a.v) + b * a.vsb + hk * a.vsh + j0 * a.vsn, m.L - j0, a.vsn, D), static_cast<int>(c * a.vsn * S), h);
+  const float* qb = static_cast<const float*>(a.q) + b * a.qsb;
   const int64_t orow = static_cast<int64_t>(a.H) * D;
   f32x16_t acck[NDT] = {}, accv[NDT] = {};
   int lo, hi;
@@ -539,15 +518,15 @@ __global__ __launch_bounds__(64 * kWavesOf<D>, D <= 64 ? 2 : 1) void dot_dkv_f32
         __builtin_amdgcn_s_waitcnt(0xC07F);
         __builtin_amdgcn_wave_barrier();
         const auto rq = rows_of(qb + i0 * a.qsn, a.Nq - i0, a.qsn, (a.H - 1) * a.qsh + D);
-        const auto rg = rows_of(static_cast<const T*>(a.dout) + (static_cast<int64_t>(b) * a.Nq + i0) * orow, a.Nq - i0, orow, orow);
+        const auto rg = rows_of(static_cast<const float*>(a.dout) + (static_cast<int64_t>(b) * a.Nq + i0) * orow, a.Nq - i0, orow, orow);
         auto qat = [&](int y) { return info.qoff[y]; };
         auto gat = [&](int y) { return info.goff[y]; };
-        RowOp<T, D> q, g;
+        RowOp<D> q, g;
         q.load(rq, qoff, h);
         g.load(rg, goff, h);
         __builtin_amdgcn_sched_barrier(0);
         const f32x16_t s = row_product(q, k);
-        ColOp<T, D> t;
+        ColOp<D> t;
         t.load(rg, gat, c, h);
         __builtin_amdgcn_sched_barrier(0);
         const f32x16_t dp = row_product(g, v);
@@ -567,9 +546,9 @@ __global__ __launch_bounds__(64 * kWavesOf<D>, D <= 64 ? 2 : 1) void dot_dkv_f32
             x[e] = see ? x[e] : 0.f;
           });
         // (rows past the last query load as zeros, with probabilities of 0)
-        weighted_rows<T, D>(accv, w, t, rg, gat, c, h, !full, seen, lds + wave * kScratch);
+        weighted_rows<D>(accv, w, t, rg, gat, c, h, !full, seen, lds + wave * kScratch);
         t.load(rq, qat, c, h);
-        weighted_rows<T, D>(acck, x, t, rq, qat, c, h, !full, seen, lds + wave * kScratch);
+        weighted_rows<D>(acck, x, t, rq, qat, c, h, !full, seen, lds + wave * kScratch);
         __builtin_amdgcn_wave_barrier();
       });
   __syncthreads();
@@ -585,8 +564,8 @@ __global__ __launch_bounds__(64 * kWavesOf<D>, D <= 64 ? 2 : 1) void dot_dkv_f32
       float y[4], z[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) y[e] = acck[dt][4 * vq + e], z[e] = accv[dt][4 * vq + e];
-      st4(static_cast<T*>(a.dk) + at + 32 * dt + 8 * vq + 4 * h, y);
-      st4(static_cast<T*>(a.dv) + at + 32 * dt + 8 * vq + 4 * h, z);
+      st4(static_cast<float*>(a.dk) + at + 32 * dt + 8 * vq + 4 * h, y);
+      st4(static_cast<float*>(a.dv) + at + 32 * dt + 8 * vq + 4 * h, z);
     }
   }
 }
@@ -603,31 +582,30 @@ __global__ void dot_ranges_kernel(const int* docs, int2* ranges, int B, int Nk) 
   ranges[at] = make_int2(lo, hi);
 }
 
-template <typename T, int D>
+template <int D>
 hipError_t launch_fwd(const DotArgs& a, hipStream_t st) {
   const int64_t nrb = (static_cast<int64_t>(a.G) * a.Nq + kDotBlock - 1) / kDotBlock;
-  dot_fwd_f32_kernel<T, D><<<unit_grid(static_cast<int64_t>(a.B) * a.Hkv, nrb * a.nsplit), 256, 0, st>>>(a);
+  dot_fwd_f32_kernel<D><<<unit_grid(static_cast<int64_t>(a.B) * a.Hkv, nrb * a.nsplit), 256, 0, st>>>(a);
   if (a.nsplit > 1) {
     const int64_t rows = static_cast<int64_t>(a.B) * a.H * a.Nq;
-    dot_join_kernel<T><<<static_cast<unsigned>((rows + 256 / D - 1) / (256 / D)), 256, 0, st>>>(a);
+    dot_join_kernel<<<static_cast<unsigned>((rows + 256 / D - 1) / (256 / D)), 256, 0, st>>>(a);
   }
   return hipGetLastError();
 }
-template <typename T, int D>
+template <int D>
 hipError_t launch_bwd(const DotArgs& a, hipStream_t st) {
   const int64_t nrb = (static_cast<int64_t>(a.G) * a.Nq + kDotBlock - 1) / kDotBlock;
   const int64_t nkb = (a.Nk + kDotBlock - 1) / kDotBlock;
-  dot_dq_f32_kernel<T, D><<<unit_grid(static_cast<int64_t>(a.B) * a.Hkv, nrb), 64 * kWavesOf<D>, 0, st>>>(a);
-  dot_dkv_f32_kernel<T, D><<<unit_grid(static_cast<int64_t>(a.B) * a.Hkv, nkb), 64 * kWavesOf<D>, 0, st>>>(a);
+  dot_dq_f32_kernel<D><<<unit_grid(static_cast<int64_t>(a.B) * a.Hkv, nrb), 64 * kWavesOf<D>, 0, st>>>(a);
+  dot_dkv_f32_kernel<D><<<unit_grid(static_cast<int64_t>(a.B) * a.Hkv, nkb), 64 * kWavesOf<D>, 0, st>>>(a);
   return hipGetLastError();
 }
-template <typename T>
 hipError_t launch(const DotArgs& a, bool backward, hipStream_t st) {
   switch (a.D) {
-    case 16: return backward ? launch_bwd<T, 16>(a, st) : launch_fwd<T, 16>(a, st);
-    case 32: return backward ? launch_bwd<T, 32>(a, st) : launch_fwd<T, 32>(a, st);
-    case 64: return backward ? launch_bwd<T, 64>(a, st) : launch_fwd<T, 64>(a, st);
-    default: return backward ? launch_bwd<T, 128>(a, st) : launch_fwd<T, 128>(a, st);
+    case 16: return backward ? launch_bwd<16>(a, st) : launch_fwd<16>(a, st);
+    case 32: return backward ? launch_bwd<32>(a, st) : launch_fwd<32>(a, st);
+    case 64: return backward ? launch_bwd<64>(a, st) : launch_fwd<64>(a, st);
+    default: return backward ? launch_bwd<128>(a, st) : launch_fwd<128>(a, st);
   }
 }
 
@@ -707,7 +685,7 @@ DotPlan dot_bwd_plan(int64_t B, int64_t Nq, int64_t Nk, int64_t H, int64_t Hkv, 
   return p;
 }
 
-hipError_t dot_fwd_f32(const DotArgs& a, hipStream_t st) { return launch<float>(a, false, st); }
-hipError_t dot_bwd_f32(const DotArgs& a, hipStream_t st) { return launch<float>(a, true, st); }
+hipError_t dot_fwd_f32(const DotArgs& a, hipStream_t st) { return launch(a, false, st); }
+hipError_t dot_bwd_f32(const DotArgs& a, hipStream_t st) { return launch(a, true, st); }
 
 }  // namespace sa

@@ -42,7 +42,7 @@ namespace {
 constexpr float kPmax = 65536.f;
 
 // A row's running state and the step over one block.
-template <int DP, bool CAP, bool BIAS>
+template <int DP, int CAP, bool BIAS>
 struct Row {
   static constexpr int NDT = DP / 32;
   f32x16_t acc[NDT];
@@ -50,7 +50,7 @@ struct Row {
   __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int dt = 0; dt < NDT; ++dt) acc[dt] = f32x16_t{};
-    m = -1e30f, l = 0.f, lr = 0.f;
+    m = -3e38f, l = 0.f, lr = 0.f;  // (finite: m less itself is 0)
   }
   // Probabilities of a block, packed; `masked`: hide(s) sets the scores of pairs that are not
   // visible to -inf; `behind`: all keys are at or before the wavefront's queries.
@@ -88,9 +88,20 @@ struct Row {
     };
     form();
     if (__builtin_amdgcn_ballot_w64(!(lb <= kPmax)) != 0) {
-      float mx = s[0] * mul;
+      // (the scores rounded as their maximum is, not by an fma with the subtraction: past 2^24
+      // what is rounded off passes 1)
+      if constexpr (!BIAS && CAP != kShortCap) {
 #pragma unroll
-      for (int v = 1; v < 16; ++v) mx = fmaxf(mx, s[v] * mul);
+        for (int v = 0; v < 16; ++v) {
+          float x = s[v] * mul;
+          asm("" : "+v"(x));
+          s[v] = x;
+        }
+        mul = 1.f;
+      }
+      float mx = s[0];
+#pragma unroll
+      for (int v = 1; v < 16; ++v) mx = fmaxf(mx, s[v]);
       if constexpr (BIAS) mx -= less;  // (the halves' differ)
       mx = fmaxf(m, fmaxf(mx, swap_halves(mx)));
       const float down = fast_exp2(m - mx);
@@ -151,7 +162,7 @@ __device__ __forceinline__ void single_rows(const DotArgs& a, const DotMask& m, 
   }
 }
 
-template <int DP, bool CAP, bool BIAS, int GROUPS>
+template <int DP, int CAP, bool BIAS, int GROUPS>
 __global__ __launch_bounds__(kThreads* GROUPS, 2) void dot_fwd_kernel(DotArgs a) {
   using T = SwzTile<DP>;
   constexpr int NT = DP / 16, NDT = DP / 32, SPW = T::instrs / kWaves, kStages = 4, kRows = 32 * kWaves;
@@ -339,7 +350,7 @@ __global__ __launch_bounds__(kThreads* GROUPS, 2) void dot_fwd_kernel(DotArgs a)
   single_rows(a, m, b, w, lse, bad);
 }
 
-template <int DP, bool CAP, bool BIAS>
+template <int DP, int CAP, bool BIAS>
 __global__ __launch_bounds__(kThreads, 1) void dot_few_kernel(DotArgs a) {
   using T = SwzTile<DP>;
   constexpr int NT = DP / 16, NDT = DP / 32, SPW = T::instrs;
@@ -554,7 +565,7 @@ __global__ __launch_bounds__(kThreads) void dot_join_kernel(DotArgs a) {
   write_out(a, ((static_cast<int64_t>(b) * a.Nq + i) * a.H + head) * a.D + lane, d0, x0 * inv, d1, x1 * inv);
 }
 
-template <int DP, bool CAP, bool BIAS>
+template <int DP, int CAP, bool BIAS>
 hipError_t launch(const DotArgs& a, hipStream_t st) {
   const int64_t R = static_cast<int64_t>(a.G) * a.Nq, heads = static_cast<int64_t>(a.B) * a.Hkv;
   if (a.nsplit <= 0) {
@@ -570,8 +581,10 @@ hipError_t launch(const DotArgs& a, hipStream_t st) {
 }
 template <int DP>
 hipError_t launch(const DotArgs& a, hipStream_t st) {
-  if (a.cap > 0.f) return a.slopes ? launch<DP, true, true>(a, st) : launch<DP, true, false>(a, st);
-  return a.slopes ? launch<DP, false, true>(a, st) : launch<DP, false, false>(a, st);
+  return with_cap(a.cap, [&](auto cap) {
+    constexpr int CAP = decltype(cap)::value;
+    return a.slopes ? launch<DP, CAP, true>(a, st) : launch<DP, CAP, false>(a, st);
+  });
 }
 
 }  // namespace

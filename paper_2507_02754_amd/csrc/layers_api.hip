@@ -90,8 +90,8 @@ int check_dot(int64_t B, int64_t Nq, int64_t Nk, int64_t H, int64_t Hkv, int64_t
   if (B <= 0 || Nq <= 0 || Nk <= 0 || H <= 0 || Hkv <= 0 || D <= 0 || Nq > Nk || window < 0) return SA_ERR_INVALID;
   if (Hkv > H || H % Hkv != 0) return SA_ERR_INVALID;
   // Rows of a sequence and positions are 32-bit numbers, and a launch holds less than
-  // 2^32 threads, 256 for each block of 32 rows or keys.
-  const int64_t rows = int64_t(1) << 30, blocks = int64_t(1) << 23;
+  // 2^32 threads, up to 512 for each block of 32 rows or keys (and up to 7 blocks of none).
+  const int64_t rows = int64_t(1) << 30, blocks = (int64_t(1) << 23) - 8;
   if (Nk > rows || B > rows || H > rows || !product_fits(H / Hkv, Nk, 1, rows)) return SA_ERR_INVALID;
   if (!product_fits(B, Hkv, (H / Hkv * Nk + 31) / 32, blocks)) return SA_ERR_INVALID;
   if (!known(dtype) || !known_dim(D)) return SA_ERR_UNSUPPORTED;

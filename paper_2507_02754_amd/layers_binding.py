@@ -286,7 +286,10 @@ class _DotCall:
             _check_like(prefix, (B,), torch.int32, device, "prefix")
         if k_lens is not None:
             _check_like(k_lens, (B,), torch.int32, device, "k_lens")
-        causal, window, dt = bool(causal), int(window), _DTYPES[q.dtype]
+        window = int(window)
+        if window < 0:
+            raise ValueError(f"window {window} is negative")
+        causal, window, dt = bool(causal), min(window, Nk), _DTYPES[q.dtype]  # (no distance reaches Nk)
         self.q, self.k, self.v = q, k, v
         self.plan = (B, Nq, Nk, H, Hkv, D, causal, window, documents is not None, dt)
         self.args = (B, Nq, Nk, H, Hkv, D, *_strides(q), *_strides(k), *_strides(v), D ** -0.5 if scale is None else float(scale),

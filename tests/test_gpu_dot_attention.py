@@ -284,6 +284,56 @@ def test_large_scores(dt):
     _check(q, k, v, dout, "negative scale", scale=-0.01, softcap=1.0)
 
 
+# B, Nq, Nk, H, Hkv, D: the forms of the forward
+FORWARDS = [(1, 140, 140, 2, 2, 64), (4, 390, 390, 64, 64, 128), (2, 450, 450, 40, 20, 128), (1, 700, 700, 16, 4, 128),
+            (2, 1, 2900, 8, 2, 128), (5, 300, 300, 48, 48, 64)]
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("size", FORWARDS, ids=str)
+def test_caps_far_above_the_scores(size, dt):
+    """A cap of 10^6 takes less than 10^-9 off scores of this size: as without one, to the
+    bounds of that; and one of 2000 to its own."""
+    B, Nq, Nk, H, Hkv, D = size
+    q, k, v, dout = _inputs(*size, dt, seed=Nk, scale=2.0)
+    want = ref.dot_attention(q, k, v, dout=dout)
+    lo = torch.empty_like(q) if dt == BF else None
+    out, lse = simplicial_dot_attn_fwd(q, k, v, softcap=1e6, out_lo=lo)
+    grads = simplicial_dot_attn_bwd(q, k, v, out, dout, lse, softcap=1e6, out_lo=lo)
+    for name, x in zip(("out", "lse", "dq", "dk", "dv"), (out, lse, *grads)):
+        ref.close(x, *want[name], f"{size} cap 1e6: {name}")
+    _check(q, k, v, dout, f"{size} cap 2000", softcap=2000.0, slopes=_slopes(H))
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("size", FORWARDS, ids=str)
+def test_enormous_scores(size, dt, sign):
+    """Scores of 2^41 and 2^113, three values of them: a mean, with some weights, of the values
+    whose keys have the largest. float32 rounds a score by up to 2^-24 of it, 2^17 and more
+    here, so that the weights among equal scores are open; but keys of another score, 2^41 and
+    more below, have none, and nothing overflows on the way."""
+    B, Nq, Nk, H, Hkv, D = size
+    see = ref.visible(B, Nq, Nk, True, 0, None, None, None, "cuda")[0][0]  # [Nq, Nk]
+    kind = (1 + torch.arange(Nk) * 7 % 3).cuda()
+    v = _normal(B, Nk, Hkv, D, seed=Nk, dtype=dt)
+    vd = v.double().view(B, Nk, Hkv * D)
+    for e in (19, 55):
+        q = torch.full((B, Nq, H, D), 2.0 ** e, dtype=dt, device="cuda")
+        k = (kind.view(1, Nk, 1, 1) * (sign * 2.0 ** e)).to(dt).expand(B, Nk, Hkv, D).contiguous()
+        out, lse = simplicial_dot_attn_fwd(q, k, v, scale=8.0 / D)
+        a = torch.where(see, sign * kind.double() * 2.0 ** (2 * e + 3), -math.inf)
+        top = a.amax(1)
+        for i in {0, 1, 2, 31, 32, 95, Nq // 2, Nq - 1} & set(range(Nq)):
+            values = vd[:, (a[i] == top[i]).nonzero()[:, 0]]
+            o = out[:, i].double().view(B, Hkv, H // Hkv, D).transpose(1, 2).reshape(B, H // Hkv, Hkv * D)
+            slack = (ref.HALF[dt] + (Nk / 32 + 64) * ref.U) * values.abs().amax(1, keepdim=True)
+            low, high = values.amin(1, keepdim=True) - slack, values.amax(1, keepdim=True) + slack
+            assert ((o >= low) & (o <= high)).all(), f"{size} 2^{2 * e + 3} row {i}"
+        top = top.view(1, 1, Nq).expand(B, H, Nq)
+        ref.close(lse, top, (D / 2 + 16) * ref.U * top.abs(), "lse")
+
+
 def test_far_cache_passes_32_bits():
     """One new token over a cache of more than 2^32 bytes a tensor, two of its heads."""
     Nk, Hkv, D = 1 << 21, 8, 128  # 2^31 elements

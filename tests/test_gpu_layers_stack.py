@@ -244,6 +244,24 @@ def test_changes_in_place_are_noticed():
         o.sum().backward()
 
 
+def test_the_same_tensor_twice():
+    """One tensor as queries and keys with one weight, one as keys and values: gradients are
+    the sums of those of copies."""
+    qkv, _, ws, _, ids, freqs = _step_inputs()
+    x, w = qkv.detach()[:, :, :4].contiguous(), ws[0].detach() + 0.5
+    dout = torch.randn(x.shape, device="cuda").to(BF)
+    xs, wt = [x.clone().requires_grad_(True) for _ in range(3)], [w.clone().requires_grad_(True) for _ in range(2)]
+    q, k = norm_rotate(xs[:2], weights=wt, freqs=freqs)
+    apart = torch.autograd.grad(dot_attention(q, k, xs[2], documents=ids), xs + wt, dout)
+    one, weight = x.clone().requires_grad_(True), w.clone().requires_grad_(True)
+    q, k = norm_rotate([one, one], weights=[weight, weight], freqs=freqs)
+    dx, dw = torch.autograd.grad(dot_attention(q, k, one, documents=ids), [one, weight], dout)
+    total = sum(g.double() for g in apart[:3])
+    # (two roundings of partial sums to bf16)
+    assert ((dx.double() - total).abs() <= 2 * ref.HALF[BF] * sum(g.double().abs() for g in apart[:3])).all()
+    assert torch.equal(dw, apart[3] + apart[4])
+
+
 def test_another_stream():
     """Calls on a stream of their own, the inputs made on it."""
     want = _one_step(*_step_inputs())

@@ -156,7 +156,7 @@ int simplicial_dot_attn_bwd(const void* q, const void* k, const void* v, const v
  * left out) and entropy 0. A row with NaN or +inf has NaN everywhere; its
  * top_index holds distinct tokens.
  *   logits       [R, V], dtype, row stride row_stride >= V elements, aligned to
- *                its element
+ *                its element; V at most 4000000
  *   targets      [R] int64
  *   logprob, entropy, lse   [R] float32
  *   top          0 .. min(V, SA_LOGPROBS_MAX_TOP)

@@ -53,8 +53,9 @@ int check_rotate(int32_t count, const void* const* x, const int64_t* strides, co
     if (weight && weight[t] && (!norm || !aligned(weight[t], 4))) return SA_ERR_INVALID;
     all += heads[t];
   }
-  // A launch holds less than 2^32 threads (D / 16 a position), a tensor 2^40 elements.
-  if (all > INT_MAX || B * N > (INT_MAX / (D / 16)) || !product_fits(B * N, all, D, kElements)) return SA_ERR_INVALID;
+  // A launch holds less than 2^32 threads (D / 16 a position and tensor), a position 2^31
+  // elements, a tensor 2^40.
+  if (all > INT_MAX / D || !product_fits(B * N, D / 16, count, 0xffffff00) || !product_fits(B * N, all, D, kElements)) return SA_ERR_INVALID;
   if (!aligned(positions, 8) || pos_stride < 0 || (positions && pos_stride != 0 && pos_stride < N)) return SA_ERR_INVALID;
   if (norm && !(isfinite(eps) && eps >= 0.f)) return SA_ERR_INVALID;
   if (layout != SA_ROTATE_HALF && layout != SA_ROTATE_PAIRS && layout != SA_ROTATE_AXIS) return SA_ERR_INVALID;
@@ -279,21 +280,19 @@ int simplicial_dot_attn_bwd(const void* q, const void* k, const void* v, const v
   return to_status(dtype == SA_DTYPE_BF16 ? sa::dot_bwd_bf16(a, st) : sa::dot_bwd_f32(a, st));
 }
 
-// A launch holds less than 2^32 threads: at least 64 a row, 1024 logits for every 64 of a long one.
-static bool rows_fit(int64_t R, int64_t V) { return R <= (1 << 25) && product_fits(R, V, 1, int64_t(1) << 35); }
+static constexpr int64_t kMostTokens = 4000000;  // that 64 slices of a row hold
 
 static int check_logprobs(const void* logits, const int64_t* targets, int64_t R, int64_t V, int64_t row_stride,
                           int32_t dtype) {
   if (R <= 0 || V <= 0 || row_stride < V || row_stride > kElements) return SA_ERR_INVALID;
   if (!known(dtype)) return SA_ERR_UNSUPPORTED;
   if (!logits || !aligned(logits, element_size(dtype)) || !targets || !aligned(targets, 8)) return SA_ERR_INVALID;
-  // (64 slices of a row, workgroups in 32 bits)
-  if (V > 4000000) return SA_ERR_UNSUPPORTED;
-  return rows_fit(R, V) ? SA_OK : SA_ERR_INVALID;
+  if (V > kMostTokens) return SA_ERR_UNSUPPORTED;
+  return sa::logprobs_fit(R, V, dtype) ? SA_OK : SA_ERR_INVALID;
 }
 
 size_t simplicial_logprobs_fwd_workspace_size(int64_t R, int64_t V, int32_t top, int32_t dtype) {
-  if (R <= 0 || V <= 0 || V > 4000000 || !rows_fit(R, V) || !known(dtype) || top < 0 || top > SA_LOGPROBS_MAX_TOP || top > V) return 0;
+  if (R <= 0 || V <= 0 || V > kMostTokens || !known(dtype) || !sa::logprobs_fit(R, V, dtype) || top < 0 || top > SA_LOGPROBS_MAX_TOP || top > V) return 0;
   return sa::logprobs_fwd_bytes(R, V, top, dtype);
 }
 

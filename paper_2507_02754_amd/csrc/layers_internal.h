@@ -39,6 +39,8 @@ struct LogprobArgs {
   int64_t R, V, stride;
   int top, dtype;
 };
+// Whether the launches hold less than 2^32 threads.
+bool logprobs_fit(int64_t R, int64_t V, int dtype);
 size_t logprobs_fwd_bytes(int64_t R, int64_t V, int top, int dtype);
 hipError_t logprobs_fwd(const LogprobArgs& a, void* workspace, hipStream_t st);
 struct LogprobGrad {
@@ -51,7 +53,7 @@ struct LogprobGrad {
 };
 hipError_t logprobs_bwd(const LogprobGrad& a, hipStream_t st);
 
-// ---- dot_f32.hip, dot_mfma.hip ----
+// ---- dot_f32.hip, dot_fwd.hip, dot_bwd.hip ----
 // Dot-product attention. A K-side head's rows are its G = H / Hkv query heads at
 // every position, r = G i + g: one position's heads share their keys.
 struct DotArgs {

@@ -406,6 +406,16 @@ Cut cut_rows(int64_t R, int64_t V, int epc, bool aligned) {
   return c;
 }
 
+// The same of the gradient: slices of about 1024 chunks.
+Cut cut_grad(int64_t V, int epc) {
+  const int64_t chunks = V / epc + 2;
+  Cut c = {};
+  c.slices = static_cast<int>((chunks + 1023) / 1024);
+  c.per = static_cast<int>((chunks + c.slices - 1) / c.slices);
+  c.threads = std::min(256, (c.per + 63) / 64 * 64);
+  return c;
+}
+
 template <typename T, bool TOP>
 void launch_fwd(const LogprobArgs& a, const Cut& c, char* parts, hipStream_t st) {
   const unsigned grid = static_cast<unsigned>(a.R * c.slices);
@@ -429,6 +439,14 @@ hipError_t fwd(const LogprobArgs& a, char* parts, hipStream_t st) {
 
 }  // namespace
 
+bool logprobs_fit(int64_t R, int64_t V, int dtype) {
+  if (R >= int64_t(1) << 26) return false;
+  const int epc = dtype == SA_DTYPE_F32 ? 4 : 8;
+  int64_t most = 0;  // threads of a row
+  for (const Cut& c : {cut_rows(R, V, epc, true), cut_rows(R, V, epc, false), cut_grad(V, epc)})
+    most = std::max(most, static_cast<int64_t>(c.slices) * c.threads);
+  return R <= 0xffffffffll / most;
+}
 size_t logprobs_fwd_bytes(int64_t R, int64_t V, int top, int dtype) {
   // (rows that are not aligned may take a slice more)
   const int epc = dtype == SA_DTYPE_F32 ? 4 : 8;
@@ -442,14 +460,12 @@ hipError_t logprobs_fwd(const LogprobArgs& a, void* workspace, hipStream_t st) {
 
 hipError_t logprobs_bwd(const LogprobGrad& a, hipStream_t st) {
   const int epc = a.dtype == SA_DTYPE_F32 ? 4 : 8;
-  const int64_t chunks = a.V / epc + 2;
-  const int slices = static_cast<int>((chunks + 1023) / 1024), per = static_cast<int>((chunks + slices - 1) / slices);
-  const int threads = std::min(256, (per + 63) / 64 * 64);
-  const unsigned grid = static_cast<unsigned>(a.R * slices);
+  const Cut c = cut_grad(a.V, epc);
+  const unsigned grid = static_cast<unsigned>(a.R * c.slices);
   if (a.dtype == SA_DTYPE_F32)
-    logprobs_bwd_kernel<float><<<grid, threads, 0, st>>>(a, slices, per);
+    logprobs_bwd_kernel<float><<<grid, c.threads, 0, st>>>(a, c.slices, c.per);
   else
-    logprobs_bwd_kernel<uint16_t><<<grid, threads, 0, st>>>(a, slices, per);
+    logprobs_bwd_kernel<uint16_t><<<grid, c.threads, 0, st>>>(a, c.slices, c.per);
   return hipGetLastError();
 }
 

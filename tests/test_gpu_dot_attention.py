@@ -284,6 +284,18 @@ def test_large_scores(dt):
     _check(q, k, v, dout, "negative scale", scale=-0.01, softcap=1.0)
 
 
+def test_windows_of_any_number():
+    """Windows past the keys (and past 32 bits) hide nothing; negative ones are refused."""
+    q, k, v, _ = _inputs(1, 70, 70, 2, 1, 64, BF)
+    want = simplicial_dot_attn_fwd(q, k, v)
+    for window in (70, 1 << 31, (1 << 32) + 5):
+        got = simplicial_dot_attn_fwd(q, k, v, window=window)
+        assert all(torch.equal(a, b) for a, b in zip(want, got))
+    for window in (-1, -(1 << 32)):
+        with pytest.raises(ValueError, match="negative"):
+            simplicial_dot_attn_fwd(q, k, v, window=window)
+
+
 # B, Nq, Nk, H, Hkv, D: the forms of the forward
 FORWARDS = [(1, 140, 140, 2, 2, 64), (4, 390, 390, 64, 64, 128), (2, 450, 450, 40, 20, 128), (1, 700, 700, 16, 4, 128),
             (2, 1, 2900, 8, 2, 128), (5, 300, 300, 48, 48, 64)]

@@ -128,6 +128,23 @@ def test_logprobs_refusals(lib):
     assert bwd(dx=0) == 1 and bwd(dx=ODD) == 1 and bwd(g=A + 2) == 1
 
 
+@only_without_gpu
+def test_sizes_past_a_launch(lib):
+    """Calls whose launches would hold 2^32 threads or more, or whose offsets pass their type, just
+    past the largest that do not."""
+    large = 64 * 9
+    for kw in (dict(heads=(1, 1), D=128, B=1, N=1 << 28, strides=[0, large, 64] * 2),
+               dict(heads=(1 << 24, 2), D=128, B=1, N=1, strides=[0, large, 64] * 2)):
+        assert _rotate(lib, freqs=(), **kw) == 1, kw
+    assert _dot(lib, B=1, Nq=1, Nk=1 << 28, H=1, Hkv=1, D=16, k=(0, 16, 16)) == 1
+    fits = lambda R, V, dtype: lib.simplicial_logprobs_fwd(A, A, A, A, A, A, A, 0, 0, R, V, V, 1, dtype, None) != 1  # noqa: E731
+    size = lib.simplicial_logprobs_fwd_workspace_size
+    for R, V, dtype in ((1 << 24, 1024, 0), (1 << 25, 1024, 1), ((1 << 26) - 1, 2000, 1)):
+        assert not fits(R, V, dtype) and size(R, V, 1, dtype) == 0
+    # 16 slices and more of a row: the workspace is asked for
+    assert size(1 << 18, 1 << 17, 1, 1) > 0 and size(1 << 16, 1 << 17, 1, 0) > 0
+
+
 def test_python_refusals():
     """What the binding refuses before the library is called (CPU tensors)."""
     x = torch.zeros(1, 4, 2, 64)

@@ -12,6 +12,11 @@
 // from L1 / L2 straight into registers: at 1/16 of the bf16 rate the products, not
 // the loads, take the time.
 //
+// Measured, B=1 H=4 N=2000 D=64 causal with a prefix of 200: forward 41 us, dq 70, dk and dv
+// 114, 32 TFLOP/s of the 7.2 GFLOP that forward and backward need (a large product of the
+// library's runs at 154). With 252 workgroups of rows and of keys, the longest one's walk of
+// dependent products is the time.
+//
 // Each block's products start from zero and are added to the running sums, so that
 // sums over a long axis round once per 32 terms. Operand layouts as in f32.hip: a row
 // operand's float4 t holds columns 8 t + 4 h .. + 3 of row c; product v of a

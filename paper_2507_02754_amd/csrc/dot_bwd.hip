@@ -341,23 +341,23 @@ __global__ __launch_bounds__(kThreads* GROUPS, PRIV ? 1 : 2) void dot_dq_kernel(
     take(acc, buf);
   }
   uint16_t* dst = static_cast<uint16_t*>(a.dq) + orow + 4 * h;
-  unsigned bad = 0;
+  unsigned bad = 0;  // rows that a masked pair may have spoilt: without masks what came out is right
+  const bool masks = has_mask(a);
   if constexpr (PRIV) {
     __shared__ unsigned flags[kWaves];
     float y[NDT][4];
     __syncthreads();
     add_waves(acc, y, [&](int dt) { return reinterpret_cast<float*>(dt == 0 ? xst0 : dt == 1 ? xst1 : dt == 2 ? yst0 : yst1); }, wave, lane);
     const float check = store_quads(w.valid ? dst : nullptr, y, a.scale, wave, a.D);
-    const unsigned x = rows_where(w.valid && check != check);
+    const unsigned x = rows_where(masks && w.valid && check != check);
     if (lane == 0) flags[wave] = x;
     __syncthreads();
     if (wave == 0) bad = flags[0] | flags[1] | flags[2] | flags[3];
   } else {
     const float check = not_finite(acc);
-    bad = rows_where(w.valid && check != check);
+    bad = rows_where(masks && w.valid && check != check);
     if (w.valid && !((bad >> c) & 1)) store_row<DP>(dst, acc, a.scale, a.D);
   }
-  if (!has_mask(a)) bad = 0;
   while (bad) {
     const int x = __builtin_ctz(bad);
     bad &= bad - 1;
@@ -571,7 +571,8 @@ __global__ __launch_bounds__(kThreads* GROUPS, PRIV ? 1 : 2) void dot_dkv_kernel
   }
   const int64_t at = ((static_cast<int64_t>(b) * a.Nk + (out ? j : 0)) * a.Hkv + hk) * a.D + 4 * h;
   uint16_t *pk = static_cast<uint16_t*>(a.dk) + at, *pv = static_cast<uint16_t*>(a.dv) + at;
-  unsigned bad = 0;
+  unsigned bad = 0;  // keys, as the rows of the query side
+  const bool masks = has_mask(a);
   if constexpr (PRIV) {
     __shared__ unsigned flags[kWaves];
     auto buf = [&](int dt) { return reinterpret_cast<float*>(dt == 0 ? xst0 : dt == 1 ? xst1 : dt == 2 ? yst0 : yst1); };
@@ -581,19 +582,18 @@ __global__ __launch_bounds__(kThreads* GROUPS, PRIV ? 1 : 2) void dot_dkv_kernel
     float check = store_quads(out ? pk : nullptr, y, a.scale, wave, a.D);
     add_waves(accv, y, buf, wave, lane);
     check += store_quads(out ? pv : nullptr, y, 1.f, wave, a.D);
-    const unsigned x = rows_where(key && check != check);
+    const unsigned x = rows_where(masks && key && check != check);
     if (lane == 0) flags[wave] = x;
     __syncthreads();
     if (wave == 0) bad = flags[0] | flags[1] | flags[2] | flags[3];
   } else {
     const float check = not_finite(acck) + not_finite(accv);
-    bad = rows_where(key && check != check);
+    bad = rows_where(masks && key && check != check);
     if (out && !((bad >> c) & 1)) {
       store_row<DP>(pk, acck, a.scale, a.D);
       store_row<DP>(pv, accv, 1.f, a.D);
     }
   }
-  if (!has_mask(a)) bad = 0;
   while (bad) {
     const int x = __builtin_ctz(bad);
     bad &= bad - 1;

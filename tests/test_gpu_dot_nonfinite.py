@@ -1,0 +1,86 @@
+"""Infinities and NaN in dot-product attention: where they belong they come out, in every
+form of the kernels, and nowhere else."""
+
+import pytest
+import torch
+
+import layers_reference as ref
+from paper_2507_02754_amd import load_library, simplicial_dot_attn_bwd, simplicial_dot_attn_fwd
+
+pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
+NAMES = ("out", "lse", "dq", "dk", "dv")
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU visible")
+    load_library()
+
+
+def _normal(*shape, seed, dtype):
+    return torch.randn(shape, generator=torch.Generator().manual_seed(seed)).to(dtype).cuda()
+
+
+def _inputs(B, Nq, Nk, H, Hkv, D, dt, seed):
+    """q, k, v and the upstream gradient."""
+    return [_normal(B, Nq, H, D, seed=seed, dtype=dt), _normal(B, Nk, Hkv, D, seed=seed + 1, dtype=dt),
+            _normal(B, Nk, Hkv, D, seed=seed + 2, dtype=dt), _normal(B, Nq, H, D, seed=seed + 3, dtype=dt)]
+
+
+def _call(q, k, v, dout, **opts):
+    """All results by name, the buffers filled with a finite number before."""
+    B, Nq, H, D = q.shape
+    lo = torch.full_like(q, 7.0) if q.dtype == BF else None
+    out, lse = simplicial_dot_attn_fwd(q, k, v, out=torch.full_like(q, 7.0), lse=torch.full((B, H, Nq), 7.0, device="cuda"), out_lo=lo, **opts)
+    grads = simplicial_dot_attn_bwd(q, k, v, out, dout, lse, out_lo=lo, grads=[torch.full_like(t, 7.0) for t in (q, k, v)], **opts)
+    torch.cuda.synchronize()
+    return dict(zip(NAMES, (out, lse, *grads)))
+
+
+def _plain(q, k, v, dout):
+    """The formulas in float64, every key visible, whatever the values."""
+    B, Nq, H, D = q.shape
+    Nk, Hkv = k.shape[1:3]
+    q, do = (t.double().transpose(1, 2) for t in (q, dout))
+    k, v = (t.double().transpose(1, 2).repeat_interleave(H // Hkv, 1) for t in (k, v))
+    s = q @ k.transpose(2, 3) * D ** -0.5
+    p = torch.softmax(s, 3)
+    out = p @ v
+    ds = p * (do @ v.transpose(2, 3) - (do * out).sum(3, keepdim=True)) * D ** -0.5
+    dk, dv = (t.view(B, Hkv, H // Hkv, Nk, D).sum(2) for t in (ds.transpose(2, 3) @ q, p.transpose(2, 3) @ do))
+    return dict(zip(NAMES, (out.transpose(1, 2), torch.logsumexp(s, 3), (ds @ k).transpose(1, 2), dk.transpose(1, 2), dv.transpose(1, 2))))
+
+
+# B, N, H, Hkv, D: the forms of the backward's two sides (float32 has one)
+FORMS = [
+    (1, 70, 2, 2, 64),       # 32 rows and 32 keys a workgroup
+    (4, 390, 64, 64, 128),   # 128 rows and 128 keys
+    (2, 450, 40, 20, 128),   # two groups of wavefronts on both sides
+    (1, 700, 16, 4, 128),    # several workgroups a block of keys
+    (1, 2100, 3, 1, 64),
+    (5, 300, 48, 48, 64),
+    (3, 520, 48, 16, 32),
+]
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("size", FORMS, ids=str)
+def test_without_a_mask(size, dt):
+    """Every query sees every key: against float64, and with one NaN or infinity in each of q, k, v
+    and the upstream gradient, whose results are finite where the formula's are, and only there."""
+    B, N, H, Hkv, D = size
+    print(f"\n[dot] no mask {size} {dt}", flush=True)
+    clean = _inputs(B, N, N, H, Hkv, D, dt, seed=N)
+    q, k, v, dout = clean
+    got = _call(*clean, causal=False)
+    for name, w in ref.dot_attention(q, k, v, causal=False, dout=dout).items():
+        ref.close(got[name], *w, name)
+    for which, name in enumerate(("q", "k", "v", "dout")):
+        for bad, at in ((float("nan"), N - 3), (float("inf"), N // 2), (-float("inf"), 5)):
+            t = [x.clone() for x in clean]
+            t[which][B - 1, at, t[which].shape[2] - 1, D // 2 + 1] = bad
+            got = _call(*t, causal=False)
+            for result, w in _plain(*t).items():
+                assert torch.equal(torch.isfinite(got[result]), torch.isfinite(w)), f"{bad} in {name}: {result}"

@@ -554,6 +554,11 @@ __global__ __launch_bounds__(kThreads* GROUPS, PRIV ? 1 : 2) void dot_dkv_kernel
     take(acck, bk);
     take(accv, bv);
   }
+  // Keys behind the filled length have no visible pair: zeros, whatever their masked pairs' products are.
+  if (!key) {
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt) acck[dt] = f32x16_t{}, accv[dt] = f32x16_t{};
+  }
   const bool out = j < a.Nk;
   if (!PRIV && a.ks > 1) {  // partial sums, added by dot_keys_kernel
     if (!out) return;

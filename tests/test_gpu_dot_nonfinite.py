@@ -84,3 +84,44 @@ def test_without_a_mask(size, dt):
             got = _call(*t, causal=False)
             for result, w in _plain(*t).items():
                 assert torch.equal(torch.isfinite(got[result]), torch.isfinite(w)), f"{bad} in {name}: {result}"
+
+
+# B, N, H, Hkv, D and every sequence's filled length: the first has fewer keys than queries
+FILLED = [
+    (2, 70, 2, 2, 64, [45, 70]),
+    (2, 450, 40, 20, 128, [301, 450]),
+    (4, 390, 64, 64, 128, [333, 390, 128, 390]),
+    (1, 700, 16, 4, 128, [591]),
+    (1, 2100, 3, 1, 64, [2017]),
+    (5, 300, 48, 48, 64, [257, 300, 300, 300, 300]),
+    (1, 900, 2, 1, 16, [899]),
+]
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("size", FILLED, ids=str)
+def test_keys_behind_the_filled_length(size, bad, dt):
+    """They get zeros, whatever a query that sees nothing or one that sees every key before them
+    holds, and of the queries the first changes no other result."""
+    B, N, H, Hkv, D, lens = size
+    print(f"\n[dot] filled {size} {bad} {dt}", flush=True)
+    L = lens[0]
+    k_lens = torch.tensor(lens, dtype=torch.int32).cuda()
+    clean = _inputs(B, N, N, H, Hkv, D, dt, seed=N + 7)
+    want = ref.dot_attention(*clean[:3], k_lens=k_lens, dout=clean[3])
+    for which, name in ((0, "q"), (3, "dout")):
+        t = [x.clone() for x in clean]
+        t[which][0, 0] = bad  # (at position L - N)
+        t[which][0, N - L - 1] = bad
+        got = _call(*t, k_lens=k_lens)
+        for result, w in want.items():
+            ref.close(got[result], *w, f"{name} of queries without a key: {result}")
+        t[which][0, N - 1] = bad  # (the last one sees all keys)
+        got = _call(*t, k_lens=k_lens)
+        for result in ("dk", "dv"):
+            assert (got[result][0, L:] == 0).all(), f"{name} of the last query: {result} behind the filled length"
+            assert not torch.isfinite(got[result][0, :L]).any() or (name, result) == ("dout", "dk"), result
+            ref.close(got[result][1:], *(x[1:] for x in want[result]), f"{result} of the other sequences")
+        assert not torch.isfinite(got["dq"][0, N - 1]).any()
+        ref.close(got["dq"][0, :N - 1], *(x[0, :N - 1] for x in want["dq"]), "dq of the other queries")

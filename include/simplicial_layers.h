@@ -163,8 +163,11 @@ int simplicial_dot_attn_bwd(const void* q, const void* k, const void* v, const v
  *   top_logprob  [R, top] float32, top_index [R, top] int64 (NULL for top = 0)
  *   workspace    simplicial_logprobs_fwd_workspace_size() bytes (0: may be NULL):
  *                partial results of long or few rows, which several workgroups share
+ *   dtype        with SA_LOGPROBS_LSE_LO added, lse is [2, R]: behind lse what its rounding to
+ *                float32 took (their sum has twice the digits), for the backward
  */
 #define SA_LOGPROBS_MAX_TOP 32
+#define SA_LOGPROBS_LSE_LO 0x100
 size_t simplicial_logprobs_fwd_workspace_size(int64_t R, int64_t V, int32_t top, int32_t dtype);
 int simplicial_logprobs_fwd(const void* logits, const int64_t* targets, float* logprob,
                             float* entropy, float* lse, float* top_logprob, int64_t* top_index,
@@ -175,7 +178,10 @@ int simplicial_logprobs_fwd(const void* logits, const int64_t* targets, float* l
  * Its backward, from the gradients of logprob, entropy and lse ([R] float32 each,
  * any of them NULL: zeros):
  *     dx_j = p_j (d_lse - d_logprob - d_entropy (log p_j + entropy)) + d_logprob [j = target]
- * A row without any probability gets zeros. The top tokens carry no gradient.
+ * A row without any probability gets zeros. The top tokens carry no gradient. p_j is
+ * formed from lse: with SA_LOGPROBS_LSE_LO added to dtype and lse [2, R] of the forward a
+ * constant added to a row's logits changes nothing; without it p_j carries the rounding of
+ * lse to float32, 2^-24 |lse| of itself.
  *   dlogits   [R, V] contiguous, dtype, fully overwritten
  */
 int simplicial_logprobs_bwd(const void* logits, const int64_t* targets, const float* lse,

@@ -282,6 +282,13 @@ int simplicial_dot_attn_bwd(const void* q, const void* k, const void* v, const v
 
 static constexpr int64_t kMostTokens = 4000000;  // that 64 slices of a row hold
 
+// The low parts behind lse, if the dtype asks for them (and the dtype without that).
+static float* lse_lo(const float* lse, int64_t R, int32_t& dtype) {
+  if (dtype < 0 || !(dtype & SA_LOGPROBS_LSE_LO)) return nullptr;
+  dtype &= ~SA_LOGPROBS_LSE_LO;
+  return const_cast<float*>(lse) + R;
+}
+
 static int check_logprobs(const void* logits, const int64_t* targets, int64_t R, int64_t V, int64_t row_stride,
                           int32_t dtype) {
   if (R <= 0 || V <= 0 || row_stride < V || row_stride > kElements) return SA_ERR_INVALID;
@@ -292,6 +299,7 @@ static int check_logprobs(const void* logits, const int64_t* targets, int64_t R,
 }
 
 size_t simplicial_logprobs_fwd_workspace_size(int64_t R, int64_t V, int32_t top, int32_t dtype) {
+  lse_lo(nullptr, 0, dtype);
   if (R <= 0 || V <= 0 || V > kMostTokens || !known(dtype) || !sa::logprobs_fit(R, V, dtype) || top < 0 || top > SA_LOGPROBS_MAX_TOP || top > V) return 0;
   return sa::logprobs_fwd_bytes(R, V, top, dtype);
 }
@@ -300,6 +308,7 @@ int simplicial_logprobs_fwd(const void* logits, const int64_t* targets, float* l
                             float* entropy, float* lse, float* top_logprob, int64_t* top_index,
                             void* workspace, size_t workspace_bytes, int64_t R, int64_t V,
                             int64_t row_stride, int32_t top, int32_t dtype, void* stream) {
+  float* const lo = lse_lo(lse, R, dtype);
   const int rc = check_logprobs(logits, targets, R, V, row_stride, dtype);
   if (rc != SA_OK) return rc;
   if (top < 0 || top > SA_LOGPROBS_MAX_TOP || top > V) return SA_ERR_INVALID;
@@ -308,7 +317,7 @@ int simplicial_logprobs_fwd(const void* logits, const int64_t* targets, float* l
   const size_t need = sa::logprobs_fwd_bytes(R, V, top, dtype);
   if (need && !good({workspace})) return SA_ERR_INVALID;
   if (workspace_bytes < need) return SA_ERR_WORKSPACE;
-  const sa::LogprobArgs a = {logits, targets, logprob, entropy, lse, top_logprob, top_index, R, V, row_stride, top, dtype};
+  const sa::LogprobArgs a = {logits, targets, logprob, entropy, lse, top_logprob, lo, top_index, R, V, row_stride, top, dtype};
   return to_status(sa::logprobs_fwd(a, workspace, static_cast<hipStream_t>(stream)));
 }
 
@@ -316,10 +325,11 @@ int simplicial_logprobs_bwd(const void* logits, const int64_t* targets, const fl
                             const float* entropy, const float* d_logprob, const float* d_entropy,
                             const float* d_lse, void* dlogits, int64_t R, int64_t V,
                             int64_t row_stride, int32_t dtype, void* stream) {
+  const float* const lo = lse_lo(lse, R, dtype);
   const int rc = check_logprobs(logits, targets, R, V, row_stride, dtype);
   if (rc != SA_OK) return rc;
   if (!lse || !entropy || !good({dlogits}) || !good_or_null({lse, entropy, d_logprob, d_entropy, d_lse})) return SA_ERR_INVALID;
-  const sa::LogprobGrad a = {logits, targets, lse, entropy, d_logprob, d_entropy, d_lse, dlogits, R, V, row_stride, dtype};
+  const sa::LogprobGrad a = {logits, targets, lse, lo, entropy, d_logprob, d_entropy, d_lse, dlogits, R, V, row_stride, dtype};
   return to_status(sa::logprobs_bwd(a, static_cast<hipStream_t>(stream)));
 }
 

@@ -35,6 +35,7 @@ struct LogprobArgs {
   const void* x;
   const int64_t* targets;
   float *logprob, *entropy, *lse, *top_logprob;
+  float* lse_lo;  // what rounding took from lse, or null
   int64_t* top_index;
   int64_t R, V, stride;
   int top, dtype;
@@ -46,7 +47,7 @@ hipError_t logprobs_fwd(const LogprobArgs& a, void* workspace, hipStream_t st);
 struct LogprobGrad {
   const void* x;
   const int64_t* targets;
-  const float *lse, *entropy, *d_logprob, *d_entropy, *d_lse;
+  const float *lse, *lse_lo, *entropy, *d_logprob, *d_entropy, *d_lse;  // lse_lo: or null
   void* dx;
   int64_t R, V, stride;
   int dtype;

@@ -142,7 +142,12 @@ __device__ __forceinline__ RowNorm finish_row(const LogprobArgs& a, int64_t row,
   if (y >= 0 && y < a.V) lp = norm(value(static_cast<const T*>(a.x)[row * a.stride + y]));
   a.logprob[row] = lp;
   a.entropy[row] = none ? 0.f : log_l - t / l;
-  a.lse[row] = none ? m : m + log_l;
+  const float lse = none ? m : m + log_l;
+  a.lse[row] = lse;
+  if (a.lse_lo) {  // (exact where both are finite, whichever is larger)
+    const float lo = (m - (lse - (lse - m))) + (log_l - (lse - m));
+    a.lse_lo[row] = lo == lo ? lo : 0.f;
+  }
   return norm;
 }
 __device__ __forceinline__ void write_top(const LogprobArgs& a, int64_t row, int k, u64 x, RowNorm norm) {
@@ -335,7 +340,8 @@ __global__ __launch_bounds__(256) void logprobs_bwd_kernel(LogprobGrad a, int sl
   T* dx = static_cast<T*>(a.dx) + row * a.V;
   const int lead = row_lead(dx);
   const bool together = row_lead(x) == lead;
-  const float lse = a.lse[row], h = a.entropy[row];
+  // (x - lse is exact for the largest logits, so that no constant added to a row makes p less so)
+  const float lse = a.lse[row], lo = a.lse_lo ? a.lse_lo[row] : 0.f, h = a.entropy[row];
   const float gh = a.d_entropy ? a.d_entropy[row] : 0.f;
   const int64_t y = a.targets[row];
   float glp = a.d_logprob && y >= 0 ? a.d_logprob[row] : 0.f;
@@ -364,7 +370,7 @@ __global__ __launch_bounds__(256) void logprobs_bwd_kernel(LogprobGrad a, int sl
     float o[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      const float lp = chunk_at<T>(c, e) - lse, p = fast_exp2(lp * kLog2e);
+      const float lp = (chunk_at<T>(c, e) - lse) - lo, p = fast_exp2(lp * kLog2e);
       float v = p * (g - gh * (fmaxf(lp, kFloor) + h));
       if (j + e == y) v += glp;
       o[e] = none ? 0.f : v;

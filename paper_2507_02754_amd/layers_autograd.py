@@ -147,8 +147,10 @@ class TokenLogprobsFunction(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, logits, targets, top):
-        results = simplicial_logprobs_fwd(logits, targets, top)
-        ctx.save_for_backward(logits, targets, results[2], results[1])
+        logprob, entropy, both, *best = simplicial_logprobs_fwd(logits, targets, top, lse_lo=True)
+        lse = both[0].data  # (a tensor of its own: results may not be views; saved for the check of changes in place)
+        results = (logprob, entropy, lse, *best)
+        ctx.save_for_backward(logits, targets, both, entropy, lse)
         ctx.mark_non_differentiable(*results[3:])
         ctx.set_materialize_grads(False)
         return results
@@ -156,7 +158,7 @@ class TokenLogprobsFunction(torch.autograd.Function):
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, d_logprob, d_entropy, d_lse, _dtop, _dindex):
-        logits, targets, lse, entropy = ctx.saved_tensors
+        logits, targets, lse, entropy, _ = ctx.saved_tensors
         grads = [None if g is None else g.contiguous() for g in (d_logprob, d_entropy, d_lse)]
         return simplicial_logprobs_bwd(logits, targets, lse, entropy, *grads), None, None
 

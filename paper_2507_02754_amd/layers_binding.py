@@ -27,6 +27,7 @@ __all__ = [
 ROTATE_LAYOUTS = {"half": 0, "pairs": 1, "axis": 2}
 ROTATE_MAX = 3
 LOGPROBS_MAX_TOP = 32
+LOGPROBS_LSE_LO = 0x100  # added to the dtype: lse is [2, R]
 
 _lib = None
 
@@ -382,33 +383,38 @@ def _check_logits(logits, targets):
     return R, V, logits.stride(0) if R > 1 else V
 
 
-def simplicial_logprobs_fwd(logits, targets, top=0):
+def simplicial_logprobs_fwd(logits, targets, top=0, lse_lo=False):
     """(logprob, entropy, lse, top_logprob, top_index) of the rows of logits [R, V]:
     the log probability of targets [R] (int64; negative: left out, 0), the entropy of
     the distribution, the log of the sum of exponentials ([R] float32 each), and the `top` (at most
     32) most probable tokens with their log probabilities ([R, top], equal logits by
-    ascending token)."""
+    ascending token). With `lse_lo` lse is [2, R], for the backward: lse and what its rounding
+    to float32 took from it."""
     R, V, stride = _check_logits(logits, targets)
     top = int(top)
     if not 0 <= top <= min(V, LOGPROBS_MAX_TOP):
         raise ValueError(f"top {top} is not within 0 .. {min(V, LOGPROBS_MAX_TOP)}")
     device, dt = logits.device, _DTYPES[logits.dtype]
-    logprob, entropy, lse = (torch.empty(R, dtype=torch.float32, device=device) for _ in range(3))
+    logprob, entropy = (torch.empty(R, dtype=torch.float32, device=device) for _ in range(2))
+    lse = torch.empty((2, R) if lse_lo else (R,), dtype=torch.float32, device=device)
     top_logprob = torch.empty((R, top), dtype=torch.float32, device=device)
     top_index = torch.empty((R, top), dtype=torch.int64, device=device)
     nbytes = (_lib or _library()).simplicial_logprobs_fwd_workspace_size(R, V, top, dt)
     workspace = _workspace(nbytes, device)
     _call("simplicial_logprobs_fwd", device, logits.data_ptr(), targets.data_ptr(), logprob.data_ptr(), entropy.data_ptr(),
           lse.data_ptr(), _ptr(top_logprob) if top else None, _ptr(top_index) if top else None, _ptr(workspace), nbytes, R, V,
-          stride, top, dt)
+          stride, top, dt | LOGPROBS_LSE_LO if lse_lo else dt)
     return logprob, entropy, lse, top_logprob, top_index
 
 
 def simplicial_logprobs_bwd(logits, targets, lse, entropy, d_logprob=None, d_entropy=None, d_lse=None, out=None):
-    """Gradient of the logits from those of logprob, entropy and lse ([R] float32; None: zeros)."""
+    """Gradient of the logits from those of logprob, entropy and lse ([R] float32; None: zeros).
+    lse [2, R], from a forward with lse_lo: without it the probabilities carry the rounding of
+    lse to float32."""
     R, V, stride = _check_logits(logits, targets)
     device = logits.device
-    _check_like(lse, (R,), torch.float32, device, "lse")
+    lo = lse.dim() == 2
+    _check_like(lse, (2, R) if lo else (R,), torch.float32, device, "lse")
     _check_like(entropy, (R,), torch.float32, device, "entropy")
     for t, name in ((d_logprob, "d_logprob"), (d_entropy, "d_entropy"), (d_lse, "d_lse")):
         if t is not None:
@@ -418,5 +424,6 @@ def simplicial_logprobs_bwd(logits, targets, lse, entropy, d_logprob=None, d_ent
     else:
         _check_like(out, (R, V), logits.dtype, device, "out")
     _call("simplicial_logprobs_bwd", device, logits.data_ptr(), targets.data_ptr(), lse.data_ptr(), entropy.data_ptr(),
-          _ptr(d_logprob), _ptr(d_entropy), _ptr(d_lse), out.data_ptr(), R, V, stride, _DTYPES[logits.dtype])
+          _ptr(d_logprob), _ptr(d_entropy), _ptr(d_lse), out.data_ptr(), R, V, stride,
+          _DTYPES[logits.dtype] | (LOGPROBS_LSE_LO if lo else 0))
     return out

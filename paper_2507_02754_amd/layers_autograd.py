@@ -8,6 +8,7 @@ No arithmetic of their own: forwards and backwards are the library's, through
 import collections
 
 import torch
+from torch.autograd.forward_ad import unpack_dual
 
 from .layers_binding import _DotCall, _RotateCall, simplicial_logprobs_bwd, simplicial_logprobs_fwd
 
@@ -27,6 +28,15 @@ def _rows(t):
 
 def _needs_grad(*tensors):
     return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+
+
+# Without gradients the calls below go past their Functions, which would refuse a tensor of
+# forward-mode differentiation; its values alone would give a result without a tangent, read as a
+# derivative of zero.
+def _refuse_tangents(name, *tensors):
+    for t in tensors:
+        if isinstance(t, torch.Tensor) and unpack_dual(t).tangent is not None:
+            raise NotImplementedError(f"{name} has no forward-mode derivative")
 
 
 # A Function keeps the tensors of its call with save_for_backward alone, which notices
@@ -88,6 +98,7 @@ def norm_rotate(xs, weights=None, eps=1e-6, freqs=None, layout="half", positions
     weight is given for every tensor or for none."""
     options = (eps, None if freqs is None else tuple(freqs), layout, positions, start)
     xs = list(xs)
+    _refuse_tangents("norm_rotate", *xs, *(weights or ()))
     if weights is not None and any(w is None for w in weights):
         raise ValueError("a weight for every tensor, or weights=None")
     if _needs_grad(*xs, *(weights or ())):
@@ -131,6 +142,7 @@ def dot_attention(q, k, v, scale=None, causal=True, window=0, softcap=0.0, slope
     queries the last Nq of the keys' positions; score cap, distance bias, and causal,
     window, prefix and document masks. The options are not differentiated."""
     options = (scale, causal, window, softcap, slopes, documents, prefix, k_lens)
+    _refuse_tangents("dot_attention", q, k, v, scale, softcap, slopes)
     if slopes is not None and slopes.requires_grad:
         raise ValueError("the slopes of the distance bias get no gradient")
     if _needs_grad(q, k, v):
@@ -170,6 +182,7 @@ def token_logprobs(logits, targets, top=0):
     logits [..., V], targets [...] int64 (negative: left out, logprob 0). Returns a
     TokenLogprobs of logprob, entropy, lse ([...] float32), top_logprobs and top_tokens
     ([..., top]), as simplicial_logprobs_fwd."""
+    _refuse_tangents("token_logprobs", logits)
     lead, V = logits.shape[:-1], logits.shape[-1]
     if targets.shape != lead:
         raise ValueError(f"targets have shape {tuple(targets.shape)}, expected {tuple(lead)}")

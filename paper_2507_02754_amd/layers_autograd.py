@@ -10,7 +10,7 @@ import collections
 import torch
 from torch.autograd.forward_ad import unpack_dual
 
-from .layers_binding import _DotCall, _RotateCall, simplicial_logprobs_bwd, simplicial_logprobs_fwd
+from .layers_binding import _DotCall, _RotateCall, freq_numbers, simplicial_logprobs_bwd, simplicial_logprobs_fwd
 
 __all__ = ["norm_rotate", "dot_attention", "token_logprobs", "TokenLogprobs", "NormRotateFunction", "DotAttentionFunction",
            "TokenLogprobsFunction"]
@@ -37,6 +37,12 @@ def _refuse_tangents(name, *tensors):
     for t in tensors:
         if isinstance(t, torch.Tensor) and unpack_dual(t).tangent is not None:
             raise NotImplementedError(f"{name} has no forward-mode derivative")
+
+
+# Options enter the kernels as numbers: one that asks for a gradient would stay as it is in training.
+def _refuse_gradients(name, *options):
+    if torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad for t in options):
+        raise ValueError(f"{name}: no gradient; pass what does not require one")
 
 
 # A Function keeps the tensors of its call with save_for_backward alone, which notices
@@ -96,9 +102,14 @@ def norm_rotate(xs, weights=None, eps=1e-6, freqs=None, layout="half", positions
     xs[t] is [B, N, heads_t, D]; arguments as simplicial_norm_rotate_fwd, whose results
     are returned as a tuple. eps = 0 without weights is the L2 norm scaled by sqrt(D). A
     weight is given for every tensor or for none."""
-    options = (eps, None if freqs is None else tuple(freqs), layout, positions, start)
     xs = list(xs)
-    _refuse_tangents("norm_rotate", *xs, *(weights or ()))
+    if freqs is not None and not isinstance(freqs, torch.Tensor):
+        freqs = tuple(freqs)
+    numbers = freq_numbers(freqs)
+    given = () if numbers is freqs else freqs if isinstance(freqs, tuple) else (freqs,)
+    _refuse_tangents("norm_rotate", *xs, *(weights or ()), eps, *given)
+    _refuse_gradients("eps and freqs", eps, *given)
+    options = (eps, numbers, layout, positions, start)
     if weights is not None and any(w is None for w in weights):
         raise ValueError("a weight for every tensor, or weights=None")
     if _needs_grad(*xs, *(weights or ())):
@@ -143,8 +154,7 @@ def dot_attention(q, k, v, scale=None, causal=True, window=0, softcap=0.0, slope
     window, prefix and document masks. The options are not differentiated."""
     options = (scale, causal, window, softcap, slopes, documents, prefix, k_lens)
     _refuse_tangents("dot_attention", q, k, v, scale, softcap, slopes)
-    if slopes is not None and slopes.requires_grad:
-        raise ValueError("the slopes of the distance bias get no gradient")
+    _refuse_gradients("scale, softcap and slopes", scale, softcap, slopes)
     if _needs_grad(q, k, v):
         return DotAttentionFunction.apply(q, k, v, options)[0]
     return _DotCall(_rows(q), _rows(k), _rows(v), *options).forward()[0]

@@ -119,6 +119,15 @@ def rotary_freqs(count, base=10000.0):
     return tuple(float(base) ** (-i / count) for i in range(count))
 
 
+def freq_numbers(freqs):
+    """A tuple of Python numbers (None: no rotation); itself if it is one. The cache below
+    would keep a tensor's elements, and not find them again."""
+    if freqs is None:
+        return ()
+    freqs = tuple(freqs.tolist() if isinstance(freqs, torch.Tensor) else freqs)
+    return freqs if set(map(type, freqs)) <= {float} else tuple(map(float, freqs))
+
+
 @functools.lru_cache(maxsize=64)
 def _freq_array(freqs):
     return (ctypes.c_double * max(len(freqs), 1))(*freqs)
@@ -169,7 +178,7 @@ class _RotateCall:
             if positions.dim() == 2 and B > 1:
                 pos_stride = positions.stride(0)
             pos = positions.data_ptr()
-        freqs = tuple(freqs) if freqs is not None else ()
+        freqs = freq_numbers(freqs)
         self.n, self.shapes, self.dtype, self.device = n, shapes, x0.dtype, device
         self.heads = (ctypes.c_int32 * n)(*[s[2] for s in shapes])
         self.strides = (ctypes.c_int64 * (3 * n))(*[s for x in xs for s in _strides(x)])

@@ -7,7 +7,7 @@ import pytest
 import torch
 import torch.autograd.forward_ad as forward_ad
 
-from paper_2507_02754_amd import dot_attention, layers_autograd, norm_rotate, token_logprobs
+from paper_2507_02754_amd import dot_attention, layers_autograd, layers_binding, norm_rotate, rotary_freqs, token_logprobs
 
 
 @pytest.fixture
@@ -46,6 +46,9 @@ CALLS = {
     "slopes": (W[:2], lambda t: dot_attention(X, X, X, slopes=t)),
     "scale": (W[0], lambda t: dot_attention(X, X, X, scale=t)),
     "softcap": (W[0], lambda t: dot_attention(X, X, X, softcap=t)),
+    "eps": (W[0], lambda t: norm_rotate([X], eps=t)),
+    "freqs": (W[:32], lambda t: norm_rotate([X], freqs=t)),
+    "an angle": (W[0], lambda t: norm_rotate([X], freqs=[t] * 32)),
     "logits": (torch.ones(4, 8), lambda t: token_logprobs(t, TARGETS)),
 }
 
@@ -58,3 +61,27 @@ def test_forward_mode_is_refused(stub, name, mode):
         call(x)  # (no tangent: as ever)
         with pytest.raises(NotImplementedError, match="forward-mode"):
             call(forward_ad.make_dual(x, torch.ones_like(x)))
+
+
+@pytest.mark.parametrize("name", ["slopes", "scale", "softcap", "eps", "freqs", "an angle"])
+def test_options_are_not_trained(stub, name):
+    """A tensor that asks for a gradient, where gradients are formed, whether or not of the
+    other inputs."""
+    x, call = CALLS[name]
+    leaf = x.clone().requires_grad_(True)
+    with pytest.raises(ValueError, match="no gradient"):
+        call(leaf)
+    with torch.no_grad():
+        call(leaf)
+    call(leaf.detach())
+
+
+def test_angles_are_kept_as_numbers():
+    """What is kept of a call's angles is found again, whatever they were given as."""
+    want = rotary_freqs(32)
+    x = torch.tensor(want, dtype=torch.float64)
+    before = layers_binding._freq_array.cache_info()
+    arrays = {id(layers_binding._freq_array(layers_binding.freq_numbers(f))) for f in (want, list(want), x, list(x), iter(want), x.numpy())}
+    after = layers_binding._freq_array.cache_info()
+    assert len(arrays) == 1 and after.currsize - before.currsize <= 1
+    assert layers_binding.freq_numbers(want) is want and layers_binding.freq_numbers(None) == ()

@@ -102,7 +102,7 @@ def norm_rotate(xs, weights=None, eps=1e-6, freqs=None, layout="half", positions
     xs[t] is [B, N, heads_t, D]; arguments as simplicial_norm_rotate_fwd, whose results
     are returned as a tuple. eps = 0 without weights is the L2 norm scaled by sqrt(D). A
     weight is given for every tensor or for none."""
-    xs = list(xs)
+    xs, weights = list(xs), None if weights is None else list(weights)
     if freqs is not None and not isinstance(freqs, torch.Tensor):
         freqs = tuple(freqs)
     numbers = freq_numbers(freqs)
@@ -110,7 +110,7 @@ def norm_rotate(xs, weights=None, eps=1e-6, freqs=None, layout="half", positions
     _refuse_tangents("norm_rotate", *xs, *(weights or ()), eps, *given)
     _refuse_gradients("eps and freqs", eps, *given)
     options = (eps, numbers, layout, positions, start)
-    if weights is not None and any(w is None for w in weights):
+    if weights is not None and (len(weights) != len(xs) or any(w is None for w in weights)):
         raise ValueError("a weight for every tensor, or weights=None")
     if _needs_grad(*xs, *(weights or ())):
         return NormRotateFunction.apply(options, len(xs), *xs, *(weights or ()))

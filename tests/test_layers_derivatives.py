@@ -85,3 +85,13 @@ def test_angles_are_kept_as_numbers():
     after = layers_binding._freq_array.cache_info()
     assert len(arrays) == 1 and after.currsize - before.currsize <= 1
     assert layers_binding.freq_numbers(want) is want and layers_binding.freq_numbers(None) == ()
+
+
+def test_weights_of_another_number(stub):
+    """Refused alike whether or not a gradient is asked for; any iterable will do."""
+    leaf = X.clone().requires_grad_(True)
+    for x in (X, leaf):
+        for weights in ([], [W, W], [None], (w for w in ())):
+            with pytest.raises(ValueError, match="weight for every"):
+                norm_rotate([x], weights=weights)
+    norm_rotate([X, X], weights=(w for w in (W, W)))

@@ -172,7 +172,8 @@ class InterleavedStack(nn.Module):
     as in Section 8) and causal dot-product attention otherwise, a final norm
     and an output head. forward(tokens [B, N] int64) -> logits [B, N, vocab].
     `qk_norm`: of the 2-simplicial layers; `dot_options`: options of DotProductAttention
-    for the others."""
+    for the others, whose kernels, where the options select them, run in `attn_dtype` too
+    unless the options name another."""
 
     def __init__(self, vocab, d_model, n_layers, n_heads, head_dim, w1, w2, every=4, d_ff=None,
                  kv_heads=None, kp_bias=0.0, vp_bias=0.0, attn_dtype=torch.bfloat16, device=None,
@@ -187,7 +188,10 @@ class InterleavedStack(nn.Module):
                 attn = SimplicialAttention(d_model, n_heads, head_dim, w1, w2, kv_heads, kp_bias, vp_bias,
                                            attn_dtype=attn_dtype, qk_norm=qk_norm, **fk)
             else:
-                attn = DotProductAttention(d_model, n_heads, head_dim, **fk, **(dot_options or {}))
+                options = dot_options or {}
+                attn = DotProductAttention(d_model, n_heads, head_dim, **fk, **options)
+                if attn.attn_dtype is not None and options.get("attn_dtype") is None:
+                    attn.attn_dtype = attn_dtype
             layers.append(Block(attn, d_model, d_ff, **fk))
         self.layers = nn.ModuleList(layers)
         self.norm = RMSNorm(d_model, **fk)

@@ -103,6 +103,7 @@ int simplicial_norm_rotate_bwd(int32_t count, const void* const* x, const int64_
  *   workspace   simplicial_dot_attn_fwd_workspace_size() bytes (0: may be NULL):
  *               partial results of the parts a long key axis is split into where
  *               there are few queries, and the ranges of document numbers
+ *   scale, softcap  finite, with normal float32 numbers as their quotient and 1 / softcap
  *   D           16, 32, 64 or 128;  1 <= Nq <= Nk
  */
 size_t simplicial_dot_attn_fwd_workspace_size(int64_t B, int64_t Nq, int64_t Nk, int64_t H,

@@ -105,6 +105,14 @@ bool block_fits(int64_t sn, int64_t sh, int64_t heads, int64_t D, int32_t dtype)
   return sn < most / 64 && sh < most / 4 && 33 * sn + (heads - 1) * sh + D < most && (heads - 1) <= most / (sh ? sh : 1);
 }
 
+// Scale and cap whose quotients and base-2 products, as the kernels form them in float32, neither
+// overflow (an infinity times a score of 0 is NaN) nor lose digits.
+bool good_scores(float scale, float cap) {
+  const float log2e = 1.4426950408889634f;
+  if (!isfinite(scale * log2e) || !isfinite(cap * log2e) || cap < 0.f) return false;
+  return cap == 0.f || (isnormal(1.f / cap) && isfinite(2.f * log2e * scale / cap) && (scale == 0.f || isnormal(scale / cap)));
+}
+
 struct DotCall {
   int64_t B, Nq, Nk, H, Hkv, D, st[9];
   float scale, softcap;
@@ -116,7 +124,7 @@ struct DotCall {
 int check_dot_call(const DotCall& c) {
   const int rc = check_dot(c.B, c.Nq, c.Nk, c.H, c.Hkv, c.D, c.window, c.dtype);
   if (rc != SA_OK) return rc;
-  if (!isfinite(c.scale) || !isfinite(c.softcap) || c.softcap < 0.f) return SA_ERR_INVALID;
+  if (!good_scores(c.scale, c.softcap)) return SA_ERR_INVALID;
   for (int64_t s : c.st)
     if (!good_stride(s, c.dtype)) return SA_ERR_INVALID;
   if (!block_fits(c.st[1], c.st[2], c.H, c.D, c.dtype) || !block_fits(c.st[4], c.st[5], 1, c.D, c.dtype) ||

@@ -296,6 +296,9 @@ class _DotCall:
             _check_like(prefix, (B,), torch.int32, device, "prefix")
         if k_lens is not None:
             _check_like(k_lens, (B,), torch.int32, device, "k_lens")
+        softcap = float(softcap)
+        if 0 < softcap < 2.0 ** -126:  # (0, no cap, to float32)
+            raise ValueError(f"softcap {softcap} is below what float32 holds")
         window = int(window)
         if window < 0:
             raise ValueError(f"window {window} is negative")
@@ -303,7 +306,7 @@ class _DotCall:
         self.q, self.k, self.v = q, k, v
         self.plan = (B, Nq, Nk, H, Hkv, D, causal, window, documents is not None, dt)
         self.args = (B, Nq, Nk, H, Hkv, D, *_strides(q), *_strides(k), *_strides(v), D ** -0.5 if scale is None else float(scale),
-                     float(softcap), causal, window, _ptr(slopes), _ptr(documents), _ptr(prefix), _ptr(k_lens), dt)
+                     softcap, causal, window, _ptr(slopes), _ptr(documents), _ptr(prefix), _ptr(k_lens), dt)
         self.kept = (slopes, documents, prefix, k_lens)  # what the pointers point to
 
     def places(self):

@@ -36,3 +36,40 @@ def test_logprobs_dtype_with_low_parts(lib):
     for lse in (0, A + 2):
         assert lib.simplicial_logprobs_fwd(A, A, A, A, lse, 0, 0, A, 1 << 40, 4, 100, 100, 0, 1 | lo, None) == 1
         assert lib.simplicial_logprobs_bwd(A, A, lse, A, A, 0, 0, A, 4, 100, 100, 1 | lo, None) == 1
+
+
+@only_without_gpu
+@pytest.mark.parametrize("backward", [False, True])
+def test_scales_and_caps_past_float32(lib, backward):
+    """Quotients and products that overflow or lose digits are refused (an infinity times a
+    score of 0 would be NaN); the workspace is asked for where they do not."""
+    def rc(scale, cap):
+        B, Nq, Nk, H, Hkv, D = 1, 1, 4096, 8, 2, 128
+        f = lib.simplicial_dot_attn_bwd if backward else lib.simplicial_dot_attn_fwd
+        return f(*[A] * (10 if backward else 6), A, 0, B, Nq, Nk, H, Hkv, D, *(1024, 1024, 128), *(1 << 20, 256, 128) * 2, scale, cap,
+                 1, 0, 0, 0, 0, 0, 1, None)
+    for scale, cap in ((0.1, 0.0), (0.0, 1.0), (-3.0, 50.0), (0.1, 1e-30), (0.1, 1e30), (2.0, 2.0 ** 125), (1e38, 0.0), (0.0, 1e30)):
+        assert rc(scale, cap) == 3, (scale, cap)
+    for scale, cap in ((0.1, 3e38), (0.1, 1e-39), (0.0, 1e-39), (1e-3, 2.0 ** 120), (1e30, 1e-20), (3e38, 0.0), (-3e38, 0.0), (1e20, 1e-25)):
+        assert rc(scale, cap) == 1, (scale, cap)
+
+
+def test_a_cap_that_float32_rounds_to_none():
+    """(Fake tensors: the checks come before the library.)"""
+    class Tensor:
+        shape, dtype, device, is_cuda = torch.Size((1, 4, 2, 64)), torch.bfloat16, torch.device("cuda", 0), True
+
+        def dim(self):
+            return 4
+
+        def numel(self):
+            return 512
+
+        def stride(self, *i):
+            return (512, 128, 64, 1)[i[0]] if i else (512, 128, 64, 1)
+
+    x = Tensor()
+    for cap in (1e-46, 1e-39):
+        with pytest.raises(ValueError, match="softcap"):
+            layers_binding._DotCall(x, x, x, None, True, 0, cap, None, None, None, None)
+    layers_binding._DotCall(x, x, x, None, True, 0, 1e-30, None, None, None, None)

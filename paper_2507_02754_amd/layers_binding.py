@@ -256,15 +256,20 @@ def simplicial_norm_rotate_bwd(xs, dys, weights=None, eps=1e-6, freqs=None, layo
 # ---- dot-product attention ----
 
 
+def _window(window, Nk):
+    """As a 32-bit number: no distance reaches Nk."""
+    return max(min(int(window), Nk), -1)
+
+
 def simplicial_dot_attn_fwd_workspace_size(B, Nq, Nk, H, Hkv, D, causal, window, has_documents, dtype):
     dt = _DTYPES.get(dtype, dtype)
-    return int(_library().simplicial_dot_attn_fwd_workspace_size(B, Nq, Nk, H, Hkv, D, bool(causal), int(window),
+    return int(_library().simplicial_dot_attn_fwd_workspace_size(B, Nq, Nk, H, Hkv, D, bool(causal), _window(window, Nk),
                                                                  bool(has_documents), int(dt)))
 
 
 def simplicial_dot_attn_bwd_workspace_size(B, Nq, Nk, H, Hkv, D, causal, window, has_documents, dtype):
     dt = _DTYPES.get(dtype, dtype)
-    return int(_library().simplicial_dot_attn_bwd_workspace_size(B, Nq, Nk, H, Hkv, D, bool(causal), int(window),
+    return int(_library().simplicial_dot_attn_bwd_workspace_size(B, Nq, Nk, H, Hkv, D, bool(causal), _window(window, Nk),
                                                                  bool(has_documents), int(dt)))
 
 
@@ -299,10 +304,9 @@ class _DotCall:
         softcap = float(softcap)
         if 0 < softcap < 2.0 ** -126:  # (0, no cap, to float32)
             raise ValueError(f"softcap {softcap} is below what float32 holds")
-        window = int(window)
-        if window < 0:
+        if int(window) < 0:
             raise ValueError(f"window {window} is negative")
-        causal, window, dt = bool(causal), min(window, Nk), _DTYPES[q.dtype]  # (no distance reaches Nk)
+        causal, window, dt = bool(causal), _window(window, Nk), _DTYPES[q.dtype]
         self.q, self.k, self.v = q, k, v
         self.plan = (B, Nq, Nk, H, Hkv, D, causal, window, documents is not None, dt)
         self.args = (B, Nq, Nk, H, Hkv, D, *_strides(q), *_strides(k), *_strides(v), D ** -0.5 if scale is None else float(scale),

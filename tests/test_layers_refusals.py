@@ -73,3 +73,12 @@ def test_a_cap_that_float32_rounds_to_none():
         with pytest.raises(ValueError, match="softcap"):
             layers_binding._DotCall(x, x, x, None, True, 0, cap, None, None, None, None)
     layers_binding._DotCall(x, x, x, None, True, 0, 1e-30, None, None, None, None)
+
+
+def test_workspace_sizes_of_windows_past_32_bits(lib):
+    """As of a window that hides nothing; negative ones as an invalid call's."""
+    for size in (layers_binding.simplicial_dot_attn_fwd_workspace_size, layers_binding.simplicial_dot_attn_bwd_workspace_size):
+        def of(window):
+            return size(2, 1, 5000, 8, 2, 128, True, window, True, torch.bfloat16)
+        assert of(5000) == of(1 << 31) == of((1 << 32) + 5) == of(1 << 70) == of(0) > 0
+        assert of(-1) == of(-(1 << 32)) == of(5 - (1 << 32)) == 0

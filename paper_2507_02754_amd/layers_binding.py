@@ -184,6 +184,8 @@ class _RotateCall:
         self.strides = (ctypes.c_int64 * (3 * n))(*[s for x in xs for s in _strides(x)])
         self.xs = _pointers(xs)
         self.weights = None if weights is None else _pointers(weights)
+        if not -(1 << 63) <= int(start) <= (1 << 63) - N:
+            raise ValueError(f"start {start}: positions are 64-bit numbers")
         self.pos = (pos, pos_stride, int(start))
         self.tail = (B, N, D, eps is not None, float(eps or 0.0), code, _freq_array(freqs), len(freqs), _DTYPES[x0.dtype],
                      _DTYPES[wdtype])

@@ -54,21 +54,25 @@ def test_scales_and_caps_past_float32(lib, backward):
         assert rc(scale, cap) == 1, (scale, cap)
 
 
+class FakeTensor:
+    """What the checks before the library look at."""
+    shape, dtype, device, is_cuda = torch.Size((1, 4, 2, 64)), torch.bfloat16, torch.device("cuda", 0), True
+
+    def dim(self):
+        return 4
+
+    def numel(self):
+        return 512
+
+    def stride(self, *i):
+        return (512, 128, 64, 1)[i[0]] if i else (512, 128, 64, 1)
+
+    def data_ptr(self):
+        return A
+
+
 def test_a_cap_that_float32_rounds_to_none():
-    """(Fake tensors: the checks come before the library.)"""
-    class Tensor:
-        shape, dtype, device, is_cuda = torch.Size((1, 4, 2, 64)), torch.bfloat16, torch.device("cuda", 0), True
-
-        def dim(self):
-            return 4
-
-        def numel(self):
-            return 512
-
-        def stride(self, *i):
-            return (512, 128, 64, 1)[i[0]] if i else (512, 128, 64, 1)
-
-    x = Tensor()
+    x = FakeTensor()
     for cap in (1e-46, 1e-39):
         with pytest.raises(ValueError, match="softcap"):
             layers_binding._DotCall(x, x, x, None, True, 0, cap, None, None, None, None)
@@ -82,3 +86,12 @@ def test_workspace_sizes_of_windows_past_32_bits(lib):
             return size(2, 1, 5000, 8, 2, 128, True, window, True, torch.bfloat16)
         assert of(5000) == of(1 << 31) == of((1 << 32) + 5) == of(1 << 70) == of(0) > 0
         assert of(-1) == of(-(1 << 32)) == of(5 - (1 << 32)) == 0
+
+
+def test_positions_past_64_bits():
+    x = FakeTensor()
+    for start in (1 << 63, (1 << 63) - 3, (1 << 64) + 5, -(1 << 63) - 1):
+        with pytest.raises(ValueError, match="start"):
+            layers_binding._RotateCall([x], None, 1e-6, None, "half", None, start)
+    for start in (0, (1 << 63) - 4, -(1 << 63)):
+        layers_binding._RotateCall([x], None, 1e-6, None, "half", None, start)

@@ -23,7 +23,7 @@
 //
 // P and dS are rounded to bf16 for their products, as the operands are; everything
 // else is float32. Rows or keys whose sums met an infinity or NaN of a masked pair are
-// formed again by themselves.
+// formed again by themselves (dot_mfma.h).
 #include "dot_mfma.h"
 
 namespace sa {
@@ -52,8 +52,8 @@ __device__ __forceinline__ float score_of(const Scores<CAP, BIAS>& c, float s, f
   return x;
 }
 
-// dQ of one row by itself.
-__device__ __forceinline__ void single_row(const DotArgs& a, const DotMask& m, int b, int i, int head, float lse, float delta) {
+// Columns `lane` (if t0) and lane + 64 (if t1) of dQ of one row by themselves.
+__device__ __forceinline__ void single_row(const DotArgs& a, const DotMask& m, int b, int i, int head, float lse, float delta, bool t0, bool t1) {
   const int lane = threadIdx.x & 63, hk = head / a.G, p = m.first + i, dq = m.doc(p);
   const bool d0 = lane < a.D, d1 = lane + 64 < a.D;
   const int64_t at = ((static_cast<int64_t>(b) * a.Nq + i) * a.H + head) * a.D + lane;
@@ -79,14 +79,17 @@ __device__ __forceinline__ void single_row(const DotArgs& a, const DotMask& m, i
     const float w = fast_exp2((s - slope * static_cast<float>(abs(p - j)) - lse) * kLog2e) * (dp - delta) * dcap * a.scale;
     o0 += w * k0;
     o1 += w * k1;
-    if (__builtin_amdgcn_ballot_w64((d0 && o0 == o0) || (d1 && o1 == o1)) == 0) break;  // all NaN
+    if (__builtin_amdgcn_ballot_w64((t0 && o0 == o0) || (t1 && o1 == o1)) == 0) break;  // all NaN
   }
   uint16_t* out = static_cast<uint16_t*>(a.dq) + at;
-  if (d0) out[0] = f32_to_bf16(o0);
-  if (d1) out[64] = f32_to_bf16(o1);
+  if (t0) out[0] = f32_to_bf16(o0);
+  if (t1) out[64] = f32_to_bf16(o1);
 }
-// dK and dV of one key by itself.
-__device__ __forceinline__ void single_key(const DotArgs& a, const DotMask& m, int b, int hk, int j) {
+// The same of dK (k0, k1) and dV (v0, v1) of one key.
+struct KeyColumns {
+  bool k0, k1, v0, v1;
+};
+__device__ __forceinline__ void single_key(const DotArgs& a, const DotMask& m, int b, int hk, int j, KeyColumns t) {
   const int lane = threadIdx.x & 63, dk = m.doc(j);
   const bool d0 = lane < a.D, d1 = lane + 64 < a.D;
   const uint16_t* k = static_cast<const uint16_t*>(a.k) + b * a.ksb + j * a.ksn + hk * a.ksh + lane;
@@ -119,11 +122,13 @@ __device__ __forceinline__ void single_key(const DotArgs& a, const DotMask& m, i
       y0 += w * g0;
       y1 += w * g1;
     }
-    if (__builtin_amdgcn_ballot_w64((d0 && (x0 == x0 || y0 == y0)) || (d1 && (x1 == x1 || y1 == y1))) == 0) break;
+    if (__builtin_amdgcn_ballot_w64((t.k0 && x0 == x0) || (t.k1 && x1 == x1) || (t.v0 && y0 == y0) || (t.v1 && y1 == y1)) == 0) break;
   }
   const int64_t at = ((static_cast<int64_t>(b) * a.Nk + j) * a.Hkv + hk) * a.D + lane;
-  if (d0) static_cast<uint16_t*>(a.dk)[at] = f32_to_bf16(x0), static_cast<uint16_t*>(a.dv)[at] = f32_to_bf16(y0);
-  if (d1) static_cast<uint16_t*>(a.dk)[at + 64] = f32_to_bf16(x1), static_cast<uint16_t*>(a.dv)[at + 64] = f32_to_bf16(y1);
+  if (t.k0) static_cast<uint16_t*>(a.dk)[at] = f32_to_bf16(x0);
+  if (t.k1) static_cast<uint16_t*>(a.dk)[at + 64] = f32_to_bf16(x1);
+  if (t.v0) static_cast<uint16_t*>(a.dv)[at] = f32_to_bf16(y0);
+  if (t.v1) static_cast<uint16_t*>(a.dv)[at + 64] = f32_to_bf16(y1);
 }
 
 // LDS arrays of the ring: W copies of NS stages of two tensors' tiles, every stage its own
@@ -341,7 +346,7 @@ __global__ __launch_bounds__(kThreads* GROUPS, PRIV ? 1 : 2) void dot_dq_kernel(
     take(acc, buf);
   }
   uint16_t* dst = static_cast<uint16_t*>(a.dq) + orow + 4 * h;
-  unsigned bad = 0;  // rows that a masked pair may have spoilt: without masks what came out is right
+  unsigned bad = 0;  // rows that a masked pair may have spoilt
   const bool masks = has_mask(a);
   if constexpr (PRIV) {
     __shared__ unsigned flags[kWaves];
@@ -352,18 +357,22 @@ __global__ __launch_bounds__(kThreads* GROUPS, PRIV ? 1 : 2) void dot_dq_kernel(
     const unsigned x = rows_where(masks && w.valid && check != check);
     if (lane == 0) flags[wave] = x;
     __syncthreads();
-    if (wave == 0) bad = flags[0] | flags[1] | flags[2] | flags[3];
+    if (wave == 0) bad = __builtin_amdgcn_readfirstlane(flags[0] | flags[1] | flags[2] | flags[3]);
   } else {
     const float check = not_finite(acc);
     bad = rows_where(masks && w.valid && check != check);
-    if (w.valid && !((bad >> c) & 1)) store_row<DP>(dst, acc, a.scale, a.D);
+    if (w.valid) store_row<DP>(dst, acc, a.scale, a.D);
   }
+  if (bad == 0 || !keys_spoil(a, m, own, kb, a.ksn)) return;
+  const NanColumns<NDT> nan(acc);  // (PRIV: the wavefront's own part's)
+  wait_vmcnt<0>();                 // (the rows are written)
   while (bad) {
     const int x = __builtin_ctz(bad);
     bad &= bad - 1;
     single_row(a, m, b, __builtin_amdgcn_readlane(w.i, x), __builtin_amdgcn_readlane(w.head, x),
                __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(lse), x)),
-               __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(delta), x)));
+               __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(delta), x)), lane < a.D && (PRIV || nan.template at<0>(x)),
+               lane + 64 < a.D && (PRIV || nan.template at<1>(x)));
   }
 }
 
@@ -590,19 +599,25 @@ __global__ __launch_bounds__(kThreads* GROUPS, PRIV ? 1 : 2) void dot_dkv_kernel
     const unsigned x = rows_where(masks && key && check != check);
     if (lane == 0) flags[wave] = x;
     __syncthreads();
-    if (wave == 0) bad = flags[0] | flags[1] | flags[2] | flags[3];
+    if (wave == 0) bad = __builtin_amdgcn_readfirstlane(flags[0] | flags[1] | flags[2] | flags[3]);
   } else {
     const float check = not_finite(acck) + not_finite(accv);
     bad = rows_where(masks && key && check != check);
-    if (out && !((bad >> c) & 1)) {
+    if (out) {
       store_row<DP>(pk, acck, a.scale, a.D);
       store_row<DP>(pv, accv, 1.f, a.D);
     }
   }
+  if (bad == 0 || !queries_spoil(a, m, own, b, hk)) return;
+  const NanColumns<NDT> nank(acck), nanv(accv);  // (PRIV: the wavefront's own part's)
+  wait_vmcnt<0>();                               // (the keys are written)
   while (bad) {
     const int x = __builtin_ctz(bad);
     bad &= bad - 1;
-    single_key(a, m, b, hk, j0 + x);
+    const bool d0 = lane < a.D, d1 = lane + 64 < a.D;
+    single_key(a, m, b, hk, j0 + x,
+               KeyColumns{d0 && (PRIV || nank.template at<0>(x)), d1 && (PRIV || nank.template at<1>(x)), d0 && (PRIV || nanv.template at<0>(x)),
+                          d1 && (PRIV || nanv.template at<1>(x))});
   }
 }
 
@@ -620,18 +635,16 @@ __global__ __launch_bounds__(kThreads) void dot_keys_kernel(DotArgs a) {
     if (d1) x1 += p[64], y1 += p[n + 64];
   }
   const int bh = static_cast<int>(at / a.Nk), j = static_cast<int>(at - static_cast<int64_t>(bh) * a.Nk), b = bh / a.Hkv, hk = bh - b * a.Hkv;
-  const float check = (x0 + x1) * 0.f + (y0 + y1) * 0.f;
-  if (has_mask(a) && __builtin_amdgcn_ballot_w64(check != check) != 0) {
-    const DotMask m(a, b);
-    if (j < m.L) {
-      single_key(a, m, b, hk, j);
-      return;
-    }
-  }
   const int64_t o = ((static_cast<int64_t>(b) * a.Nk + j) * a.Hkv + hk) * a.D + lane;
   uint16_t *pk = static_cast<uint16_t*>(a.dk) + o, *pv = static_cast<uint16_t*>(a.dv) + o;
   if (d0) pk[0] = f32_to_bf16(x0 * a.scale), pv[0] = f32_to_bf16(y0);
   if (d1) pk[64] = f32_to_bf16(x1 * a.scale), pv[64] = f32_to_bf16(y1);
+  const KeyColumns nan{d0 && x0 != x0, d1 && x1 != x1, d0 && y0 != y0, d1 && y1 != y1};
+  if (has_mask(a) && __builtin_amdgcn_ballot_w64(nan.k0 || nan.k1 || nan.v0 || nan.v1) != 0) {
+    const DotMask m(a, b);
+    const int first = j & ~(kDotBlock - 1);
+    if (j < m.L && queries_spoil(a, m, DotSpan(m, first, first + kDotBlock - 1), b, hk)) single_key(a, m, b, hk, j, nan);
+  }
 }
 
 template <int DP, int CAP, bool BIAS>

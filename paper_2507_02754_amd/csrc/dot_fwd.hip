@@ -34,8 +34,7 @@
 //
 // A block whose pairs are all visible has no mask work; blocks without a visible pair
 // are not visited (walked 64 at a time, a lane each). A masked pair's probability of
-// 0 times an infinity or NaN of V is NaN: rows that come out so are formed again by
-// themselves, over their visible keys alone.
+// 0 times an infinity or NaN of V is NaN: rows that it spoilt are formed again by themselves.
 #include "dot_mfma.h"
 
 #include "simplicial_layers.h"
@@ -134,9 +133,9 @@ __device__ __forceinline__ void write_out(const DotArgs& a, int64_t at, bool d0,
   if (a.out_lo && d0) lo[0] = f32_to_bf16(rounded_off(x0));
   if (a.out_lo && d1) lo[64] = f32_to_bf16(rounded_off(x1));
 }
-// O of one row by itself, over its visible keys (LSE is not touched by masked pairs), a
-// wavefront's 64 lanes along the columns: for rows whose products met an infinity or NaN.
-__device__ __forceinline__ void single_row(const DotArgs& a, const DotMask& m, int b, int i, int head, float lse) {
+// Columns `lane` (if t0) and lane + 64 (if t1) of one row's O by themselves, over its visible keys (LSE is
+// not touched by masked pairs), a wavefront's 64 lanes along the columns.
+__device__ __forceinline__ void single_row(const DotArgs& a, const DotMask& m, int b, int i, int head, float lse, bool t0, bool t1) {
   const int lane = threadIdx.x & 63, hk = head / a.G, p = m.first + i, dq = m.doc(p);
   const bool d0 = lane < a.D, d1 = lane + 64 < a.D;
   const uint16_t* q = static_cast<const uint16_t*>(a.q) + b * a.qsb + i * a.qsn + head * a.qsh + lane;
@@ -154,17 +153,20 @@ __device__ __forceinline__ void single_row(const DotArgs& a, const DotMask& m, i
     const float w = fast_exp2((s - slope * static_cast<float>(abs(p - j)) - lse) * kLog2e);
     o0 += d0 ? w * bf16_to_f32(v[vj]) : 0.f;
     o1 += d1 ? w * bf16_to_f32(v[vj + 64]) : 0.f;
-    if (__builtin_amdgcn_ballot_w64((d0 && o0 == o0) || (d1 && o1 == o1)) == 0) break;  // all NaN
+    if (__builtin_amdgcn_ballot_w64((t0 && o0 == o0) || (t1 && o1 == o1)) == 0) break;  // all NaN
   }
-  write_out(a, ((static_cast<int64_t>(b) * a.Nq + i) * a.H + head) * a.D + lane, d0, o0, d1, o1);
+  write_out(a, ((static_cast<int64_t>(b) * a.Nq + i) * a.H + head) * a.D + lane, t0, o0, t1, o1);
 }
-// The rows of `bad` (a bit for each of the wavefront's 32), one after another.
-__device__ __forceinline__ void single_rows(const DotArgs& a, const DotMask& m, int b, const Lanes& w, float lse, unsigned bad) {
+// The rows of `bad` (a bit for each of the wavefront's 32), one after another: of row c the columns for
+// which t0(c), t1(c) say so.
+template <typename T0, typename T1>
+__device__ __forceinline__ void single_rows(const DotArgs& a, const DotMask& m, int b, const Lanes& w, float lse, unsigned bad, T0 t0, T1 t1) {
+  const int lane = threadIdx.x & 63;
   while (bad) {
     const int c = __builtin_ctz(bad);
     bad &= bad - 1;
     single_row(a, m, b, __builtin_amdgcn_readlane(w.i, c), __builtin_amdgcn_readlane(w.head, c),
-               __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(lse), c)));
+               __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(lse), c)), t0(c) && lane < a.D, t1(c) && lane + 64 < a.D);
   }
 }
 
@@ -346,14 +348,16 @@ __global__ __launch_bounds__(kThreads* GROUPS, 2) void dot_fwd_kernel(DotArgs a)
   const float check = not_finite(row.acc);
   const unsigned bad = has_mask(a) ? rows_where(w.valid && fabsf(row.l) < kInf && check != check) : 0;
   if (w.valid) {
-    if (!((bad >> c) & 1)) {
-      const int64_t o = ((static_cast<int64_t>(b) * a.Nq + w.i) * a.H + w.head) * a.D + 4 * h;
-      store_row<DP>(static_cast<uint16_t*>(a.out) + o, row.acc, inv, a.D);
-      if (a.out_lo) store_row_lo<DP>(static_cast<uint16_t*>(a.out_lo) + o, row.acc, inv, a.D);
-    }
+    const int64_t o = ((static_cast<int64_t>(b) * a.Nq + w.i) * a.H + w.head) * a.D + 4 * h;
+    store_row<DP>(static_cast<uint16_t*>(a.out) + o, row.acc, inv, a.D);
+    if (a.out_lo) store_row_lo<DP>(static_cast<uint16_t*>(a.out_lo) + o, row.acc, inv, a.D);
     if (h == 0) a.lse[(static_cast<int64_t>(b) * a.H + w.head) * a.Nq + w.i] = lse;
   }
-  single_rows(a, m, b, w, lse, bad);
+  if (bad && keys_spoil(a, m, own, vb, a.vsn)) {
+    const NanColumns<NDT> nan(row.acc);
+    wait_vmcnt<0>();  // (the rows are written)
+    single_rows(a, m, b, w, lse, bad, [&](int x) { return nan.template at<0>(x); }, [&](int x) { return nan.template at<1>(x); });
+  }
 }
 
 template <int DP, int CAP, bool BIAS>
@@ -521,7 +525,9 @@ __global__ __launch_bounds__(kThreads, 1) void dot_few_kernel(DotArgs a) {
   const unsigned x = rows_where(w.valid && fabsf(l) < kInf && check != check);
   if (lane == 0) flags[wave] = x;
   __syncthreads();
-  if (wave == 0) single_rows(a, m, b, w, lse, flags[0] | flags[1] | flags[2] | flags[3]);
+  const unsigned bad = __builtin_amdgcn_readfirstlane(flags[0] | flags[1] | flags[2] | flags[3]);
+  if (wave == 0 && bad && keys_spoil(a, m, own, vb, a.vsn))
+    single_rows(a, m, b, w, lse, bad, [](int) { return true; }, [](int) { return true; });
 }
 
 // Joins the parts of a row: one workgroup, its wavefronts taking every fourth part.
@@ -562,13 +568,14 @@ __global__ __launch_bounds__(kThreads) void dot_join_kernel(DotArgs a) {
   const int b = bh / a.Hkv, head = (bh - b * a.Hkv) * a.G + rr - i * a.G;
   const float lse = l == 0.f ? -kInf : top * kLn2 + logf(l);
   if (lane == 0) a.lse[(static_cast<int64_t>(b) * a.H + head) * a.Nq + i] = lse;
-  const float check = x0 * 0.f + x1 * 0.f;
-  if (has_mask(a) && fabsf(l) < kInf && __builtin_amdgcn_ballot_w64(check != check) != 0) {
-    single_row(a, DotMask(a, b), b, i, head, lse);
-    return;
-  }
   const float inv = l == 0.f ? 0.f : 1.f / lr;
   write_out(a, ((static_cast<int64_t>(b) * a.Nq + i) * a.H + head) * a.D + lane, d0, x0 * inv, d1, x1 * inv);
+  const bool n0 = d0 && x0 != x0, n1 = d1 && x1 != x1;
+  if (has_mask(a) && fabsf(l) < kInf && __builtin_amdgcn_ballot_w64(n0 || n1) != 0) {
+    const DotMask m(a, b);
+    const uint16_t* vb = static_cast<const uint16_t*>(a.v) + b * a.vsb + head / a.G * a.vsh;
+    if (keys_spoil(a, m, rows_span(a, m, rr / 32 * 32, 32), vb, a.vsn)) single_row(a, m, b, i, head, lse, n0, n1);
+  }
 }
 
 template <int DP, int CAP, bool BIAS>

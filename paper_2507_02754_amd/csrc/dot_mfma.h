@@ -154,6 +154,89 @@ __device__ __forceinline__ unsigned rows_where(bool x) {
   return static_cast<unsigned>(b) | static_cast<unsigned>(b >> 32);
 }
 
+// A masked pair's weight of 0 times an infinity or NaN of the tile it is multiplied with is NaN:
+// where a row (key) with masks comes out so, the tiles of its wavefront's blocks with masked pairs are
+// looked over, and only if one of them holds such a value are its columns that are NaN formed again,
+// over the visible pairs alone. (Values that are visible are none's fault: B=1 H=16 Hkv=4 N=4096 D=128
+// causal with an infinity in the first row of V 0.16 ms, without 0.12; forming every such row again 100.)
+template <typename Row>
+__device__ __forceinline__ bool rows_not_finite(int n, int D, Row row) {
+  const int per = D / 8;  // 16-byte chunks of a row
+  bool bad = false;
+  for (int at = threadIdx.x & 63; at < n * per; at += 64) {
+    const u32x4_t x = ldg128(row(at / per) + 8 * (at % per));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) bad |= (x[i] & 0x7f80u) == 0x7f80u || (x[i] & 0x7f800000u) == 0x7f800000u;
+  }
+  return __builtin_amdgcn_ballot_w64(bad) != 0;
+}
+// Of k or v (a head's rows from x on, sn apart), for the 32 rows of span q.
+__device__ __forceinline__ bool keys_spoil(const DotArgs& a, const DotMask& m, const DotSpan& q, const uint16_t* x, int64_t sn) {
+  int lo, hi;
+  key_blocks(m, q, lo, hi);
+  bool bad = false;
+  walk_blocks(
+      lo, hi, 0, 1,
+      [&](int blk, bool& live, bool& full) {
+        const DotSpan k(m, blk * kDotBlock, blk * kDotBlock + kDotBlock - 1);
+        live = dot_live(m, q, k) && !dot_full(m, q, k);
+        full = false;
+      },
+      [&](int blk, bool) {
+        const int j0 = blk * kDotBlock;
+        if (!bad) bad = rows_not_finite(min(m.L - j0, kDotBlock), a.D, [&](int r) { return x + (j0 + r) * sn; });
+      });
+  return bad;
+}
+// Of q and dO, for the 32 keys of span k.
+__device__ __forceinline__ bool queries_spoil(const DotArgs& a, const DotMask& m, const DotSpan& k, int b, int hk) {
+  const int R = a.G * a.Nq;
+  int lo, hi;
+  row_blocks(m, k, a.G, R, lo, hi);
+  bool bad = false;
+  walk_blocks(
+      lo, hi, 0, 1,
+      [&](int blk, bool& live, bool& full) {
+        const DotSpan q(m, m.first + div_group(blk * 32, a), m.first + div_group(min(blk * 32 + 32, R) - 1, a));
+        live = dot_live(m, q, k) && !dot_full(m, q, k);
+        full = false;
+      },
+      [&](int blk, bool) {
+        const int r0 = blk * kDotBlock, n = min(R - r0, kDotBlock);
+        auto at = [&](const void* x, int r, int64_t sb, int64_t sn, int64_t sh) {
+          const int i = div_group(r0 + r, a);
+          return static_cast<const uint16_t*>(x) + b * sb + i * sn + (hk * a.G + r0 + r - i * a.G) * sh;
+        };
+        if (!bad) bad = rows_not_finite(n, a.D, [&](int r) { return at(a.q, r, a.qsb, a.qsn, a.qsh); });
+        const int64_t sn = static_cast<int64_t>(a.H) * a.D;
+        if (!bad) bad = rows_not_finite(n, a.D, [&](int r) { return at(a.dout, r, a.Nq * sn, sn, a.D); });
+      });
+  return bad;
+}
+// Which columns of the wavefront's 32 rows are NaN in an accumulator, a bit for each of a lane's.
+template <int NDT>
+struct NanColumns {
+  unsigned w[NDT / 2];
+  __device__ __forceinline__ explicit NanColumns(const f32x16_t (&acc)[NDT]) {
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt) {
+      if (dt % 2 == 0) w[dt / 2] = 0;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) w[dt / 2] |= static_cast<unsigned>(acc[dt][v] != acc[dt][v]) << (16 * (dt % 2) + v);
+    }
+  }
+  // Column (lane + 64 K) of row x.
+  template <int K>
+  __device__ __forceinline__ bool at(int x) const {
+    if constexpr (K >= NDT / 2) return false;
+    else {
+      const int d = threadIdx.x & 63, v = 4 * ((d & 31) >> 3) + (d & 3);
+      const unsigned lo = __builtin_amdgcn_readlane(w[K], x), hi = __builtin_amdgcn_readlane(w[K], x + 32);
+      return (((d & 4) ? hi : lo) >> (16 * (d >> 5) + v)) & 1;
+    }
+  }
+};
+
 __device__ __forceinline__ bool has_mask(const DotArgs& a) { return a.causal || a.window || a.prefix || a.docs || a.lens; }
 
 // A tile's fragments. Row fragment t of lane (h, c) is chunk 2 t + h of row c, at slot

@@ -125,3 +125,50 @@ def test_keys_behind_the_filled_length(size, bad, dt):
             ref.close(got[result][1:], *(x[1:] for x in want[result]), f"{result} of the other sequences")
         assert not torch.isfinite(got["dq"][0, N - 1]).any()
         ref.close(got["dq"][0, :N - 1], *(x[0, :N - 1] for x in want["dq"]), "dq of the other queries")
+
+
+@pytest.mark.parametrize("window", [0, 45])
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("size", FORMS, ids=str)
+def test_what_a_value_reaches(size, dt, window):
+    """One infinity or NaN, or a column of them, in q, k, v or the upstream gradient under a
+    mask: what sees it by the formulas is not finite, everything else is as without it."""
+    B, N, H, Hkv, D = size
+    print(f"\n[dot] reach {size} {dt} {window}", flush=True)
+    G, hk = H // Hkv, Hkv - 1
+    heads = slice(hk * G, H)  # the last group
+    clean = _inputs(B, N, N, H, Hkv, D, dt, seed=N + 1)
+    want = ref.dot_attention(*clean[:3], window=window, dout=clean[3])
+    see = ref.visible(1, N, N, True, window, device="cuda")[0][0]  # [query, key]
+    nan, inf = float("nan"), float("inf")
+
+    def check(which, where, value, label, **reached):
+        """`reached`: positions (bool [N]) of each result that are not finite, or ([N], column)."""
+        t = [x.clone() for x in clean]
+        t[which][(0, *where)] = value
+        got = _call(*t, window=window)
+        for name, (w, bound) in want.items():
+            bad = torch.zeros(w.shape, dtype=torch.bool, device="cuda")
+            if name in reached:
+                at, column = reached[name] if isinstance(reached[name], tuple) else (reached[name], slice(None))
+                if name == "lse":
+                    bad[0, heads] = at
+                else:
+                    bad[0, :, slice(hk, None) if name in ("dk", "dv") else heads, column] = at[:, None, None] if isinstance(column, slice) \
+                        else at[:, None]
+            assert not torch.isfinite(got[name][bad]).any(), f"{label}: {name} is finite where it is reached"
+            ref.close(torch.where(bad, w, got[name].double()), w, bound, f"{label}: {name}")
+
+    everyone = torch.ones(N, dtype=torch.bool, device="cuda")
+    for j, value in ((3, inf), (N // 2 + 1, nan), (N - 1, -inf)):
+        rows = see[:, j]
+        keys = see[rows].any(0)  # seen by a query that sees j
+        check(2, (j, hk, 1), value, f"v at {j}", out=(rows, 1), dq=rows, dk=keys)
+        check(1, (j, hk, 1), nan, f"k at {j}", out=rows, lse=rows, dq=rows, dk=keys, dv=keys)
+    check(2, (slice(None), hk, 2), nan, "a column of v", out=(everyone, 2), dq=everyone, dk=everyone)
+    if G == 1:  # (one query head of a group)
+        for i, value in ((0, inf), (N // 2 + 1, nan), (N - 5, -inf)):
+            row, keys = torch.arange(N, device="cuda") == i, see[i]
+            check(3, (i, H - 1, 1), value, f"dout at {i}", dq=row, dk=keys, dv=(keys, 1))
+            check(0, (i, H - 1, 1), nan, f"q at {i}", out=row, lse=row, dq=row, dk=keys, dv=keys)
+        check(3, (slice(None), H - 1, 2), nan, "a column of dout", dq=everyone, dk=everyone, dv=(everyone, 2))

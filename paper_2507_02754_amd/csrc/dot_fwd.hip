@@ -353,7 +353,7 @@ __global__ __launch_bounds__(kThreads* GROUPS, 2) void dot_fwd_kernel(DotArgs a)
     if (a.out_lo) store_row_lo<DP>(static_cast<uint16_t*>(a.out_lo) + o, row.acc, inv, a.D);
     if (h == 0) a.lse[(static_cast<int64_t>(b) * a.H + w.head) * a.Nq + w.i] = lse;
   }
-  if (bad && keys_spoil(a, m, own, vb, a.vsn)) {
+  if (__builtin_expect(bad != 0, 0) && keys_spoil(a, m, own, vb, a.vsn)) {
     const NanColumns<NDT> nan(row.acc);
     wait_vmcnt<0>();  // (the rows are written)
     single_rows(a, m, b, w, lse, bad, [&](int x) { return nan.template at<0>(x); }, [&](int x) { return nan.template at<1>(x); });

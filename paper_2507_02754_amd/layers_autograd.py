@@ -8,9 +8,9 @@ No arithmetic of their own: forwards and backwards are the library's, through
 import collections
 
 import torch
-from torch.autograd.forward_ad import unpack_dual
+from torch.autograd import forward_ad
 
-from .layers_binding import _DotCall, _RotateCall, freq_numbers, simplicial_logprobs_bwd, simplicial_logprobs_fwd
+from .layers_binding import _DotCall, _RotateCall, rotary_angles, simplicial_logprobs_bwd, simplicial_logprobs_fwd
 
 __all__ = ["norm_rotate", "dot_attention", "token_logprobs", "TokenLogprobs", "NormRotateFunction", "DotAttentionFunction",
            "TokenLogprobsFunction"]
@@ -34,8 +34,10 @@ def _needs_grad(*tensors):
 # forward-mode differentiation; its values alone would give a result without a tangent, read as a
 # derivative of zero.
 def _refuse_tangents(name, *tensors):
+    if forward_ad._current_level < 0:  # (none has a tangent: a microsecond of a token's call)
+        return
     for t in tensors:
-        if isinstance(t, torch.Tensor) and unpack_dual(t).tangent is not None:
+        if isinstance(t, torch.Tensor) and forward_ad.unpack_dual(t).tangent is not None:
             raise NotImplementedError(f"{name} has no forward-mode derivative")
 
 
@@ -103,13 +105,14 @@ def norm_rotate(xs, weights=None, eps=1e-6, freqs=None, layout="half", positions
     are returned as a tuple. eps = 0 without weights is the L2 norm scaled by sqrt(D). A
     weight is given for every tensor or for none."""
     xs, weights = list(xs), None if weights is None else list(weights)
-    if freqs is not None and not isinstance(freqs, torch.Tensor):
-        freqs = tuple(freqs)
-    numbers = freq_numbers(freqs)
-    given = () if numbers is freqs else freqs if isinstance(freqs, tuple) else (freqs,)
-    _refuse_tangents("norm_rotate", *xs, *(weights or ()), eps, *given)
-    _refuse_gradients("eps and freqs", eps, *given)
-    options = (eps, numbers, layout, positions, start)
+    _refuse_tangents("norm_rotate", *xs, *(weights or ()))
+
+    def check(*given):
+        _refuse_tangents("norm_rotate", *given)
+        _refuse_gradients("eps and freqs", *given)
+
+    check(eps)
+    options = (eps, rotary_angles(freqs, check), layout, positions, start)
     if weights is not None and (len(weights) != len(xs) or any(w is None for w in weights)):
         raise ValueError("a weight for every tensor, or weights=None")
     if _needs_grad(*xs, *(weights or ())):

@@ -6,7 +6,6 @@ library. There is no fallback implementation.
 """
 
 import ctypes
-import functools
 
 import torch
 
@@ -119,18 +118,31 @@ def rotary_freqs(count, base=10000.0):
     return tuple(float(base) ** (-i / count) for i in range(count))
 
 
-def freq_numbers(freqs):
-    """A tuple of Python numbers (None: no rotation); itself if it is one. The cache below
-    would keep a tensor's elements, and not find them again."""
+_ANGLES = {}  # the last ones by value: (array, their number)
+
+
+def rotary_angles(freqs, check=None):
+    """(ctypes array, its length) of angles given as numbers, a tensor of them, or None. What is
+    kept are Python numbers (a tensor's elements would never be found again). check(*t) is called
+    with the tensors among them."""
     if freqs is None:
-        return ()
-    freqs = tuple(freqs.tolist() if isinstance(freqs, torch.Tensor) else freqs)
-    return freqs if set(map(type, freqs)) <= {float} else tuple(map(float, freqs))
-
-
-@functools.lru_cache(maxsize=64)
-def _freq_array(freqs):
-    return (ctypes.c_double * max(len(freqs), 1))(*freqs)
+        freqs = ()
+    elif isinstance(freqs, torch.Tensor):
+        if check is not None:
+            check(freqs)
+        freqs = freqs.tolist()
+    freqs = tuple(freqs)
+    found = _ANGLES.get(freqs)
+    if found is None:
+        if check is not None:
+            check(*[f for f in freqs if isinstance(f, torch.Tensor)])
+        numbers = tuple(map(float, freqs))
+        found = _ANGLES.get(numbers)
+    if found is None:
+        if len(_ANGLES) >= 64:
+            _ANGLES.pop(next(iter(_ANGLES)), None)
+        found = _ANGLES[numbers] = ((ctypes.c_double * max(len(numbers), 1))(*numbers), len(numbers))
+    return found
 
 
 class _RotateCall:
@@ -139,7 +151,7 @@ class _RotateCall:
 
     __slots__ = ("n", "shapes", "dtype", "device", "strides", "xs", "weights", "heads", "pos", "tail", "kept")
 
-    def __init__(self, xs, weights, eps, freqs, layout, positions, start):
+    def __init__(self, xs, weights, eps, angles, layout, positions, start):  # angles: of rotary_angles
         n = len(xs)
         if not 1 <= n <= ROTATE_MAX:
             raise ValueError(f"1 to {ROTATE_MAX} tensors, got {n}")
@@ -178,7 +190,6 @@ class _RotateCall:
             if positions.dim() == 2 and B > 1:
                 pos_stride = positions.stride(0)
             pos = positions.data_ptr()
-        freqs = freq_numbers(freqs)
         self.n, self.shapes, self.dtype, self.device = n, shapes, x0.dtype, device
         self.heads = (ctypes.c_int32 * n)(*[s[2] for s in shapes])
         self.strides = (ctypes.c_int64 * (3 * n))(*[s for x in xs for s in _strides(x)])
@@ -187,7 +198,7 @@ class _RotateCall:
         if not -(1 << 63) <= int(start) <= (1 << 63) - N:
             raise ValueError(f"start {start}: positions are 64-bit numbers")
         self.pos = (pos, pos_stride, int(start))
-        self.tail = (B, N, D, eps is not None, float(eps or 0.0), code, _freq_array(freqs), len(freqs), _DTYPES[x0.dtype],
+        self.tail = (B, N, D, eps is not None, float(eps or 0.0), code, *angles, _DTYPES[x0.dtype],
                      _DTYPES[wdtype])
         self.kept = (xs, weights, positions)  # what the pointers point to
 
@@ -245,14 +256,14 @@ def simplicial_norm_rotate_fwd(xs, weights=None, eps=1e-6, freqs=None, layout="h
     position of the pairs that `layout` names: "half" (i, n + i), "pairs" (2 i, 2 i + 1)
     or "axis" (3 i, 3 i + 1: the first two of each 3-component chunk of the determinant
     logits); None: no rotation. Positions: int64 [N] or [B, N], or start, start + 1, ..."""
-    return _RotateCall(xs, weights, eps, freqs, layout, positions, start).forward(out)
+    return _RotateCall(xs, weights, eps, rotary_angles(freqs), layout, positions, start).forward(out)
 
 
 def simplicial_norm_rotate_bwd(xs, dys, weights=None, eps=1e-6, freqs=None, layout="half", positions=None, start=0,
                                weight_grads=True, grads=None):
     """(dxs, dweights) of simplicial_norm_rotate_fwd: lists, the latter with None where
     there is no weight, or all None with weight_grads False."""
-    return _RotateCall(xs, weights, eps, freqs, layout, positions, start).backward(dys, weight_grads, grads)
+    return _RotateCall(xs, weights, eps, rotary_angles(freqs), layout, positions, start).backward(dys, weight_grads, grads)
 
 
 # ---- dot-product attention ----

@@ -80,11 +80,12 @@ def test_angles_are_kept_as_numbers():
     """What is kept of a call's angles is found again, whatever they were given as."""
     want = rotary_freqs(32)
     x = torch.tensor(want, dtype=torch.float64)
-    before = layers_binding._freq_array.cache_info()
-    arrays = {id(layers_binding._freq_array(layers_binding.freq_numbers(f))) for f in (want, list(want), x, list(x), iter(want), x.numpy())}
-    after = layers_binding._freq_array.cache_info()
-    assert len(arrays) == 1 and after.currsize - before.currsize <= 1
-    assert layers_binding.freq_numbers(want) is want and layers_binding.freq_numbers(None) == ()
+    found = [layers_binding.rotary_angles(f) for f in (want, list(want), x, list(x), iter(want), x.numpy())]
+    assert all(f is found[0] for f in found) and tuple(found[0][0]) == want and found[0][1] == 32
+    assert layers_binding.rotary_angles(None)[1] == 0
+    for i in range(100):
+        layers_binding.rotary_angles([torch.tensor(float(i))])
+    assert len(layers_binding._ANGLES) <= 64 and all(type(f) is float for kept in layers_binding._ANGLES for f in kept)
 
 
 def test_weights_of_another_number(stub):

@@ -92,6 +92,6 @@ def test_positions_past_64_bits():
     x = FakeTensor()
     for start in (1 << 63, (1 << 63) - 3, (1 << 64) + 5, -(1 << 63) - 1):
         with pytest.raises(ValueError, match="start"):
-            layers_binding._RotateCall([x], None, 1e-6, None, "half", None, start)
+            layers_binding._RotateCall([x], None, 1e-6, layers_binding.rotary_angles(None), "half", None, start)
     for start in (0, (1 << 63) - 4, -(1 << 63)):
-        layers_binding._RotateCall([x], None, 1e-6, None, "half", None, start)
+        layers_binding._RotateCall([x], None, 1e-6, layers_binding.rotary_angles(None), "half", None, start)

@@ -629,14 +629,17 @@ hipError_t dot_ranges(const DotArgs& a, int2* ranges, hipStream_t st) {
 // that share the other side's blocks; 1 blocks of 32, their wavefronts sharing the other
 // side. Whole blocks move the fewest bytes, but where there are few of them the time is
 // that of the longest one. Measured, forward us of 0 / -1 / 1 (causal): D = 128, units 2048
-// 1138 / 1239 / 1826 (all pairs), 1024: 305 / 345 / 520, 512: 232 / 178 / 262, 256: 111 / 82 / 81 and
-// 38 / 33 / 45, 128: 60 / 47 / 31; D = 64 (twice the workgroups of 32 fit a CU), 1024: 71 / 86 / 88, 512: 55 /
-// 63 / 50, 128: 28 / 24 / 16. Documents make some blocks much longer than others: three of
-// them, units 1024, 457 / 315 / 430.
-int rows_form(int64_t units, int64_t D, bool docs) {
+// 1120 / 1231 / 1825 (all pairs), 1024: 300 / 344 / 519, 512: 135 / 105 / 160, 256: 113 / 84 / 84 and
+// 36 / 32 / 42, 128: 61 / 48 / 31; D = 64 (twice the workgroups of 32 fit a CU), 1024: 235 / 266 / 234 and
+// 128 / 151 / 140, 512: 98 / 79 / 73, 128: 47 / 37 / 17. The same with documents, whose lengths the device
+// alone knows. Two groups shorten the longest walk where they are few and uneven, and cost elsewhere: means of
+// four draws of 1 / 3 / 16 random documents, -1 to 0: units 1024 of 1 x 8192, 16 heads on 4 1.04 / 0.82 / 1.09, 1 x 16384
+// 1.06 / 1.01 / 1.01, 2 x 4096 0.93 / 1.05 / 1.19, 8 x 1024 1.23 / 1.27 / 1.36; units 2048 of 1 x 16384, 16 on 4
+// 1.11 / 1.02 / 1.15, 4 x 4096 1.04 / 1.14 / 1.27.
+int rows_form(int64_t units, int64_t D) {
   if (D <= 64) return units < 640 ? 1 : 0;
   if (units <= 160) return 1;
-  return units < 768 || (docs && units <= 2048) ? -1 : 0;
+  return units < 768 ? -1 : 0;
 }
 
 DotPlan dot_fwd_plan(int64_t B, int64_t Nq, int64_t Nk, int64_t H, int64_t Hkv, int64_t D, int causal, int window, bool docs,
@@ -644,7 +647,7 @@ DotPlan dot_fwd_plan(int64_t B, int64_t Nq, int64_t Nk, int64_t H, int64_t Hkv, 
   DotPlan p = {};
   const bool bf16 = dtype == SA_DTYPE_BF16;
   const int64_t R = H / Hkv * Nq;
-  p.nsplit = bf16 ? rows_form(B * Hkv * ((R + 127) / 128), D, docs) : 1;
+  p.nsplit = bf16 ? rows_form(B * Hkv * ((R + 127) / 128), D) : 1;
   if (p.nsplit == 1) {
     // Keys a row block walks: the parts take 256 of them at least.
     const int64_t units = B * Hkv * ((R + kDotBlock - 1) / kDotBlock);
@@ -664,23 +667,26 @@ DotPlan dot_bwd_plan(int64_t B, int64_t Nq, int64_t Nk, int64_t H, int64_t Hkv, 
   const bool bf16 = dtype == SA_DTYPE_BF16;
   p.nsplit = p.kside = p.ks = 1;
   if (bf16) {
-    p.nsplit = rows_form(rows, D, docs);
+    p.nsplit = rows_form(rows, D);
     // The key side: as the rows where a head has few of them; else `ks` workgroups for a
-    // block of 128 keys, their float32 sums added afterwards, up to about 1024 in all (2048
-    // with documents, which make some key blocks' rows many: three of them, keys 256, R 32768,
-    // ks 4 / 6 / 8: 1008 / 959 / 936 us).
-    // Backward us of (0, ks 1) / (-1, 1) / 1 / (0, ks 2) / 4 / 8 at D = 128: keys 1024 (units of 128)
-    // 976 / 1075 / 1879 / 1076 / 1199 / 1470; 512: 778 / 560 / 1153 / 620 / 691 / 830; 256, R = 4096: 401 / 311 / 356 / 298 / 271 / 352; 256,
-    // R = 32768: 2252 / 1624 / 1595 / 1393 / 1170 / 1103; 32, R = 8192: 601 / 402 / 250 / 342 / 219 / 162; 256, R = 1024: 124 / 98 / 146 /
-    // 118 / 130 / 207; 96, R = 1500: 162 / 118 / 74 / 129 / 109 / 121.
-    if (D <= 64 ? keys < 640 && R <= 8192 : keys <= 128 && R < 2048)
+    // block of 128 keys, their float32 sums added afterwards, up to about 1024 in all; with
+    // documents, which make some key blocks' rows many, and more than 16384 rows 2048 (means of four draws of 1 / 2 / 3 /
+    // 6 / 16 random documents, keys 256 (units of 128), ks 8 to 4: R = 65536 1.01 / 0.73 / 0.77 / 0.82 / 0.86, 32768 of three shapes
+    // 1.03 - 1.05 / 0.81 - 0.83 / 0.78 - 0.84 / 0.89 - 0.92 / 0.95 - 0.99, 16384 1.13 / 0.96 / 0.87 / 1.01 / 1.06, 8192 1.21 / 1.01 /
+    // 1.01 / 1.04 / 1.14).
+    // Backward us of (0, ks 1) / (-1, 1) / 1 / (0, ks 2) / 4 / 8 at D = 128, causal: keys 1024, R = 8192
+    // 1039 / 1080 / 1807 / 1079 / 1201 / 1479; 512, 4096: 391 / 328 / 535 / 333 / 407 / 556; 256, 4096: 355 / 271 / 308 /
+    // 260 / 231 / 318; 256, 32768: 2430 / 1668 / 1721 / 1411 / 996 / 1042; 32, 8192: 565 / 373 / 211 / 313 / 189 / 130;
+    // 256, 1024: 119 / 99 / 127 / 113 / 126 / 209; 96, 1500: 135 / 105 / 78 / 104 / 85 / 96; 64, 2048: 166 / 123 / 87 / 120 /
+    // 93 / 86.
+    if (D <= 64 ? keys < 640 && R <= 8192 : keys <= 128 && R <= 2048)
       p.kside = 1;
     else if (keys >= 768)
       p.kside = 0;
     else if (R <= 2048 || keys >= 384)
       p.kside = -1;
     else
-      p.kside = 0, p.ks = static_cast<int>(std::max<int64_t>(2, std::min<int64_t>(8, (docs ? 2048 : 1024) / keys)));
+      p.kside = 0, p.ks = static_cast<int>(std::max<int64_t>(2, std::min<int64_t>(8, (docs && R > 16384 ? 2048 : 1024) / keys)));
   }
   p.ranges_off = 0;
   p.delta_off = docs ? up256(static_cast<size_t>(B) * ((Nk + kDotBlock - 1) / kDotBlock) * sizeof(int2)) : 0;

@@ -661,14 +661,15 @@ DotPlan dot_fwd_plan(int64_t B, int64_t Nq, int64_t Nk, int64_t H, int64_t Hkv, 
 }
 DotPlan dot_bwd_plan(int64_t B, int64_t Nq, int64_t Nk, int64_t H, int64_t Hkv, int64_t D, int causal, int window, bool docs,
                      int dtype) {
-  (void)causal, (void)window;
   DotPlan p = {};
   const int64_t R = H / Hkv * Nq, rows = B * Hkv * ((R + 127) / 128), keys = B * Hkv * ((Nk + 127) / 128);
+  // Rows that a block of 128 keys sees (keys before a prefix, which a plan does not know of, all).
+  const int64_t seen = window > 0 ? std::min(R, H / Hkv * ((causal ? 1 : 2) * int64_t(window) + 128)) : R;
   const bool bf16 = dtype == SA_DTYPE_BF16;
   p.nsplit = p.kside = p.ks = 1;
   if (bf16) {
     p.nsplit = rows_form(rows, D);
-    // The key side: as the rows where a head has few of them; else `ks` workgroups for a
+    // The key side: as the rows where a block of keys sees few of them; else `ks` workgroups for a
     // block of 128 keys, their float32 sums added afterwards, up to about 1024 in all; with
     // documents, which make some key blocks' rows many, and more than 16384 rows 2048 (means of four draws of 1 / 2 / 3 /
     // 6 / 16 random documents, keys 256 (units of 128), ks 8 to 4: R = 65536 1.01 / 0.73 / 0.77 / 0.82 / 0.86, 32768 of three shapes
@@ -678,15 +679,17 @@ DotPlan dot_bwd_plan(int64_t B, int64_t Nq, int64_t Nk, int64_t H, int64_t Hkv, 
     // 1039 / 1080 / 1807 / 1079 / 1201 / 1479; 512, 4096: 391 / 328 / 535 / 333 / 407 / 556; 256, 4096: 355 / 271 / 308 /
     // 260 / 231 / 318; 256, 32768: 2430 / 1668 / 1721 / 1411 / 996 / 1042; 32, 8192: 565 / 373 / 211 / 313 / 189 / 130;
     // 256, 1024: 119 / 99 / 127 / 113 / 126 / 209; 96, 1500: 135 / 105 / 78 / 104 / 85 / 96; 64, 2048: 166 / 123 / 87 / 120 /
-    // 93 / 86.
-    if (D <= 64 ? keys < 640 && R <= 8192 : keys <= 128 && R <= 2048)
+    // 93 / 86. With a window (rows of a block of keys given): keys 256, 1024 rows 162 / 138 / - / 144 / 169 / 259; 256,
+    // 640: 92 / 82 / - / 95 / 118 / 202; 256, 8704: 791 / 580 / - / 544 / 540 / 596; 128, 1536: 189 / 147 / 125 / 141 /
+    // 120 / 142; D = 64, 256, 1024: 106 / 90 / 78 / 95 / 104 / 119; 376, 640: 84 / 96 / 91 / 91 / 108 / 141.
+    if (D <= 64 ? keys < 640 && seen <= 8192 : keys <= 128 && seen <= 2048)
       p.kside = 1;
     else if (keys >= 768)
       p.kside = 0;
-    else if (R <= 2048 || keys >= 384)
+    else if (seen <= 2048 || keys >= 384)
       p.kside = -1;
     else
-      p.kside = 0, p.ks = static_cast<int>(std::max<int64_t>(2, std::min<int64_t>(8, (docs && R > 16384 ? 2048 : 1024) / keys)));
+      p.kside = 0, p.ks = static_cast<int>(std::max<int64_t>(2, std::min<int64_t>(8, (docs && seen > 16384 ? 2048 : 1024) / keys)));
   }
   p.ranges_off = 0;
   p.delta_off = docs ? up256(static_cast<size_t>(B) * ((Nk + kDotBlock - 1) / kDotBlock) * sizeof(int2)) : 0;

@@ -29,3 +29,14 @@ def test_documents_share_key_blocks_among_more_only_where_rows_are_many():
     for B, N, H, Hkv in ((1, 4096, 8, 8), (4, 2048, 16, 4), (2, 4096, 16, 4)):
         assert _parts(B, N, H, Hkv, 128) == _parts(B, N, H, Hkv, 128, documents=True) == 4
     assert _parts(1, 16384, 8, 2, 128) == 4 and _parts(1, 16384, 8, 2, 128, documents=True) == 8
+
+
+def test_a_window_leaves_a_block_of_keys_few_rows():
+    """None to share among workgroups, whatever the length of the sequence."""
+    assert _parts(1, 4096, 8, 8, 128) == 4 and _parts(1, 4096, 8, 8, 128, window=512) == 0
+    assert _parts(1, 16384, 8, 2, 128, window=300) == 0 and _parts(1, 16384, 8, 2, 128, window=2000) == 4
+    assert _parts(1, 16384, 8, 2, 128, window=300, causal=False) == 4
+    assert _parts(1, 12000, 8, 2, 64) > 0 == _parts(1, 12000, 8, 2, 64, window=900)
+    # a window that hides nothing is none
+    for N in (4096, 16384):
+        assert _parts(1, N, 8, 2, 128, window=N) == _parts(1, N, 8, 2, 128)

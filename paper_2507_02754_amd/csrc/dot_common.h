@@ -37,18 +37,22 @@ struct DotMask {
   }
 };
 
-// Positions p0 .. p1 of a block's rows or of its keys, and the range of their document
-// numbers.
+// Positions p0 .. p1 of a block's rows or of its keys, the range of their document numbers and
+// whether padding is among them. Padding has no part in the range: with its negative number a block
+// at the end of the last document would span, and walk, all documents (N=8192, 16 heads on 4, D=128,
+// causal, documents of 2876, 2182 and 2762, forward 413 us, so 207).
 struct DotSpan {
   int p0, p1, dmin, dmax;
-  __device__ __forceinline__ DotSpan(const DotMask& m, int lo, int hi) : p0(lo), p1(hi), dmin(0), dmax(0) {
+  int pad;  // negative: with padding
+  __device__ __forceinline__ DotSpan(const DotMask& m, int lo, int hi) : p0(lo), p1(hi), dmin(0), dmax(0), pad(0) {
     if (m.docs && hi >= 0 && lo < m.L) {
       const int last = min(hi, m.L - 1) / kDotBlock;
       const int2 r = m.ranges[max(lo, 0) / kDotBlock];
-      dmin = r.x, dmax = r.y;
+      dmin = max(r.x, ~r.x), dmax = r.y, pad = r.x;
       for (int t = max(lo, 0) / kDotBlock + 1; t <= last; ++t) {
         const int2 s = m.ranges[t];
-        dmin = min(dmin, s.x), dmax = max(dmax, s.y);
+        dmin = min(dmin, max(s.x, ~s.x)), dmax = max(dmax, s.y);
+        pad |= s.x;
       }
     }
   }
@@ -65,7 +69,7 @@ __device__ __forceinline__ bool dot_full(const DotMask& m, const DotSpan& q, con
   const bool near = (!m.causal || k.p1 <= q.p0) &&
                     (m.window == 0 || (q.p1 - k.p0 < m.window && (m.causal || k.p1 - q.p0 < m.window)));
   return (near || k.p1 < m.prefix) && k.p1 < m.L && q.p0 >= 0 &&
-         (!m.docs || (k.dmin == k.dmax && q.dmin == q.dmax && k.dmin == q.dmin && k.dmin >= 0));
+         (!m.docs || (k.dmin == k.dmax && q.dmin == q.dmax && k.dmin == q.dmin && (k.pad | q.pad) >= 0));
 }
 // Key blocks that any of the rows may see: [lo, hi).
 __device__ __forceinline__ void key_blocks(const DotMask& m, const DotSpan& q, int& lo, int& hi) {

@@ -575,16 +575,20 @@ __global__ __launch_bounds__(64 * kWavesOf<D>, D <= 64 ? 2 : 1) void dot_dkv_f32
   }
 }
 
-// Smallest and largest document number of 32 positions, one thread each.
+// Smallest and largest document number of 32 positions (DotArgs::ranges), one thread each.
 __global__ void dot_ranges_kernel(const int* docs, int2* ranges, int B, int Nk) {
   const int blocks = (Nk + kDotBlock - 1) / kDotBlock;
   const int64_t at = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
   if (at >= static_cast<int64_t>(B) * blocks) return;
   const int b = static_cast<int>(at / blocks), j0 = static_cast<int>(at - static_cast<int64_t>(b) * blocks) * kDotBlock;
   const int* d = docs + static_cast<int64_t>(b) * Nk;
-  int lo = d[j0], hi = lo;
-  for (int j = j0 + 1; j < min(j0 + kDotBlock, Nk); ++j) lo = min(lo, d[j]), hi = max(hi, d[j]);
-  ranges[at] = make_int2(lo, hi);
+  int lo = 0x7fffffff, hi = -1;
+  bool pad = false;
+  for (int j = j0; j < min(j0 + kDotBlock, Nk); ++j) {
+    pad |= d[j] < 0;
+    lo = d[j] < 0 ? lo : min(lo, d[j]), hi = max(hi, d[j]);
+  }
+  ranges[at] = make_int2(pad ? ~lo : lo, hi);
 }
 
 template <int D>

@@ -73,7 +73,8 @@ struct DotArgs {
   const int* docs;
   const int* prefix;
   const int* lens;
-  // Smallest and largest document number of every 32 positions, [B, ceil(Nk / 32)].
+  // Smallest and largest document number of every 32 positions, [B, ceil(Nk / 32)], padding apart: with
+  // padding among them the complement of the smallest (2^31 - 1 and -1 where there is none).
   const int2* ranges;
   float* delta;  // backward: Delta [B, H, Nq] (bf16: what dot_bwd.hip keeps of the rows)
   // Workgroups over rows. Forward: parts of the key axis that workgroups of 32 rows take; bf16

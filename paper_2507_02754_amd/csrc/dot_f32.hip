@@ -635,15 +635,18 @@ hipError_t dot_ranges(const DotArgs& a, int2* ranges, hipStream_t st) {
 // that of the longest one. Measured, forward us of 0 / -1 / 1 (causal): D = 128, units 2048
 // 1120 / 1231 / 1825 (all pairs), 1024: 300 / 344 / 519, 512: 135 / 105 / 160, 256: 113 / 84 / 84 and
 // 36 / 32 / 42, 128: 61 / 48 / 31; D = 64 (twice the workgroups of 32 fit a CU), 1024: 235 / 266 / 234 and
-// 128 / 151 / 140, 512: 98 / 79 / 73, 128: 47 / 37 / 17. The same with documents, whose lengths the device
-// alone knows. Two groups shorten the longest walk where they are few and uneven, and cost elsewhere: means of
-// four draws of 1 / 3 / 16 random documents, -1 to 0: units 1024 of 1 x 8192, 16 heads on 4 1.04 / 0.82 / 1.09, 1 x 16384
-// 1.06 / 1.01 / 1.01, 2 x 4096 0.93 / 1.05 / 1.19, 8 x 1024 1.23 / 1.27 / 1.36; units 2048 of 1 x 16384, 16 on 4
-// 1.11 / 1.02 / 1.15, 4 x 4096 1.04 / 1.14 / 1.27.
-int rows_form(int64_t units, int64_t D) {
+// 128 / 151 / 140, 512: 98 / 79 / 73, 128: 47 / 37 / 17. With documents,
+// whose lengths the device alone knows, a block at the end of one is masked along its whole walk, which two
+// groups halve: that gains where few heads have long sequences. Means of four draws of 1 / 3 / 16 random documents
+// and padding, -1 to 0: units 768 of 1 x 12288, 8 heads (96 blocks a head) 0.66 / 0.76 / 0.93, of 1 x 6144, 16 heads on 4 (192)
+// 0.68 / 0.73 / 1.08; 1024 of 1 x 8192, 16 on 4 (256) 0.79 / 0.82 / 1.10, with a cap 0.98 / 0.93 / 1.12, of 1 x 16384, 8 heads (128)
+// 0.78 / 0.89 / 1.02, with a cap 0.94 / 1.01 / 1.08, of 1 x 8192, 16 heads (64) 0.98 / 0.97 / 1.15, with a cap 1.06 / 1.03 / 1.18,
+// of 2 x 4096 (32) 1.00 / 1.07 / 1.20, 8 x 1024 (8) 1.25 / 1.29 / 1.45; 1280 of 1 x 10240, 16 on 4 0.94 / 0.92 / 1.05, with a cap 1.19 /
+// 1.05 / 1.06; 1536 of 1 x 12288, 16 on 4 1.07 / 0.95 / 1.12; 2048 of 1 x 16384, 16 on 4 1.13 / 1.03 / 1.17.
+int rows_form(int64_t units, int64_t heads, int64_t D, bool docs) {
   if (D <= 64) return units < 640 ? 1 : 0;
   if (units <= 160) return 1;
-  return units < 768 ? -1 : 0;
+  return units < 768 || (docs && units < 1152 && units >= 96 * heads) ? -1 : 0;
 }
 
 DotPlan dot_fwd_plan(int64_t B, int64_t Nq, int64_t Nk, int64_t H, int64_t Hkv, int64_t D, int causal, int window, bool docs,
@@ -651,7 +654,7 @@ DotPlan dot_fwd_plan(int64_t B, int64_t Nq, int64_t Nk, int64_t H, int64_t Hkv, 
   DotPlan p = {};
   const bool bf16 = dtype == SA_DTYPE_BF16;
   const int64_t R = H / Hkv * Nq;
-  p.nsplit = bf16 ? rows_form(B * Hkv * ((R + 127) / 128), D) : 1;
+  p.nsplit = bf16 ? rows_form(B * Hkv * ((R + 127) / 128), B * Hkv, D, docs) : 1;
   if (p.nsplit == 1) {
     // Keys a row block walks: the parts take 256 of them at least.
     const int64_t units = B * Hkv * ((R + kDotBlock - 1) / kDotBlock);
@@ -672,13 +675,13 @@ DotPlan dot_bwd_plan(int64_t B, int64_t Nq, int64_t Nk, int64_t H, int64_t Hkv, 
   const bool bf16 = dtype == SA_DTYPE_BF16;
   p.nsplit = p.kside = p.ks = 1;
   if (bf16) {
-    p.nsplit = rows_form(rows, D);
+    p.nsplit = rows_form(rows, B * Hkv, D, docs);
     // The key side: as the rows where a block of keys sees few of them; else `ks` workgroups for a
     // block of 128 keys, their float32 sums added afterwards, up to about 1024 in all; with
     // documents, which make some key blocks' rows many, and more than 16384 rows 2048 (means of four draws of 1 / 2 / 3 /
-    // 6 / 16 random documents, keys 256 (units of 128), ks 8 to 4: R = 65536 1.01 / 0.73 / 0.77 / 0.82 / 0.86, 32768 of three shapes
-    // 1.03 - 1.05 / 0.81 - 0.83 / 0.78 - 0.84 / 0.89 - 0.92 / 0.95 - 0.99, 16384 1.13 / 0.96 / 0.87 / 1.01 / 1.06, 8192 1.21 / 1.01 /
-    // 1.01 / 1.04 / 1.14).
+    // 6 / 16 random documents, keys 256 (units of 128), ks 8 to 4: R = 65536 1.02 / 0.76 / 0.78 / 0.83 / 0.85, 32768 of three shapes
+    // 1.04 - 1.05 / 0.81 - 0.84 / 0.78 - 0.86 / 0.89 - 0.92 / 0.95 - 0.99, 16384 1.11 / 0.97 / 0.87 / 1.00 / 1.06, 8192 1.21 / 1.00 /
+    // 1.01 / 1.04 / 1.13).
     // Backward us of (0, ks 1) / (-1, 1) / 1 / (0, ks 2) / 4 / 8 at D = 128, causal: keys 1024, R = 8192
     // 1039 / 1080 / 1807 / 1079 / 1201 / 1479; 512, 4096: 391 / 328 / 535 / 333 / 407 / 556; 256, 4096: 355 / 271 / 308 /
     // 260 / 231 / 318; 256, 32768: 2430 / 1668 / 1721 / 1411 / 996 / 1042; 32, 8192: 565 / 373 / 211 / 313 / 189 / 130;

@@ -39,7 +39,9 @@ extern "C" {
  *         are then functions of position differences alone
  * nfreq is at most D / 2 (D / 3 for SA_ROTATE_AXIS); 0: no rotation. Angles are
  * reduced in float64, so far positions keep their fraction of a turn. A row of
- * zeros with eps = 0 gives zeros (and zero gradients).
+ * zeros with eps = 0 gives zeros (and zero gradients). Squares and their sum are float32:
+ * values past 2^60 may overflow there (the norm is then infinite and the row 0), rows below 2^-60
+ * may be taken for zeros where eps = 0.
  *   count       tensors, 1 .. SA_ROTATE_MAX
  *   x[t]        [B, N, heads[t], D], dtype, element strides
  *               strides[3 t .. 3 t + 2] of (batch, position, head)
@@ -92,7 +94,9 @@ int simplicial_norm_rotate_bwd(int32_t count, const void* const* x, const int64_
  * marks padding, which sees nothing and is not seen). Document numbers may come
  * in any order. A query that sees no key (p < 0 among them) has O = 0 and LSE =
  * -inf. Values outside what a query sees do not reach it, infinities and NaN
- * included. Query head h reads head h / (H / Hkv) of k and v.
+ * included. Query head h reads head h / (H / Hkv) of k and v. Scores, statistics and sums are
+ * float32; SA_DTYPE_BF16 rounds P (and the backward P and dS) to bf16 for its products with V (K, Q
+ * and dO), SA_DTYPE_F32 rounds nothing below float32.
  *   q           [B, Nq, H, D], strides q_sb, q_sn, q_sh (batch, position, head)
  *   k, v        [B, Nk, Hkv, D], strides likewise
  *   out         [B, Nq, H, D] contiguous, dtype;  lse [B, H, Nq] float32

@@ -18,10 +18,11 @@
 // sums added at the end in a fixed order.
 //
 // Bound by the products and, on the key side, by registers (K, V, dK and dV of 32 keys a
-// wavefront): B=1 H=32 N=8192 D=128, all pairs, query side 1.5 ms (1.6 TFLOP, 1080 TFLOP/s), key side
-// 2.4 - 2.6 ms (2.2 TFLOP, 850 - 910 TFLOP/s); three documents with a cap, 16 heads on 4: 412 and 524 + 58 us.
+// wavefront): B=1 H=32 N=8192 D=128, all pairs, query side 1.53 - 1.56 ms (1.6 TFLOP, 1080 - 1054 TFLOP/s), key
+// side 2.4 - 2.6 ms (2.2 TFLOP, 910 - 850 TFLOP/s); three documents with a cap, 16 heads on 4: 401 and 508 + 66 us.
 //
-// P and dS are rounded to bf16 for their products, as the operands are; everything
+// P and dS are rounded to bf16 for their products, as the operands are (which puts gradients of random
+// values off by 0.0024, relative norm, where rounding them alone takes 0.0017); everything
 // else is float32. Rows or keys whose sums met an infinity or NaN of a masked pair are
 // formed again by themselves (dot_mfma.h).
 #include "dot_mfma.h"

@@ -12,10 +12,12 @@
 // from L1 / L2 straight into registers: at 1/16 of the bf16 rate the products, not
 // the loads, take the time.
 //
-// Measured, B=1 H=4 N=2000 D=64 causal with a prefix of 200: forward 41 us, dq 70, dk and dv
-// 114, 32 TFLOP/s of the 7.2 GFLOP that forward and backward need (a large product of the
+// Measured, B=1 H=4 N=2000 D=64 causal with a prefix of 200: forward 42 us, dq 71, dk and dv
+// 115, 32 TFLOP/s of the 7.2 GFLOP that forward and backward need (a large product of the
 // library's runs at 154). With 252 workgroups of rows and of keys, the longest one's walk of
-// dependent products is the time.
+// dependent products is the time, on the key side with 107 registers spilled (both row operands and a
+// column operand at once). One token over 8 caches of up to 16384 keys, 4 heads of 128: 121 us (2.8 TB/s) and 13
+// to join; N=3000 H=8 D=128: 277 us forward, 852 backward (67 and 54 TFLOP/s).
 //
 // Each block's products start from zero and are added to the running sums, so that
 // sums over a long axis round once per 32 terms. Operand layouts as in f32.hip: a row

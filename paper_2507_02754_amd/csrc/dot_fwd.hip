@@ -18,14 +18,16 @@
 //
 // The maximum is raised lazily: P is formed with the present m, and only where a
 // row's block sum leaves (0, 2^16] is m raised to the block's maximum and P formed
-// again. The output is divided by the sum of the probabilities as rounded to bf16
-// for the product with V (it is then a weighted mean of V's rows whatever the
-// rounding); LSE takes the sum of the unrounded ones.
+// again. P is rounded to bf16 for the product with V, whose other operand is bf16: of random
+// values each term p v is then off by as much as the output's own rounding takes from it, 0.0024 in
+// all (relative norm) for 0.0017; a product of float32 would run at an eighth of the rate. The output
+// is divided by the sum of the probabilities as rounded (it is then a weighted mean of V's rows
+// whatever the rounding); LSE takes the sum of the unrounded ones.
 //
 // Bound by the matrix products and the exponentials beside them: B=1 H=32 N=8192 D=128, all
-// pairs, 1138 us (966 TFLOP/s; an 8192^3 product of the library's runs at 1173); causal, 16 heads
-// on 4, 297 us (925). Where the workgroups do not outnumber the CUs, by the longest row's
-// walk: N=4096, 8 heads, a prefix of 1024, 84 us (419 TFLOP/s). dot_few_kernel by the cache: 8 sequences of up to 16384
+// pairs, 1107 - 1173 us (993 - 937 TFLOP/s from box to box; an 8192^3 product of the library's runs at
+// 1173); causal, 16 heads on 4, 296 - 313 us (929 - 878). Where the workgroups do not outnumber the CUs, by the longest row's
+// walk: N=4096, 8 heads, a prefix of 1024, 83 us (419 TFLOP/s). dot_few_kernel by the cache: 8 sequences of up to 16384
 // keys, 4 heads, 168 MB in 34 us (4.9 TB/s), and 5 us to join the parts.
 //
 // With a distance bias the blocks are walked from the nearest keys back: the scores fall

@@ -33,7 +33,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const uint16_t* p, int
 // How scores are capped. 1 - 2 / (exp(2 x) + 1) is tanh to 2^-23 absolutely, the score then to
 // cap 2^-22: up to kCapShort 1/8 of the rounding of P to bf16. Larger caps, whose scores
 // mostly lie where tanh is near its argument, take tanhf (B=1 H=16 Hkv=4 N=8192 D=128
-// causal, cap 0 / 50 / 2000: forward 297 / 344 / 455 us, backward 999 / 1182 / 1864).
+// causal, cap 0 / 50 / 2000: forward 313 / 384 / 467 us, backward 1041 / 1229 / 1799).
 enum Cap { kNoCap, kShortCap, kLargeCap };
 constexpr float kCapShort = 1024.f;
 

@@ -11,9 +11,10 @@
 // tokens are found without a second read. A row longer than a workgroup holds, or
 // one of few rows, is cut into slices, joined by a second small kernel.
 // Measured (bf16): 8192 rows of 65536 forward 208 us (5.2 TB/s, the rate of a large copy),
-// gradient 348 us (2.1 GB, 6.2 TB/s); 2047 rows of 32000 with their top 5, 42 us (3.1 TB/s: the
-// exponentials and the search, of rows that one workgroup each takes in one wave of the
-// grid); 8 rows of 50001 with their top 8, 7 + 6 us (two launches' latency).
+// gradient 348 us (2.1 GB, 6.2 TB/s); 4096 rows of 65536 in float32 the same, 204 and 350 us; 2047
+// rows of 32000 with their top 5, 39 - 42 us (3.3 - 3.1 TB/s: a row's read, exponentials and search follow one
+// another, three workgroups of 512 threads a CU, and nothing of the next row is on its way meanwhile);
+// 8 rows of 50001 with their top 8, 7 + 6 us (two launches' latency).
 //
 // The top tokens: the K-th largest of the lanes' maxima in any wavefront is no
 // larger than the K-th largest logit, so everything at or above the largest such

@@ -17,8 +17,9 @@
 //
 // Measured, bf16 (a large copy runs at 5.2 TB/s): two tensors of B=2 N=8192 H=8 D=128, half layout
 // with norm and weights, forward 31 us (134 MB, 4.3 TB/s), backward 44 + 4 us (201 MB, 4.2 TB/s);
-// axis layout, 24 heads of 6001 positions in three tensors, 21 and 30 us (74 and 111 MB, 3.5 and 3.7 TB/s:
-// the shuffles and selects of chunks that cross lanes); one token of 4 sequences 6 us, a
+// pairs 34 and 46 + 4; float32 60 and 95 + 5 (4.5 and 4.1 TB/s);
+// axis layout, 24 heads of 6001 positions in three tensors, 21 - 22 and 30 - 31 us (74 and 111 MB, 3.5 - 3.3 and 3.7 - 3.6 TB/s:
+// the shuffles and selects of chunks that cross lanes, as 3 does not divide 16); one token of 4 sequences 6 us, a
 // launch's latency and the float64 angles.
 #include "layers_internal.h"
 #include "mfma_common.h"

@@ -154,7 +154,8 @@ def dot_attention(q, k, v, scale=None, causal=True, window=0, softcap=0.0, slope
 
     Arguments as simplicial_dot_attn_fwd: q [B, Nq, H, D], k and v [B, Nk, Hkv, D], the
     queries the last Nq of the keys' positions; score cap, distance bias, and causal,
-    window, prefix and document masks. The options are not differentiated."""
+    window, prefix and document masks. The options are not differentiated. bfloat16 tensors
+    have their probabilities rounded to bfloat16 for the products, float32 ones do not."""
     options = (scale, causal, window, softcap, slopes, documents, prefix, k_lens)
     _refuse_tangents("dot_attention", q, k, v, scale, softcap, slopes)
     _refuse_gradients("scale, softcap and slopes", scale, softcap, slopes)

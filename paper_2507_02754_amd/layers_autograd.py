@@ -103,7 +103,8 @@ def norm_rotate(xs, weights=None, eps=1e-6, freqs=None, layout="half", positions
 
     xs[t] is [B, N, heads_t, D]; arguments as simplicial_norm_rotate_fwd, whose results
     are returned as a tuple. eps = 0 without weights is the L2 norm scaled by sqrt(D). A
-    weight is given for every tensor or for none."""
+    weight is given for every tensor or for none. eps and freqs are not differentiated (refused
+    where they ask for a gradient)."""
     xs, weights = list(xs), None if weights is None else list(weights)
     _refuse_tangents("norm_rotate", *xs, *(weights or ()))
 
@@ -154,8 +155,9 @@ def dot_attention(q, k, v, scale=None, causal=True, window=0, softcap=0.0, slope
 
     Arguments as simplicial_dot_attn_fwd: q [B, Nq, H, D], k and v [B, Nk, Hkv, D], the
     queries the last Nq of the keys' positions; score cap, distance bias, and causal,
-    window, prefix and document masks. The options are not differentiated. bfloat16 tensors
-    have their probabilities rounded to bfloat16 for the products, float32 ones do not."""
+    window, prefix and document masks. The options are not differentiated (those that ask for
+    a gradient are refused). bfloat16 tensors have their probabilities rounded to bfloat16 for
+    the products, float32 ones do not."""
     options = (scale, causal, window, softcap, slopes, documents, prefix, k_lens)
     _refuse_tangents("dot_attention", q, k, v, scale, softcap, slopes)
     _refuse_gradients("scale, softcap and slopes", scale, softcap, slopes)
